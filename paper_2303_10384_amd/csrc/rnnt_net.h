@@ -1,0 +1,237 @@
+// Shared by the operators between an encoder and the loss (include/rnnt_network_mi355x.h):
+// element access of any width, the gate and activation functions, the random numbers of
+// dropout, and the host's checks and workspaces.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "rnnt_device.h"
+#include "rnnt_network_mi355x.h"
+
+namespace rnnt {
+
+// ---- VEC consecutive elements as floats -------------------------------------
+// One access of VEC * sizeof(T) bytes (2, 4, 8, 16, or 32 as two of 16), aligned to itself.
+
+template <typename T, int VEC>
+struct Pack {
+  static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
+  static constexpr int kWords = (kBytes + 3) / 4;
+  uint32_t w[kWords];
+
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kBytes == 2) {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
+    } else if constexpr (kBytes == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (kBytes == 8) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      w[0] = v.x;
+      w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) {
+        const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+        w[4 * i] = v.x;
+        w[4 * i + 1] = v.y;
+        w[4 * i + 2] = v.z;
+        w[4 * i + 3] = v.w;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (kBytes == 2) {
+      *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(w[0]);
+    } else if constexpr (kBytes == 4) {
+      *reinterpret_cast<uint32_t*>(p) = w[0];
+    } else if constexpr (kBytes == 8) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i)
+        reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    if constexpr (kBytes == 2) f[0] = ElemTraits<T>::from_bits(w[0]);
+    else ElemTraits<T>::template unpack_words<kWords>(w, f);
+  }
+  __device__ __forceinline__ void set(const float* f) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) w[i] = __float_as_uint(f[i]);
+    } else if constexpr (kBytes == 2) {
+      T t;
+      ElemTraits<T>::store1(&t, f[0]);
+      w[0] = t.bits;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC / 2; ++i) w[i] = pack2(f[2 * i], f[2 * i + 1]);
+    }
+  }
+  __device__ static __forceinline__ uint32_t pack2(float a, float b) {
+    if constexpr (__is_same(T, f16_t)) return pack2_f16(a, b);
+    else return pack2_bf16(a, b);
+  }
+};
+
+// ---- functions of one float ---------------------------------------------------
+
+// e^-y for y >= 0 within 2 ulp: the product with log2 e in two parts, so that a large y does
+// not cost its digits (|y| log2 e rounded alone would be off by up to 5e-6 of the result at
+// y = 80).  A y past 104, infinity included, gives 0; NaN stays.
+__device__ __forceinline__ float exp_neg(float y) {
+  y = y > 104.f ? 104.f : y;
+  const float t = -y * kLog2eF;
+  const float lo = __builtin_fmaf(-y, kLog2eF, -t) - y * 1.925963033500e-8f;  // log2 e - float(log2 e)
+  const float r = fast_exp2(t);
+  return __builtin_fmaf(r, lo * kLn2F, r);
+}
+
+// a = sigmoid(z) and g = 1 - a = sigmoid(-z), each to float32's relative accuracy (1 - a as a
+// difference would lose it where the gate is nearly open).
+__device__ __forceinline__ void gate(float z, float& a, float& g) {
+  const float e = exp_neg(__builtin_fabsf(z));
+  const float big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
+  a = z < 0.f ? small : big;
+  g = z < 0.f ? big : small;
+}
+
+template <int ACT>
+struct Activation;
+
+template <>
+struct Activation<RNNT_ACT_RELU> {
+  __device__ static __forceinline__ float value(float s) { return s < 0.f ? 0.f : s; }  // NaN stays
+  __device__ static __forceinline__ float slope(float s) { return s > 0.f ? 1.f : 0.f; }
+};
+
+// tanh s = (1 - u) / (1 + u) and 4u / (1 + u)^2 with u = e^-2|s|; below 0.3, where 1 - u
+// loses digits, the odd series through s^9 (the next term is 5e-8 of the value there).
+template <>
+struct Activation<RNNT_ACT_TANH> {
+  __device__ static __forceinline__ float value(float s) {
+    const float y = __builtin_fabsf(s), q = s * s;
+    const float u = exp_neg(2.f * y);
+    const float big = __builtin_copysignf((1.f - u) * __builtin_amdgcn_rcpf(1.f + u), s);
+    float p = __builtin_fmaf(q, 62.f / 2835.f, -17.f / 315.f);
+    p = __builtin_fmaf(q, p, 2.f / 15.f);
+    p = __builtin_fmaf(q, p, -1.f / 3.f);
+    return y < 0.3f ? __builtin_fmaf(q * p, s, s) : big;
+  }
+  __device__ static __forceinline__ float slope(float s) {
+    const float u = exp_neg(2.f * __builtin_fabsf(s)), r = __builtin_amdgcn_rcpf(1.f + u);
+    return 4.f * u * r * r;
+  }
+};
+
+// ---- random numbers -----------------------------------------------------------
+
+// Philox4x32 (Salmon et al., SC 2011): a round multiplies two of the counter's four words by
+// constants into 64 bits and folds the other two and the key, which advances by the Weyl
+// constants, into the high halves.  Seven rounds are the fewest that the paper finds to pass
+// every statistical test of its battery; the customary ten cost 3/7 more, and the rounds'
+// multiplies (quarter rate) are what the dropout of 16-bit data would wait for.
+struct Rng {
+  uint32_t seed_lo, seed_hi, offset_lo, offset_hi;
+};
+
+__device__ __forceinline__ Rng load_rng(const int64_t* p) {
+  const uint64_t s = static_cast<uint64_t>(p[0]), o = static_cast<uint64_t>(p[1]);
+  return Rng{static_cast<uint32_t>(s), static_cast<uint32_t>(s >> 32), static_cast<uint32_t>(o),
+             static_cast<uint32_t>(o >> 32)};
+}
+
+__device__ __forceinline__ uint4 random_block(const Rng& g, uint64_t block) {
+  uint32_t c0 = static_cast<uint32_t>(block), c1 = static_cast<uint32_t>(block >> 32);
+  uint32_t c2 = g.offset_lo, c3 = g.offset_hi, k0 = g.seed_lo, k1 = g.seed_hi;
+#pragma unroll
+  for (int r = 0; r < 7; ++r) {
+    const uint64_t p0 = static_cast<uint64_t>(c0) * 0xD2511F53u, p1 = static_cast<uint64_t>(c2) * 0xCD9E8D57u;
+    c0 = static_cast<uint32_t>(p1 >> 32) ^ c1 ^ k0;
+    c1 = static_cast<uint32_t>(p1);
+    c2 = static_cast<uint32_t>(p0 >> 32) ^ c3 ^ k1;
+    c3 = static_cast<uint32_t>(p0);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return make_uint4(c0, c1, c2, c3);
+}
+
+// the 16-bit number of element i (0..7) of a block
+__device__ __forceinline__ uint32_t random16(const uint4& b, int i) {
+  const uint32_t w = i < 4 ? (i < 2 ? b.x : b.y) : (i < 6 ? b.z : b.w);
+  return (i & 1) ? w >> 16 : w & 0xffffu;
+}
+
+// dropout by numbers below `threshold`; kept elements are multiplied by `scale`
+struct DropParams {
+  uint32_t threshold;  // 0: nothing is dropped
+  float scale;
+  const int64_t* rng;  // {seed, offset} on the device, read when threshold > 0
+};
+
+// ---- host ---------------------------------------------------------------------
+
+constexpr int64_t kMaxRows = 0x7fffffff;
+
+inline size_t net_align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+inline bool net_dtype_known(int dt) { return dt == RNNT_DTYPE_F32 || dt == RNNT_DTYPE_BF16 || dt == RNNT_DTYPE_F16; }
+inline int64_t net_elem_bytes(int dt) { return dt == RNNT_DTYPE_F32 ? 4 : 2; }
+inline bool multiple_of(int64_t bytes, const void* p) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// p in [0, 1) as a threshold of 16-bit numbers; false for any other p (NaN included).
+inline bool drop_params(double p, const int64_t* rng, DropParams* out) {
+  if (!(p >= 0.0 && p < 1.0)) return false;
+  const double q = __builtin_rint(p * 65536.0);
+  out->threshold = q > 65535.0 ? 65535u : static_cast<uint32_t>(q);
+  out->scale = static_cast<float>(65536.0 / (65536.0 - out->threshold));
+  out->rng = rng;
+  return true;
+}
+
+// The caller's workspace, or one taken for the call, stream-ordered.  None is taken for a stream
+// under capture: a graph of several calls, each with an allocation and a free of its own, has
+// faulted when it was replayed, so a captured call brings its workspace.
+struct NetWorkspace {
+  char* ptr = nullptr;
+  void* owned = nullptr;
+  hipStream_t stream = nullptr;
+  ~NetWorkspace() {
+    if (owned) (void)hipFreeAsync(owned, stream);
+  }
+  rnnt_status_t take(void* given, size_t given_bytes, size_t need, hipStream_t s) {
+    if (given && given_bytes < need) return RNNT_ERR_WORKSPACE;
+    if (given && !multiple_of(256, given)) return RNNT_ERR_ALIGNMENT;
+    ptr = static_cast<char*>(given);
+    if (!ptr && need > 0) {
+      hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+      if (hipStreamIsCapturing(s, &capture) != hipSuccess) return RNNT_ERR_HIP;
+      if (capture != hipStreamCaptureStatusNone) return RNNT_ERR_WORKSPACE;
+      if (hipMallocAsync(&owned, need, s) != hipSuccess) return RNNT_ERR_HIP;
+      stream = s;
+      ptr = static_cast<char*>(owned);
+    }
+    return RNNT_OK;
+  }
+};
+
+inline rnnt_status_t launched() { return hipGetLastError() == hipSuccess ? RNNT_OK : RNNT_ERR_HIP; }
+
+// f called with a value of the dtype's element type
+template <typename F>
+rnnt_status_t with_dtype(rnnt_dtype_t dt, F&& f) {
+  switch (dt) {
+    case RNNT_DTYPE_F32: return f(float{});
+    case RNNT_DTYPE_BF16: return f(bf16_t{});
+    default: return f(f16_t{});
+  }
+}
+
+}  // namespace rnnt

@@ -1,0 +1,155 @@
+"""The network operators without a GPU: the C-ABI's exports and refusals (every call below is
+turned down before any HIP call), workspace sizes, and the binding's checks."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = open(os.path.join(ROOT, "include", "rnnt_network_mi355x.h")).read()
+FAKE = 1 << 20  # aligned, never dereferenced
+vp = ctypes.c_void_p
+
+
+@pytest.fixture(scope="module")
+def net():
+    from paper_2303_10384_amd import binding, network
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_2303_10384_amd import build
+        build.build(verbose=False)
+    return network
+
+
+def test_header_and_exports(net):
+    src = re.sub(r"/\*.*?\*/", "", HEADER, flags=re.S)
+    names = sorted(set(re.findall(r"\b(rnnt_[a-z_0-9]+)\s*\(", src)))
+    assert names == sorted(net.EXPORTED)
+    lib = net._library()
+    for name in names:
+        assert hasattr(lib, name), name
+    assert int(re.search(r"#define RNNT_RECURRENCE_STATE_STEPS (\d+)", HEADER).group(1)) == net.STATE_STEPS
+
+
+def call(fn, defaults, over):
+    """fn on `defaults` (name -> value, in order) with some replaced."""
+    args = dict(defaults)
+    for k, v in over.items():
+        assert k in args, k
+        args[k] = v
+    return fn(*args.values())
+
+
+def test_embedding_refusals(net):
+    lib, S = net._library(), net.EmbeddingShape
+    ok = S(2, 3, 7, 5, 0, 0)
+    fwd = {"labels": FAKE, "lens": FAKE, "shape": ok, "weight": FAKE, "scale": 1.0, "out": FAKE, "stream": None}
+    for shape, want in ((S(0, 3, 7, 5, 0, 0), 2), (S(2, -1, 7, 5, 0, 0), 2), (S(2, 3, 0, 5, -1, 0), 2),
+                        (S(2, 3, 7, 0, 0, 0), 2), (S(2, 3, 7, 5, 7, 0), 2), (S(2, 3, 7, 5, -2, 0), 2),
+                        (S(2, 3, 7, 5, 0, 3), 4), (S(1 << 16, 1 << 15, 7, 5, -1, 0), 9)):
+        assert call(lib.rnnt_label_embedding, fwd, {"shape": shape}) == want
+        assert lib.rnnt_label_embedding_grad_workspace_bytes(shape) == 0
+    for over, want in (({"labels": None}, 1), ({"weight": None}, 1), ({"out": None}, 1), ({"weight": FAKE + 2}, 7),
+                       ({"out": FAKE + 1}, 7)):
+        assert call(lib.rnnt_label_embedding, fwd, over) == want
+    assert call(lib.rnnt_label_embedding, fwd, {"shape": S(2, 0, 7, 5, -1, 0), "labels": None, "out": None}) == 0
+    need = lib.rnnt_label_embedding_grad_workspace_bytes(ok)
+    assert need > 0 and need % 256 == 0
+    bwd = {"labels": FAKE, "lens": FAKE, "shape": ok, "dout": FAKE, "scale": 1.0, "dweight": FAKE, "ws": FAKE,
+           "bytes": need - 1, "stream": None}
+    for over, want in (({}, 6), ({"dout": None}, 1), ({"dweight": None}, 1), ({"dout": FAKE + 2}, 7),
+                       ({"ws": FAKE + 16, "bytes": need}, 7), ({"labels": None}, 1)):
+        assert call(lib.rnnt_label_embedding_grad, bwd, over) == want
+
+
+def test_recurrence_refusals(net):
+    lib, S = net._library(), net.RecurrenceShape
+    ok = S(2, 40, 5, 0, 200, 5, 200, 5)
+    need = lib.rnnt_recurrence_workspace_bytes(ok)
+    assert need > 0 and need % 256 == 0
+    assert lib.rnnt_recurrence_states_bytes(ok) == 2 * 3 * 5 * 4
+    fwd = {"x": FAKE, "z": FAKE, "shape": ok, "lens": FAKE, "h0": FAKE, "h": FAKE, "last": FAKE, "states": FAKE,
+           "ws": FAKE, "bytes": need - 1, "stream": None}
+    bwd = {"x": FAKE, "z": FAKE, "shape": ok, "lens": FAKE, "states": FAKE, "dh": FAKE, "dlast": FAKE, "dx": FAKE,
+           "dz": FAKE, "dh0": FAKE, "ws": FAKE, "bytes": need - 1, "stream": None}
+    for shape, want in ((S(0, 4, 5, 0, 20, 5, 20, 5), 2), (S(2, -1, 5, 0, 20, 5, 20, 5), 2),
+                        (S(2, 4, 0, 0, 20, 5, 20, 5), 2), (S(2, 4, 5, 0, -20, 5, 20, 5), 2),
+                        (S(2, 4, 5, 0, 20, 5, 20, -5), 2), (S(2, 4, 5, 9, 20, 5, 20, 5), 4)):
+        assert call(lib.rnnt_recurrence, fwd, {"shape": shape}) == want
+        assert call(lib.rnnt_recurrence_grad, bwd, {"shape": shape}) == want
+        assert lib.rnnt_recurrence_workspace_bytes(shape) == lib.rnnt_recurrence_states_bytes(shape) == 0
+    for over, want in (({}, 6), ({"x": None}, 1), ({"z": None}, 1), ({"h": None}, 1), ({"last": None}, 1),
+                       ({"x": FAKE + 2}, 7), ({"h0": FAKE + 2}, 7), ({"last": FAKE + 1}, 7), ({"states": FAKE + 8}, 7),
+                       ({"ws": FAKE + 16, "bytes": need}, 7)):
+        assert call(lib.rnnt_recurrence, fwd, over) == want
+    for over, want in (({}, 6), ({"x": None}, 1), ({"states": None}, 1), ({"dx": None}, 1), ({"dz": None}, 1),
+                       ({"dh": FAKE + 2}, 7), ({"dlast": FAKE + 2}, 7), ({"dh0": FAKE + 2}, 7),
+                       ({"dh": None, "dlast": None, "dh0": None}, 6)):
+        assert call(lib.rnnt_recurrence_grad, bwd, over) == want
+
+
+def test_dropout_refusals(net):
+    lib = net._library()
+    fwd = {"x": FAKE, "n": 0, "dtype": 0, "p": 0.5, "rng": FAKE, "rng_out": None, "y": FAKE, "stream": None}
+    for over, want in (({"n": -1}, 2), ({"dtype": 3}, 4), ({"p": 1.0}, 5), ({"p": -0.1}, 5), ({"p": float("nan")}, 5),
+                       ({"rng": None}, 1), ({"n": 4, "x": None}, 1), ({"n": 4, "y": None}, 1), ({"x": FAKE + 2}, 7),
+                       ({"rng": FAKE + 4}, 7), ({"rng_out": FAKE + 4}, 7), ({"n": 1 << 62}, 9)):
+        assert call(lib.rnnt_dropout, fwd, over) == want
+
+
+def test_joint_refusals(net):
+    lib, S = net._library(), net.JointShape
+    ok = S(2, 4, 3, 5, 0)
+    fwd = {"enc": FAKE, "pred": FAKE, "shape": ok, "tl": FAKE, "ul": FAKE, "act": 0, "p": 0.5, "rng": FAKE,
+           "rng_out": None, "h": FAKE, "stream": None}
+    need = lib.rnnt_joint_hidden_grad_workspace_bytes(ok)
+    assert need > 0 and need % 256 == 0
+    bwd = {"enc": FAKE, "pred": FAKE, "shape": ok, "tl": FAKE, "ul": FAKE, "act": 0, "p": 0.5, "rng": FAKE, "dh": FAKE,
+           "denc": FAKE, "dpred": FAKE, "ws": FAKE, "bytes": need - 1, "stream": None}
+    for shape, want in ((S(0, 4, 3, 5, 0), 2), (S(2, 0, 3, 5, 0), 2), (S(2, 4, -1, 5, 0), 2), (S(2, 4, 3, 0, 0), 2),
+                        (S(2, 1 << 20, 1 << 20, 5, 0), 2), (S(2, 4, 3, 5, 3), 4)):
+        assert call(lib.rnnt_joint_hidden, fwd, {"shape": shape}) == want
+        assert call(lib.rnnt_joint_hidden_grad, bwd, {"shape": shape}) == want
+        assert lib.rnnt_joint_hidden_grad_workspace_bytes(shape) == 0
+    both = [({"enc": None}, 1), ({"pred": None}, 1), ({"tl": None}, 1), ({"ul": None}, 1), ({"act": 2}, 5),
+            ({"p": 1.0}, 5), ({"p": -1.0}, 5), ({"p": float("nan")}, 5), ({"rng": None}, 1), ({"enc": FAKE + 2}, 7),
+            ({"rng": FAKE + 4}, 7)]
+    for over, want in both + [({"h": None}, 1), ({"h": FAKE + 1}, 7), ({"rng_out": FAKE + 4}, 7)]:
+        assert call(lib.rnnt_joint_hidden, fwd, over) == want
+    for over, want in both + [({}, 6), ({"dh": None}, 1), ({"denc": None}, 1), ({"dpred": None}, 1),
+                              ({"dpred": FAKE + 2}, 7), ({"ws": FAKE + 16, "bytes": need}, 7)]:
+        assert call(lib.rnnt_joint_hidden_grad, bwd, over) == want
+
+
+def test_binding_refuses_cpu_tensors_and_bad_arguments(net):
+    import paper_2303_10384_amd as rnnt
+    x, lens = torch.zeros(2, 3, 4), torch.ones(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU"):
+        rnnt.label_embedding(torch.zeros(2, 3, dtype=torch.int32), torch.zeros(5, 4))
+    with pytest.raises(ValueError, match="GPU"):
+        rnnt.gated_recurrence(x, x)
+    with pytest.raises(ValueError, match="GPU"):
+        rnnt.dropout(x, 0.5, torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(ValueError, match="GPU"):
+        rnnt.joint_hidden(x, x, lens, lens)
+    with pytest.raises(TypeError, match="tensor"):
+        rnnt.dropout([1.0], 0.5, None)
+
+
+def test_plain_forms_against_their_float64_results():
+    """perf/operators.py on the CPU: its plain forms at half-step tolerances of their types."""
+    import random
+    from perf import operators as O
+    rng = random.Random(11)
+    cap = {"B": 3, "N": 20, "L": 40, "T": 7, "U": 5, "D": 40, "H": 40, "V": 50}
+    for _ in range(16):
+        case = {k: min(v, cap[k]) if k in cap else v for k, v in O.draw(rng).items()}
+        got, want = O.run(O.prepare(case, 3)), O.exact(case, 3)
+        got, want = (v if isinstance(v, tuple) else (v,) for v in (got, want))
+        assert len(got) == len(want)
+        for g, w in zip(got, want):
+            step = torch.finfo(g.dtype).eps / 2
+            # each element's own rounding, and float32 arithmetic on values of the tensor's size
+            assert g.shape == w.shape
+            assert bool(((g.double() - w).abs() <= step * w.abs() + 2.0 ** -18 * w.abs().max() + 1e-30).all()), case
