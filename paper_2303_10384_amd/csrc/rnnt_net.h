@@ -13,45 +13,59 @@
 namespace rnnt {
 
 // ---- VEC consecutive elements as floats -------------------------------------
-// One access of VEC * sizeof(T) bytes (2, 4, 8, 16, or 32 as two of 16), aligned to itself.
+// One access of 2, 4, 8 or 16 bytes (32 bytes are two of 16) at the alignment of an element: the
+// hardware takes vector accesses to global memory at any address, so a row of odd length needs no
+// narrow form, only its last elements do.
+
+template <int BYTES, int ALIGN>
+struct __attribute__((packed, aligned(ALIGN))) Words {
+  uint32_t w[BYTES / 4];
+};
 
 template <typename T, int VEC>
 struct Pack {
   static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
   static constexpr int kWords = (kBytes + 3) / 4;
+  using Memory = Words<kWords * 4, static_cast<int>(sizeof(T))>;
   uint32_t w[kWords];
 
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (kBytes == 2) {
       w[0] = *reinterpret_cast<const uint16_t*>(p);
-    } else if constexpr (kBytes == 4) {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
-    } else if constexpr (kBytes == 8) {
-      const uint2 v = *reinterpret_cast<const uint2*>(p);
-      w[0] = v.x;
-      w[1] = v.y;
     } else {
+      const Memory m = *reinterpret_cast<const Memory*>(p);
 #pragma unroll
-      for (int i = 0; i < kBytes / 16; ++i) {
-        const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-        w[4 * i] = v.x;
-        w[4 * i + 1] = v.y;
-        w[4 * i + 2] = v.z;
-        w[4 * i + 3] = v.w;
-      }
+      for (int i = 0; i < kWords; ++i) w[i] = m.w[i];
     }
   }
   __device__ __forceinline__ void store(T* p) const {
     if constexpr (kBytes == 2) {
       *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(w[0]);
-    } else if constexpr (kBytes == 4) {
-      *reinterpret_cast<uint32_t*>(p) = w[0];
-    } else if constexpr (kBytes == 8) {
-      *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     } else {
+      Memory m;
 #pragma unroll
-      for (int i = 0; i < kBytes / 16; ++i)
-        reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+      for (int i = 0; i < kWords; ++i) m.w[i] = w[i];
+      *reinterpret_cast<Memory*>(p) = m;
+    }
+  }
+  // the first n (0 .. VEC) elements alone, the others 0 / not written
+  __device__ __forceinline__ void load_part(const T* p, int n) {
+    zero();
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      if (i < n) {
+        if constexpr (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t*>(p + i);
+        else w[i / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p + i)) << (16 * (i & 1));
+      }
+    }
+  }
+  __device__ __forceinline__ void store_part(T* p, int n) const {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      if (i < n) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p + i) = w[i];
+        else *reinterpret_cast<uint16_t*>(p + i) = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+      }
     }
   }
   __device__ __forceinline__ void zero() {
@@ -169,6 +183,58 @@ __device__ __forceinline__ uint32_t random16(const uint4& b, int i) {
   const uint32_t w = i < 4 ? (i < 2 ? b.x : b.y) : (i < 6 ? b.z : b.w);
   return (i & 1) ? w >> 16 : w & 0xffffu;
 }
+
+// Which of the eight elements of a block are dropped: sixteen 1 bits each, two to a word, low half
+// first.  A number x < q is found two at a time: both moved to the signed range, subtracted with
+// saturation, and the sign spread.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+struct Dropped {
+  uint32_t m[4];
+
+  __device__ __forceinline__ void none() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = 0;
+  }
+  __device__ __forceinline__ void below(const uint4& b, uint32_t q) {
+    const uint32_t w[4] = {b.x, b.y, b.z, b.w}, limit = (q ^ 0x8000u) * 0x10001u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const i16x2 x = __builtin_bit_cast(i16x2, w[i] ^ 0x80008000u);
+      const i16x2 d = __builtin_elementwise_sub_sat(x, __builtin_bit_cast(i16x2, limit));
+      m[i] = __builtin_bit_cast(uint32_t, d >> static_cast<short>(15));
+    }
+  }
+  // eight elements in memory form, the dropped ones 0
+  template <typename T>
+  __device__ __forceinline__ void clear(Pack<T, 8>& k) const {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k.w[i] &= ~m[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) k.w[i] &= ~static_cast<uint32_t>(static_cast<int32_t>((i & 1) ? m[i / 2] : m[i / 2] << 16) >> 31);
+    }
+  }
+  // elements s .. s + 7 of sixteen: this block's and the next one's
+  __device__ __forceinline__ void shift(const Dropped& next, int s) {
+    uint32_t all[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      all[i] = m[i];
+      all[4 + i] = next.m[i];
+    }
+    if (s & 4) {
+#pragma unroll
+      for (int i = 0; i < 6; ++i) all[i] = all[i + 2];
+    }
+    if (s & 2) {
+#pragma unroll
+      for (int i = 0; i < 5; ++i) all[i] = all[i + 1];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = (s & 1) ? all[i] >> 16 | all[i + 1] << 16 : all[i];
+  }
+};
 
 // dropout by numbers below `threshold`; kept elements are multiplied by `scale`
 struct DropParams {
