@@ -22,6 +22,17 @@ struct __attribute__((packed, aligned(ALIGN))) Words {
   uint32_t w[BYTES / 4];
 };
 
+template <int ALIGN>
+struct LooseVector;
+template <>
+struct LooseVector<2> {
+  typedef u32x4 type __attribute__((aligned(2)));
+};
+template <>
+struct LooseVector<4> {
+  typedef u32x4 type __attribute__((aligned(4)));
+};
+
 template <typename T, int VEC>
 struct Pack {
   static constexpr int kBytes = VEC * static_cast<int>(sizeof(T));
@@ -36,6 +47,19 @@ struct Pack {
       const Memory m = *reinterpret_cast<const Memory*>(p);
 #pragma unroll
       for (int i = 0; i < kWords; ++i) w[i] = m.w[i];
+    }
+  }
+  // a load of what is read once: it does not push lines out that are still to be written or read
+  __device__ __forceinline__ void load_once(const T* p) {
+    static_assert(kBytes % 16 == 0, "vectors of 16 bytes");
+    using loose = LooseVector<sizeof(T)>;
+#pragma unroll
+    for (int i = 0; i < kBytes / 16; ++i) {
+      const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const typename loose::type*>(p) + i);
+      w[4 * i] = v.x;
+      w[4 * i + 1] = v.y;
+      w[4 * i + 2] = v.z;
+      w[4 * i + 3] = v.w;
     }
   }
   __device__ __forceinline__ void store(T* p) const {
@@ -127,12 +151,15 @@ struct Activation<RNNT_ACT_RELU> {
 };
 
 // tanh s = (1 - u) / (1 + u) and 4u / (1 + u)^2 with u = e^-2|s|; below 0.3, where 1 - u
-// loses digits, the odd series through s^9 (the next term is 5e-8 of the value there).
+// loses digits, the odd series through s^9 (the next term is 5e-8 of the value there).  The
+// rounding of the exponent, 2|s| 2^-24 of u, needs no correction: where it grows, u is small
+// in the value, and in the slope it is what the rounding of s itself costs.
 template <>
 struct Activation<RNNT_ACT_TANH> {
+  __device__ static __forceinline__ float u_of(float s) { return fast_exp2(__builtin_fabsf(s) * (-2.f * kLog2eF)); }
   __device__ static __forceinline__ float value(float s) {
     const float y = __builtin_fabsf(s), q = s * s;
-    const float u = exp_neg(2.f * y);
+    const float u = u_of(s);
     const float big = __builtin_copysignf((1.f - u) * __builtin_amdgcn_rcpf(1.f + u), s);
     float p = __builtin_fmaf(q, 62.f / 2835.f, -17.f / 315.f);
     p = __builtin_fmaf(q, p, 2.f / 15.f);
@@ -140,8 +167,8 @@ struct Activation<RNNT_ACT_TANH> {
     return y < 0.3f ? __builtin_fmaf(q * p, s, s) : big;
   }
   __device__ static __forceinline__ float slope(float s) {
-    const float u = exp_neg(2.f * __builtin_fabsf(s)), r = __builtin_amdgcn_rcpf(1.f + u);
-    return 4.f * u * r * r;
+    const float u = u_of(s), r = __builtin_amdgcn_rcpf(1.f + u);
+    return u * r * r * 4.f;
   }
 };
 
@@ -162,15 +189,19 @@ __device__ __forceinline__ Rng load_rng(const int64_t* p) {
              static_cast<uint32_t>(o >> 32)};
 }
 
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {  // one instruction
+  return static_cast<uint32_t>(__builtin_amdgcn_bitop3_b32(static_cast<int>(a), static_cast<int>(b), static_cast<int>(c), 0x96));
+}
+
 __device__ __forceinline__ uint4 random_block(const Rng& g, uint64_t block) {
   uint32_t c0 = static_cast<uint32_t>(block), c1 = static_cast<uint32_t>(block >> 32);
   uint32_t c2 = g.offset_lo, c3 = g.offset_hi, k0 = g.seed_lo, k1 = g.seed_hi;
 #pragma unroll
   for (int r = 0; r < 7; ++r) {
     const uint64_t p0 = static_cast<uint64_t>(c0) * 0xD2511F53u, p1 = static_cast<uint64_t>(c2) * 0xCD9E8D57u;
-    c0 = static_cast<uint32_t>(p1 >> 32) ^ c1 ^ k0;
+    c0 = xor3(static_cast<uint32_t>(p1 >> 32), c1, k0);
     c1 = static_cast<uint32_t>(p1);
-    c2 = static_cast<uint32_t>(p0 >> 32) ^ c3 ^ k1;
+    c2 = xor3(static_cast<uint32_t>(p0 >> 32), c3, k1);
     c3 = static_cast<uint32_t>(p0);
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -195,14 +226,22 @@ struct Dropped {
 #pragma unroll
     for (int i = 0; i < 4; ++i) m[i] = 0;
   }
-  __device__ __forceinline__ void below(const uint4& b, uint32_t q) {
+  // only the sign bits of the halves
+  __device__ __forceinline__ void signs_below(const uint4& b, uint32_t q) {
     const uint32_t w[4] = {b.x, b.y, b.z, b.w}, limit = (q ^ 0x8000u) * 0x10001u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const i16x2 x = __builtin_bit_cast(i16x2, w[i] ^ 0x80008000u);
-      const i16x2 d = __builtin_elementwise_sub_sat(x, __builtin_bit_cast(i16x2, limit));
-      m[i] = __builtin_bit_cast(uint32_t, d >> static_cast<short>(15));
+      m[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(x, __builtin_bit_cast(i16x2, limit)));
     }
+  }
+  __device__ __forceinline__ void below(const uint4& b, uint32_t q) {
+    signs_below(b, q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = spread(m[i]);
+  }
+  __device__ static __forceinline__ uint32_t spread(uint32_t signs) {
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, signs) >> static_cast<short>(15));
   }
   // eight elements in memory form, the dropped ones 0
   template <typename T>

@@ -221,10 +221,10 @@ __global__ __launch_bounds__(256) void net_joint_odd(JointParams p) {
 }
 
 // ---- its gradient -------------------------------------------------------------
-// A block takes kTileT frames of an utterance and a slice of channels, and goes over the units: dh is read
-// once.  A wave holds the sums over u of its eight frames in registers (denc is finished in the block);
-// the sums over its frames meet in LDS, and the block's go to the workspace, one float32 row for kTileT rows
-// of dh (a sixteenth of a bfloat16 dh at 32), which net_joint_join adds up in the order of the frames.
+// A block takes tile_frames() frames of an utterance and a slice of channels, and goes over the units: dh is
+// read once.  A wave holds the sums over u of its frames in registers (denc is finished in the block); the sums
+// over its frames meet in LDS, and the block's go to the workspace, one float32 row for 32 rows of a 16-bit dh
+// or 16 of a float32 one (a sixteenth of the bytes), which net_joint_join adds up in the order of the frames.
 
 struct JointGradParams {
   const void *enc, *pred, *dh;
@@ -232,141 +232,281 @@ struct JointGradParams {
   void *denc, *dpred;
   float* part;  // (B, t_blocks, U1, H)
   DropParams drop;
+  float factor;  // of both sums: the dropout's scale, and 4 for tanh (its slope is 4u / (1 + u)^2)
   int32_t B, T, U1, H, t_blocks, slices, lanes;  // lanes: of a row, eight channels each (4, 8 or 16)
 };
 
-constexpr int kWaveT = 8;                     // frames of a wave
 constexpr int kGradWaves = 4;
-constexpr int kTileT = kWaveT * kGradWaves;   // frames of a block
-
+constexpr int wave_frames(int elem_bytes) { return elem_bytes == 4 ? 4 : 8; }
+constexpr int tile_frames(int elem_bytes) { return kGradWaves * wave_frames(elem_bytes); }  // of a block
 template <typename T>
-__device__ __forceinline__ void load_row(Pack<T, 8>& k, const T* p, int n) {  // n: channels left in the row
-  if (n >= 8) k.load(p);
-  else k.load_part(p, n);
+constexpr int kWaveT = wave_frames(sizeof(T));
+
+// Whether enc + pred > 0 for two 16-bit elements at a time, without the sums: the sum of two floats is
+// positive exactly when enc > -pred, and the bits of a float, its lower 15 flipped where the sign is set, are
+// ordered like the floats when read as a whole number.  Both zeros of enc get -1, below 0 and -1 that the
+// zeros of -pred have or equal to it; a NaN on either side compares as no.
+template <typename T>
+struct PositiveSum {
+  static constexpr uint32_t kInf = __is_same(T, f16_t) ? 0x7c007c00u : 0x7f807f80u;
+  static constexpr uint32_t kNever = 0x80008000u;       // of enc: no sum is positive
+  static constexpr uint32_t kNeverPred = 0x7fff7fffu;   // of -pred
+  __device__ static __forceinline__ i16x2 pair(uint32_t w) { return __builtin_bit_cast(i16x2, w); }
+  __device__ static __forceinline__ uint32_t nan_mask(uint32_t w) {  // magnitude past infinity
+    return Dropped::spread(__builtin_bit_cast(uint32_t, pair(kInf) - pair(w & 0x7fff7fffu)));
+  }
+  __device__ static __forceinline__ uint32_t enc_key(uint32_t w) {
+    const uint32_t o = w ^ (Dropped::spread(w) & 0x7fff7fffu), nan = nan_mask(w);
+    const uint32_t zero = (o & 0xffffu ? 0u : 0xffffu) | (o >> 16 ? 0u : 0xffff0000u);
+    return ((o | zero) & ~nan) | (nan & 0x80008000u);
+  }
+  __device__ static __forceinline__ uint32_t pred_key(uint32_t w) {  // of -pred: ~w, or w without its sign
+    const uint32_t s = Dropped::spread(w), nan = nan_mask(w);
+    const uint32_t o = (w ^ ~s) & ~(s & 0x80008000u);
+    return (o & ~nan) | (nan & 0x7fff7fffu);
+  }
+  __device__ static __forceinline__ uint32_t signs(uint32_t e, uint32_t q) {  // sign bits of q - e
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(pair(q), pair(e)));
+  }
+};
+
+// The upstream elements d times their weights but for the constant factor, added to both sums.
+// 16-bit relu works on keys (e, q: PositiveSum's), everything else on the values.
+template <typename T, int ACT, bool DROP>
+__device__ __forceinline__ void add_weighted(const Pack<T, 8>& e, const Pack<T, 8>& q, const float* qf, Pack<T, 8>& d,
+                                             const Dropped& signs, float* acc, float* ps) {
+  float w[8];
+  if constexpr (ACT == RNNT_ACT_RELU && sizeof(T) == 2) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t on = PositiveSum<T>::signs(e.w[k], q.w[k]);
+      d.w[k] &= Dropped::spread(DROP ? on & ~signs.m[k] : on);
+    }
+    d.get(w);
+  } else {
+    if constexpr (DROP) {
+      Dropped drop;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) drop.m[k] = Dropped::spread(signs.m[k]);
+      drop.clear(d);
+    }
+    float ef[8];
+    e.get(ef);
+    d.get(w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float s = ef[k] + qf[k];
+      if constexpr (ACT == RNNT_ACT_RELU) {
+        w[k] = s > 0.f ? w[k] : 0.f;
+      } else {
+        const float u = Activation<ACT>::u_of(s), r = __builtin_amdgcn_rcpf(1.f + u);
+        w[k] *= u * r * r;
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    acc[k] += w[k];
+    ps[k] += w[k];
+  }
 }
 
-template <typename T, int ACT, bool EIGHTS>
-__global__ __launch_bounds__(64 * kGradWaves) void net_joint_grad(JointGradParams p) {
-  __shared__ __attribute__((aligned(16))) float sums[2][kGradWaves][512];
-  const int slice = static_cast<int>(blockIdx.x) % p.slices, bt = static_cast<int>(blockIdx.x) / p.slices;
-  const int tb = bt % p.t_blocks, b = bt / p.t_blocks;
-  const int wave = static_cast<int>(threadIdx.x) >> 6, lane = static_cast<int>(threadIdx.x) & 63;
-  const int sub = lane / p.lanes, rows = 64 / p.lanes;
-  const int c = (slice * p.lanes + (lane & (p.lanes - 1))) * 8;
-  const int left = p.H - c;  // channels of this lane: min(left, 8), none when it is not positive
-  int tl = p.logit_lens[b], ul = p.label_lens[b];
-  if (tl < 0 || tl > p.T || ul < 0 || ul >= p.U1) tl = 0;
-  const int t0 = tb * kTileT + wave * kWaveT;
-  const int frames = max(0, min(kWaveT, tl - t0));
-  T* denc = static_cast<T*>(p.denc) + (static_cast<int64_t>(b) * p.T + t0) * p.H + c;
-  const int64_t run0 = (static_cast<int64_t>(b) * p.T + t0) * p.U1;  // row (t0, 0)
-  float acc[kWaveT][8];
+__device__ __forceinline__ uint32_t select(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
+
+// A step's rows: the wave's frames at one unit (the lane's), and the unit's row of pred.  Every load is issued,
+// at an address inside the tensors: a load under a branch would make every later wait a full drain.
+template <typename T, int FRAMES>
+struct GradRows {
+  Pack<T, 8> d[FRAMES], q;
+
+  // dh, pred: the same for a whole wave; at: the lane's element (32 bits: bases stay in scalar registers)
+  __device__ __forceinline__ void load(const T* const (&dh)[FRAMES], const T* pred, uint32_t at) {
 #pragma unroll
-  for (int i = 0; i < kWaveT; ++i)
+    for (int i = 0; i < FRAMES; ++i) d[i].load_once(dh[i] + at);
+    q.load(pred + at);
+  }
+};
+
+// The utterance of place r when the ones with the most units come first (ties by number).  A block's time is
+// its utterance's units, and a chip takes only a few blocks to a CU: the longest ones last left it idle.  Past 64
+// utterances the blocks are many and stay in order.
+__device__ __forceinline__ int longest_first(const int32_t* label_lens, int B, int r) {
+  if (B > 64) return r;
+  const int lane = static_cast<int>(threadIdx.x) & 63, mine = label_lens[min(lane, B - 1)];
+  int place = 0;
+  for (int j = 0; j < B; ++j) {
+    const int other = __builtin_amdgcn_readlane(mine, j);
+    place += other > mine || (other == mine && j < lane);
+  }
+  return __builtin_ctzll(__ballot(place == r && lane < B));
+}
+
+// EIGHTS: rows are multiples of eight elements, so that a group's numbers are one block.  H is at least 8 here: the
+// last group of a row that is no multiple begins at H - 8, its first channels also the group's before it, which
+// computes and writes the same values.
+template <typename T, int ACT, bool EIGHTS, bool DROP>
+__global__ __launch_bounds__(64 * kGradWaves) void net_joint_grad(JointGradParams p) {
+  constexpr bool KEYS = ACT == RNNT_ACT_RELU && sizeof(T) == 2;
+  constexpr int WAVES = kGradWaves, FRAMES = kWaveT<T>;
+  static_assert(WAVES == 4, "256 threads store a step's 512 sums");
+  __shared__ __attribute__((aligned(16))) float sums[2][WAVES][512];
+  const int slice = static_cast<int>(blockIdx.x) % p.slices, bt = static_cast<int>(blockIdx.x) / p.slices;
+  const int tb = bt % p.t_blocks, b = longest_first(p.label_lens, p.B, bt / p.t_blocks);
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  const int sub = lane / p.lanes, rows = 64 / p.lanes;
+  const int c0 = slice * p.lanes * 8, c = min(c0 + (lane & (p.lanes - 1)) * 8, p.H - 8);
+  int tl = p.logit_lens[b];
+  const int ul = p.label_lens[b];
+  if (tl < 0 || tl > p.T || ul < 0 || ul >= p.U1) tl = 0;
+  const int t0 = (tb * WAVES + wave) * FRAMES, frames = max(0, min(FRAMES, tl - t0));
+  float acc[FRAMES][8];
+#pragma unroll
+  for (int i = 0; i < FRAMES; ++i)
 #pragma unroll
     for (int k = 0; k < 8; ++k) acc[i][k] = 0.f;
 
-  if (tb * kTileT < tl) {
-    const T* enc = static_cast<const T*>(p.enc) + (static_cast<int64_t>(b) * p.T + t0) * p.H + c;
-    const T* pred = static_cast<const T*>(p.pred) + static_cast<int64_t>(b) * p.U1 * p.H + c;
-    const T* dh = static_cast<const T*>(p.dh) + run0 * p.H + c;
-    float* part = p.part + (static_cast<int64_t>(b) * p.t_blocks + tb) * p.U1 * p.H;
+  if (tb * WAVES * FRAMES < tl) {  // the block's waves meet at barriers: all or none
+    const int64_t run = static_cast<int64_t>(p.U1) * p.H;
+    const T* pred = static_cast<const T*>(p.pred) + b * run;
     Rng rng{};
-    if (p.drop.threshold) rng = load_rng(p.drop.rng);
-    Pack<T, 8> e[kWaveT];
+    if (DROP) rng = load_rng(p.drop.rng);
+    // a frame past the last one reads that one's rows and is left out of the sums
+    const T* dh[FRAMES];
+    uint64_t number[FRAMES];  // of element (b, t, 0, 0)
+    Pack<T, 8> e[FRAMES];
 #pragma unroll
-    for (int i = 0; i < kWaveT; ++i) {
-      e[i].zero();
-      if (i < frames && left > 0) load_row(e[i], enc + static_cast<int64_t>(i) * p.H, left);
+    for (int i = 0; i < FRAMES; ++i) {
+      const int64_t bt_i = static_cast<int64_t>(b) * p.T + min(t0 + i, tl - 1);
+      number[i] = static_cast<uint64_t>(bt_i * run);
+      dh[i] = static_cast<const T*>(p.dh) + bt_i * run;
+      e[i].load(static_cast<const T*>(p.enc) + bt_i * p.H + c);
     }
-    int buf = 0;
-    for (int u0 = 0; u0 <= ul; u0 += rows, buf ^= 1) {
+    GradRows<T, FRAMES> even, odd;
+    even.load(dh, pred, static_cast<uint32_t>(min(sub, ul) * p.H + c));
+    __builtin_amdgcn_sched_barrier(0);  // every load is on its way before the first is waited for
+    if constexpr (KEYS) {
+#pragma unroll
+      for (int i = 0; i < FRAMES; ++i) {
+        const uint32_t off = static_cast<uint32_t>((frames - 1 - i) >> 31);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[i].w[k] = select(off, PositiveSum<T>::kNever, PositiveSum<T>::enc_key(e[i].w[k]));
+      }
+    }
+    // this thread's part of a step's 512 sums: a pair of channels, neighbours in a row of the workspace
+    const __amdgpu_buffer_rsrc_t part =
+        make_buffer(p.part + (static_cast<int64_t>(b) * p.t_blocks + tb) * run, run * static_cast<int64_t>(sizeof(float)));
+    const int from = static_cast<int>(threadIdx.x) >> 2, pair = static_cast<int>(threadIdx.x) & 3;
+    const int sums_at = ((pair >> 1) * 64 + from) * 2 + (pair & 1);  // in float2
+    const int put_u = from / p.lanes, put_c = min(c0 + (from & (p.lanes - 1)) * 8, p.H - 8) + pair * 2;
+
+    auto step = [&](GradRows<T, FRAMES>& now, GradRows<T, FRAMES>& next, int u0, float (*lds)[512]) {
       const int u = u0 + sub;
-      const bool live = u <= ul && left > 0;
-      float ps[8] = {};
-      if (live) {
-        Pack<T, 8> q, d[kWaveT];
+      // a lane past the last unit reads that unit's row again and adds nothing
+      next.load(dh, pred, static_cast<uint32_t>(min(u + rows, ul) * p.H + c));
+      __builtin_amdgcn_sched_barrier(0);  // the loads stay ahead of the arithmetic
+      const uint32_t at = static_cast<uint32_t>(u * p.H + c);
+      // No branch from here to the barrier: what does not count (a lane past the last unit, a frame past the last
+      // one) is masked, in the keys where there are any, else in the upstream elements.
+      const uint32_t past = static_cast<uint32_t>((ul - u) >> 31);
+      float ps[8] = {}, qf[8];
+      if constexpr (KEYS) {
 #pragma unroll
-        for (int i = 0; i < kWaveT; ++i)
-          if (i < frames) load_row(d[i], dh + (static_cast<int64_t>(i) * p.U1 + u) * p.H, left);
-        load_row(q, pred + static_cast<int64_t>(u) * p.H, left);
-        float qf[8];
-        q.get(qf);
+        for (int k = 0; k < 4; ++k) now.q.w[k] = select(past, PositiveSum<T>::kNeverPred, PositiveSum<T>::pred_key(now.q.w[k]));
+      } else {
+        now.q.get(qf);
+      }
 #pragma unroll
-        for (int i = 0; i < kWaveT; ++i) {
-          if (i < frames) {
-            if (p.drop.threshold) {
-              const uint64_t n = static_cast<uint64_t>((run0 + static_cast<int64_t>(i) * p.U1 + u) * p.H + c);
-              Dropped drop;
-              drop.below(random_block(rng, n >> 3), p.drop.threshold);
-              if (!EIGHTS) {
-                Dropped next;
-                next.below(random_block(rng, (n >> 3) + 1), p.drop.threshold);
-                drop.shift(next, static_cast<int>(n & 7));
-              }
-              drop.clear(d[i]);
-            }
-            float ef[8], w[8];
-            e[i].get(ef);
-            d[i].get(w);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float s = ef[k] + qf[k];
-              if (ACT == RNNT_ACT_RELU) w[k] = s > 0.f ? w[k] : 0.f;
-              else w[k] *= Activation<ACT>::slope(s);
-              acc[i][k] += w[k];
-              ps[k] += w[k];
-            }
+      for (int i = 0; i < FRAMES; ++i) {
+        Dropped signs;
+        if constexpr (DROP) {
+          const uint64_t n = number[i] + at;
+          signs.signs_below(random_block(rng, n >> 3), p.drop.threshold);
+          if constexpr (!EIGHTS) {
+            Dropped after;
+            after.signs_below(random_block(rng, (n >> 3) + 1), p.drop.threshold);
+            signs.shift(after, static_cast<int>(n & 7));
           }
         }
+        if constexpr (!KEYS) {
+          const uint32_t off = past | static_cast<uint32_t>((frames - 1 - i) >> 31);
+#pragma unroll
+          for (int k = 0; k < Pack<T, 8>::kWords; ++k) now.d[i].w[k] &= ~off;
+        }
+        add_weighted<T, ACT, DROP>(e[i], now.q, qf, now.d[i], signs, acc[i], ps);
       }
-      float4* mine = reinterpret_cast<float4*>(sums[buf][wave]);
+      float4* mine = reinterpret_cast<float4*>(lds[wave]);
       mine[lane] = make_float4(ps[0], ps[1], ps[2], ps[3]);
       mine[64 + lane] = make_float4(ps[4], ps[5], ps[6], ps[7]);
-      __syncthreads();  // one to a step: the other buffer is written before the next
-      const int at = static_cast<int>(threadIdx.x), from = (at >> 1) & 63;
+      __syncthreads();  // one to a step: see the two buffers below
       float2 total = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kGradWaves; ++w) {
-        const float2 v = reinterpret_cast<const float2*>(sums[buf][w])[at];
+      for (int w = 0; w < WAVES; ++w) {
+        const float2 v = reinterpret_cast<const float2*>(lds[w])[sums_at];
         total.x += v.x;
         total.y += v.y;
       }
-      const int pu = u0 + from / p.lanes;
-      const int pc = (slice * p.lanes + (from & (p.lanes - 1))) * 8 + (at >> 7) * 4 + (at & 1) * 2;
-      if (pu <= ul) {
-        float* o = part + static_cast<int64_t>(pu) * p.H + pc;
-        if (pc < p.H) o[0] = total.x;
-        if (pc + 1 < p.H) o[1] = total.y;
-      }
+      // past the last unit: an offset past the buffer, where nothing is written
+      const int off = u0 + put_u <= ul ? ((u0 + put_u) * p.H + put_c) * 4 : kOutOfRange;
+      __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(total.x), __float_as_uint(total.y)}, part, off, 0, 0);
+    };
+    // Two sets of rows and of LDS sums in turn: the next rows are on their way while a step computes, and a wave
+    // that has passed a step's barrier writes the other sums, which everyone has read before that barrier.
+    for (int u0 = 0;;) {
+      step(even, odd, u0, sums[0]);
+      u0 += rows;
+      if (u0 > ul) break;
+      step(odd, even, u0, sums[1]);
+      u0 += rows;
+      if (u0 > ul) break;
     }
     // the rows of u that the wave's lanes shared out
     for (int off = p.lanes; off < 64; off <<= 1) {
 #pragma unroll
-      for (int i = 0; i < kWaveT; ++i)
+      for (int i = 0; i < FRAMES; ++i)
 #pragma unroll
         for (int k = 0; k < 8; ++k) acc[i][k] += __shfl_xor(acc[i][k], off);
     }
   }
-  if (sub == 0 && left > 0) {
+  if (lane < p.lanes && c0 + lane * 8 < p.H) {
+    T* denc = static_cast<T*>(p.denc) + (static_cast<int64_t>(b) * p.T + t0) * p.H + c;
 #pragma unroll
-    for (int i = 0; i < kWaveT; ++i) {
+    for (int i = 0; i < FRAMES; ++i) {
       if (t0 + i < p.T) {
         float f[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = acc[i][k] * p.drop.scale;
+        for (int k = 0; k < 8; ++k) f[k] = i < frames ? acc[i][k] * p.factor : 0.f;
         Pack<T, 8> k;
         k.set(f);
-        if (left >= 8) k.store(denc + static_cast<int64_t>(i) * p.H);
-        else k.store_part(denc + static_cast<int64_t>(i) * p.H, left);
+        k.store(denc + static_cast<int64_t>(i) * p.H);
       }
     }
   }
 }
 
-__device__ __forceinline__ void load_row4(Pack<float, 4>& k, const float* p, int n) {
-  if (n >= 4) k.load(p);
-  else k.load_part(p, n);
+// Rows of fewer than eight channels: a thread to a channel of one row of one gradient.
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void net_joint_grad_narrow(JointGradParams p, bool of_enc) {
+  const int rows = of_enc ? p.T : p.U1;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, row = at / p.H;
+  if (row >= static_cast<int64_t>(p.B) * rows) return;
+  const int c = static_cast<int>(at - row * p.H), b = static_cast<int>(row / rows), r = static_cast<int>(row - static_cast<int64_t>(b) * rows);
+  const int tl = p.logit_lens[b], ul = p.label_lens[b];
+  const bool ok = tl >= 0 && tl <= p.T && ul >= 0 && ul < p.U1;
+  const int others = !ok ? 0 : of_enc ? (r < tl ? ul + 1 : 0) : (r <= ul ? tl : 0);
+  Rng rng{};
+  if (p.drop.threshold) rng = load_rng(p.drop.rng);
+  float sum = 0.f;
+  for (int o = 0; o < others; ++o) {
+    const int64_t bt = static_cast<int64_t>(b) * p.T + (of_enc ? r : o), bu = static_cast<int64_t>(b) * p.U1 + (of_enc ? o : r);
+    const int64_t n = (bt * p.U1 + (of_enc ? o : r)) * p.H + c;
+    const float s = ElemTraits<T>::load1(static_cast<const T*>(p.enc) + bt * p.H + c) +
+                    ElemTraits<T>::load1(static_cast<const T*>(p.pred) + bu * p.H + c);
+    const bool keep = !p.drop.threshold ||
+                      random16(random_block(rng, static_cast<uint64_t>(n >> 3)), static_cast<int>(n & 7)) >= p.drop.threshold;
+    const float w = ACT == RNNT_ACT_RELU ? Activation<ACT>::slope(s) : 0.25f * Activation<ACT>::slope(s);
+    if (keep && w != 0.f) sum += ElemTraits<T>::load1(static_cast<const T*>(p.dh) + n) * w;
+  }
+  ElemTraits<T>::store1(static_cast<T*>(of_enc ? p.denc : p.dpred) + at, sum * p.factor);
 }
 
 // dpred from the blocks' sums: four channels to a thread.
@@ -381,19 +521,20 @@ __global__ __launch_bounds__(256) void net_joint_join(JointGradParams p) {
   const int tl = p.logit_lens[b], ul = p.label_lens[b];
   float f[4] = {};
   if (tl >= 0 && tl <= p.T && ul < p.U1 && u <= ul) {
-    const int n = (tl + kTileT - 1) / kTileT;
+    const int n = (tl + tile_frames(sizeof(T)) - 1) / tile_frames(sizeof(T));
     const float* part = p.part + (static_cast<int64_t>(b) * p.t_blocks * p.U1 + u) * p.H + c;
     const int64_t step = static_cast<int64_t>(p.U1) * p.H;
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
       Pack<float, 4> k;
-      load_row4(k, part + i * step, left);
+      if (left >= 4) k.load(part + i * step);
+      else k.load_part(part + i * step, left);
 #pragma unroll
       for (int j = 0; j < 4; ++j) f[j] += __uint_as_float(k.w[j]);
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) f[j] *= p.drop.scale;
+  for (int j = 0; j < 4; ++j) f[j] *= p.factor;
   Pack<T, 4> k;
   k.set(f);
   T* o = static_cast<T*>(p.dpred) + row * p.H + c;
@@ -415,10 +556,13 @@ rnnt_status_t check(const rnnt_joint_shape_t& s, rnnt_activation_t act, double p
   return RNNT_OK;
 }
 
-int tile_count(int T) { return static_cast<int>((static_cast<int64_t>(T) + kTileT - 1) / kTileT); }
+int tile_count(const rnnt_joint_shape_t& s) {
+  const int64_t n = tile_frames(static_cast<int>(net_elem_bytes(s.dtype)));
+  return static_cast<int>((s.T_max + n - 1) / n);
+}
 
 size_t grad_bytes(const rnnt_joint_shape_t& s) {
-  return net_align256(static_cast<size_t>(s.B) * tile_count(s.T_max) * (static_cast<size_t>(s.U_max) + 1) * s.H * sizeof(float));
+  return net_align256(static_cast<size_t>(s.B) * tile_count(s) * (static_cast<size_t>(s.U_max) + 1) * s.H * sizeof(float));
 }
 
 template <typename F>
@@ -527,19 +671,38 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
   q.U1 = shape.U_max + 1;
   q.H = shape.H;
   q.part = reinterpret_cast<float*>(ws.ptr);
-  q.t_blocks = tile_count(shape.T_max);
+  q.factor = q.drop.scale * (act == RNNT_ACT_TANH ? 4.f : 1.f);
+  q.t_blocks = tile_count(shape);
   q.lanes = shape.H <= 32 ? 4 : shape.H <= 64 ? 8 : 16;
   q.slices = (shape.H + 8 * q.lanes - 1) / (8 * q.lanes);
   const int64_t x = static_cast<int64_t>(shape.B) * q.t_blocks * q.slices;
   const int64_t joins = (static_cast<int64_t>(shape.B) * q.U1 * ((shape.H + 3) / 4) + 255) / 256;
-  if (x > kMaxRows / 256 || joins > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
+  // a block's sums are one buffer of less than 2^31 bytes
+  if (x > kMaxRows / 256 || joins > kMaxRows / 256 || static_cast<int64_t>(q.U1) * shape.H >= (int64_t{1} << 29))
+    return RNNT_ERR_UNSUPPORTED;
   return with_dtype(shape.dtype, [&](auto t) {
     using T = decltype(t);
+    if (shape.H < 8) {
+      return with_activation(act, [&](auto a) {
+        constexpr int A = decltype(a)::value;
+        const auto grid = [&](int rows) { return dim3(static_cast<uint32_t>((static_cast<int64_t>(shape.B) * rows * shape.H + 255) / 256)); };
+        hipLaunchKernelGGL((net_joint_grad_narrow<T, A>), grid(q.T), dim3(256), 0, stream, q, true);
+        if (launched() != RNNT_OK) return RNNT_ERR_HIP;
+        hipLaunchKernelGGL((net_joint_grad_narrow<T, A>), grid(q.U1), dim3(256), 0, stream, q, false);
+        return launched();
+      });
+    }
     const rnnt_status_t done = with_activation(act, [&](auto a) {
       constexpr int A = decltype(a)::value;
       const dim3 grid(static_cast<uint32_t>(x)), block(64 * kGradWaves);
-      if (shape.H % 8 == 0) hipLaunchKernelGGL((net_joint_grad<T, A, true>), grid, block, 0, stream, q);
-      else hipLaunchKernelGGL((net_joint_grad<T, A, false>), grid, block, 0, stream, q);
+      const bool drop = q.drop.threshold != 0;
+      if (shape.H % 8 == 0) {
+        if (drop) hipLaunchKernelGGL((net_joint_grad<T, A, true, true>), grid, block, 0, stream, q);
+        else hipLaunchKernelGGL((net_joint_grad<T, A, true, false>), grid, block, 0, stream, q);
+      } else {
+        if (drop) hipLaunchKernelGGL((net_joint_grad<T, A, false, true>), grid, block, 0, stream, q);
+        else hipLaunchKernelGGL((net_joint_grad<T, A, true, false>), grid, block, 0, stream, q);
+      }
       return launched();
     });
     if (done != RNNT_OK) return done;
