@@ -29,88 +29,298 @@ __device__ __forceinline__ int32_t token_at(const TokenSource& s, int32_t r) {
   return static_cast<uint32_t>(v) < static_cast<uint32_t>(s.V) ? v : kBadRow;
 }
 
+// Rows are covered by groups of VEC elements; the last group of a row that is no multiple of VEC begins
+// VEC before its end, and what it shares with the group before is computed and written twice alike.
+__device__ __forceinline__ int group_start(int group, int VEC, int D) { return min(group * VEC, D - VEC); }
+
 struct EmbeddingParams {
   TokenSource src;
   const void* weight;
   void* out;
   float scale;
-  int32_t D, rows, lanes;  // lanes: threads to a row, a power of two
+  int32_t D, rows, lanes, groups;  // lanes: threads to a row, a power of two; groups: of VEC elements in a row
 };
 
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void net_embedding(EmbeddingParams p) {
-  const int row = static_cast<int>(blockIdx.x) * (256 / p.lanes) + static_cast<int>(threadIdx.x) / p.lanes;
-  if (row >= p.rows) return;
-  const int32_t v = token_at(p.src, row);
-  const T* w = static_cast<const T*>(p.weight) + static_cast<int64_t>(v) * p.D;
-  T* o = static_cast<T*>(p.out) + static_cast<int64_t>(row) * p.D;
-  for (int c = (static_cast<int>(threadIdx.x) & (p.lanes - 1)) * VEC; c < p.D; c += p.lanes * VEC) {
-    float f[VEC];
-    Pack<T, VEC> k;
-    if (v >= 0) {
-      k.load(w + c);
-      k.get(f);
+  const int per = 256 / p.lanes, step = static_cast<int>(gridDim.x) * per;
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * per + static_cast<int>(threadIdx.x) / p.lanes; r < p.rows; r += step) {
+    const int row = static_cast<int>(r);
+    const int32_t v = token_at(p.src, row);
+    const T* w = static_cast<const T*>(p.weight) + static_cast<int64_t>(v) * p.D;
+    T* o = static_cast<T*>(p.out) + static_cast<int64_t>(row) * p.D;
+    for (int g = static_cast<int>(threadIdx.x) & (p.lanes - 1); g < p.groups; g += p.lanes) {
+      const int c = group_start(g, VEC, p.D);
+      float f[VEC];
+      Pack<T, VEC> k;
+      if (v >= 0) {
+        k.load(w + c);
+        k.get(f);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) f[j] *= p.scale;
-    } else {
+        for (int j = 0; j < VEC; ++j) f[j] *= p.scale;
+      } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) f[j] = v == kBadRow ? __builtin_nanf("") : 0.f;
+        for (int j = 0; j < VEC; ++j) f[j] = v == kBadRow ? __builtin_nanf("") : 0.f;
+      }
+      k.set(f);
+      k.store(o + c);
     }
-    k.set(f);
-    k.store(o + c);
   }
 }
+
+// ---- the gradient ---------------------------------------------------------------
+// Four launches: the rows' tokens; the rows sorted by token (and by position within one); sums of the runs of
+// common tokens, kRun sorted rows at a time; every weight row from its rows or, if it has more than kRun, from
+// those sums.  A row of dout is read once, and every sum has one order.
+
+constexpr int32_t kNoKey = 0x7fffffff;  // a row without a token, past every token
+constexpr int kSortWaves = 16;
+constexpr int kSortTokens = 960;   // most tokens of a sorting block: 16 x 960 counters in LDS, a thread to a token
+constexpr int kSortBlocks = 256;   // one to a CU, each looks at every row
+constexpr int kRun = 64;
 
 struct EmbeddingGradParams {
   TokenSource src;
   const void* dout;
   void* dweight;
   float scale;
-  int32_t D, rows;
+  int32_t D, rows, lanes, tiles;    // lanes: of a wave to a row of a tile, a power of two
+  int32_t per_block;                // tokens of a sorting block
+  int32_t runs;                     // ceil(rows / kRun)
+  int32_t* keys;                    // (rows)
+  int32_t* sorted;                  // (rows) positions, by token
+  int32_t* first;                   // (V + 1) where a token's rows begin in `sorted`
+  float* sums;                      // (runs, 2, D): of the run's first token, of its last one
 };
 
-// One block to a weight row: it looks at every token and adds the rows of its own, in order.
-template <typename T, int VEC>
-__global__ __launch_bounds__(256) void net_embedding_grad(EmbeddingGradParams p) {
-  const int32_t v = static_cast<int32_t>(blockIdx.x);
-  __shared__ int32_t found[256];
-  __shared__ int32_t count[4];
-  for (int c0 = 0; c0 < p.D; c0 += 256 * VEC) {
-    const int c = c0 + static_cast<int>(threadIdx.x) * VEC;
-    float sum[VEC] = {};
-    for (int r0 = 0; r0 < p.rows; r0 += 256) {
-      const int r = r0 + static_cast<int>(threadIdx.x);
-      const bool hit = r < p.rows && token_at(p.src, r) == v;
-      const uint64_t votes = __ballot(hit);
-      const int wave = static_cast<int>(threadIdx.x) >> 6, lane = static_cast<int>(threadIdx.x) & 63;
-      if (lane == 0) count[wave] = __popcll(votes);
-      __syncthreads();
-      int at = __popcll(votes & ((uint64_t{1} << lane) - 1)), n = 0;
-      for (int w = 0; w < 4; ++w) {
-        at += w < wave ? count[w] : 0;
-        n += count[w];
-      }
-      if (hit) found[at] = r;
-      __syncthreads();
-      if (c < p.D) {
-        for (int i = 0; i < n; ++i) {
-          float f[VEC];
-          Pack<T, VEC> k;
-          k.load(static_cast<const T*>(p.dout) + static_cast<int64_t>(found[i]) * p.D + c);
-          k.get(f);
+__global__ __launch_bounds__(256) void net_embedding_keys(EmbeddingGradParams p) {
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (r >= p.rows) return;
+  const int32_t v = token_at(p.src, static_cast<int32_t>(r));
+  p.keys[r] = v < 0 ? kNoKey : v;
+}
+
+// A counting sort in which every block looks at all rows and places those of its own few tokens: no pass over a
+// table of counters between blocks, one launch, and the rows of a token in order (a wave takes a stretch of the rows
+// and knows from the first look how many of each token the waves before it have).  The rows are read from L2:
+// 131072 of them are 0.5 MB to a block.
+__global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingGradParams p) {
+  extern __shared__ int32_t count[];  // [kSortWaves][per_block], then where a wave's next row of a token goes
+  __shared__ int32_t below[kSortWaves], wave_sum[kSortWaves];
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  const int64_t lo64 = static_cast<int64_t>(blockIdx.x) * p.per_block;
+  if (lo64 >= p.src.V) return;
+  const int lo = static_cast<int>(lo64), n = min(p.per_block, p.src.V - lo);
+  for (int i = threadIdx.x; i < kSortWaves * p.per_block; i += 64 * kSortWaves) count[i] = 0;
+  __syncthreads();
+  const int64_t stretch = ((static_cast<int64_t>(p.rows) + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+  const int64_t begin = wave * stretch, end = min(begin + stretch, static_cast<int64_t>(p.rows));
+  int32_t* mine = count + wave * p.per_block;
+  constexpr int BATCH = 8;
+  int less = 0;
+  for (int64_t r = begin + lane; r < end + lane; r += 64 * BATCH) {
+    int32_t key[BATCH];
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) sum[j] += f[j];
-        }
-      }
-      __syncthreads();
+    for (int i = 0; i < BATCH; ++i) {
+      const int64_t at = r + 64 * i;
+      key[i] = p.keys[min(at, static_cast<int64_t>(p.rows) - 1)];
+      key[i] = at < end ? key[i] : kNoKey;
     }
-    if (c < p.D) {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      less += __popcll(__ballot(key[i] < lo));
+      const uint32_t d = static_cast<uint32_t>(key[i]) - static_cast<uint32_t>(lo);
+      if (d < static_cast<uint32_t>(n)) atomicAdd(&mine[d], 1);
+    }
+  }
+  if (lane == 0) below[wave] = less;
+  __syncthreads();
+  // exclusive sums over (token, wave)
+  int base = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) base += below[w];
+  {
+    const int t = static_cast<int>(threadIdx.x);  // per_block is at most the block's threads
+    int total = 0;
+    if (t < n) {
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) total += count[w * p.per_block + t];
+    }
+    int upto = total;  // inclusive over the wave
+    for (int off = 1; off < 64; off <<= 1) {
+      const int v = __shfl_up(upto, off);
+      if (lane >= off) upto += v;
+    }
+    if (lane == 63) wave_sum[wave] = upto;
+    __syncthreads();
+    int at = base + upto - total;
+    for (int w = 0; w < wave; ++w) at += wave_sum[w];
+    if (t < n) {
+      p.first[lo + t] = at;
+      if (lo + t == p.src.V - 1) p.first[p.src.V] = at + total;
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) {
+        const int c = count[w * p.per_block + t];
+        count[w * p.per_block + t] = at;
+        at += c;
+      }
+    }
+  }
+  __syncthreads();
+  for (int64_t r = begin + lane; r < end + lane; r += 64 * BATCH) {
+    int32_t key[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int64_t at = r + 64 * i;
+      key[i] = p.keys[min(at, static_cast<int64_t>(p.rows) - 1)];
+      key[i] = at < end ? key[i] : kNoKey;
+    }
+#pragma unroll 1
+    for (int i = 0; i < BATCH; ++i) {
+      const uint32_t d = static_cast<uint32_t>(key[0]) - static_cast<uint32_t>(lo);
+      uint64_t left = __ballot(d < static_cast<uint32_t>(n));
+      while (left) {  // the group's tokens one by one, each with all its rows
+        const int leader = __builtin_ctzll(left);
+        const uint32_t token = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(d), leader));
+        const uint64_t same = __ballot(d == token);
+        const int at = mine[token];
+        if (d == token) p.sorted[at + __popcll(same & ((uint64_t{1} << lane) - 1))] = static_cast<int32_t>(r + 64 * i);
+        if (lane == leader) mine[token] = at + __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next look at the counter sees it
+        left &= ~same;
+      }
+#pragma unroll
+      for (int j = 0; j + 1 < BATCH; ++j) key[j] = key[j + 1];
+    }
+  }
+}
+
+// The sum of rows list[0 .. n) of a tile's columns (list null: rows 0 .. n of float32 sums), shared out to the
+// wave's groups of lanes.  Every lane gets the sum of its columns, the same in every group.
+template <typename T, int VEC>
+__device__ __forceinline__ void sum_rows(const T* rows, int64_t stride, const int32_t* list, int n, int lanes, int c, float* sum) {
+  const int lane = static_cast<int>(threadIdx.x) & 63, group = lane / lanes, groups = 64 / lanes;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+  constexpr int BATCH = 8;
+  int i = group;
+  for (; i + (BATCH - 1) * groups < n; i += BATCH * groups) {
+    Pack<T, VEC> k[BATCH];
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) k[q].load(rows + (list ? list[i + q * groups] : i + q * groups) * stride + c);
+#pragma unroll
+    for (int q = 0; q < BATCH; ++q) {
+      float f[VEC];
+      k[q].get(f);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[j] += f[j];
+    }
+  }
+  for (; i < n; i += 2 * groups) {
+    Pack<T, VEC> k[2];
+    const int i1 = min(i + groups, n - 1);
+    k[0].load(rows + (list ? list[i] : i) * stride + c);
+    k[1].load(rows + (list ? list[i1] : i1) * stride + c);
+    float f[VEC];
+    k[0].get(f);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] += f[j];
+    k[1].get(f);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] += i + groups < n ? f[j] : 0.f;
+  }
+  for (int off = lanes; off < 64; off <<= 1) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] += __shfl_xor(sum[j], off);
+  }
+}
+
+// A wave to the first or the last token of a run of sorted rows (a token of more than kRun rows: at most
+// two of them meet a run), and a tile of columns.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void net_embedding_runs(EmbeddingGradParams p) {
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int tile = static_cast<int>(item % p.tiles), last = static_cast<int>(item / p.tiles) & 1;
+  const int64_t run = item / p.tiles / 2;
+  if (run >= p.runs) return;
+  const int lane = static_cast<int>(threadIdx.x) & 63;
+  const int total = p.first[p.src.V];
+  const int64_t begin64 = run * kRun;
+  if (begin64 >= total) return;
+  const int begin = static_cast<int>(begin64), end = min(begin + kRun, total);
+  const int32_t head = p.keys[p.sorted[begin]], token = last ? p.keys[p.sorted[end - 1]] : head;
+  if (last && token == head) return;
+  const int from = p.first[token], to = p.first[token + 1];
+  if (to - from <= kRun) return;
+  const int a = max(from, begin), n = min(to, end) - a;
+  const int c = group_start(tile * p.lanes + (lane & (p.lanes - 1)), VEC, p.D);
+  float sum[VEC];
+  sum_rows<T, VEC>(static_cast<const T*>(p.dout), p.D, p.sorted + a, n, p.lanes, c, sum);
+  if (lane < p.lanes) {
+    Pack<float, VEC> k;
+    k.set(sum);
+    k.store(p.sums + (run * 2 + last) * p.D + c);
+  }
+}
+
+// A wave to a weight row and a tile of columns; behind them, a block to a run in which a common token begins.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void net_embedding_rows(EmbeddingGradParams p, int32_t row_blocks) {
+  __shared__ float parts[4][64 * VEC];
+  const int wave = static_cast<int>(threadIdx.x) >> 6, lane = static_cast<int>(threadIdx.x) & 63;
+  float sum[VEC];
+  if (static_cast<int>(blockIdx.x) < row_blocks) {
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    const int tile = static_cast<int>(item % p.tiles);
+    const int64_t v = item / p.tiles;
+    if (v >= p.src.V) return;
+    const int from = p.first[v], n = p.first[v + 1] - from;
+    if (n > kRun) return;
+    const int c = group_start(tile * p.lanes + (lane & (p.lanes - 1)), VEC, p.D);
+    sum_rows<T, VEC>(static_cast<const T*>(p.dout), p.D, p.sorted + from, n, p.lanes, c, sum);
+    if (lane < p.lanes) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) sum[j] *= p.scale;
       Pack<T, VEC> k;
       k.set(sum);
-      k.store(static_cast<T*>(p.dweight) + static_cast<int64_t>(v) * p.D + c);
+      k.store(static_cast<T*>(p.dweight) + v * p.D + c);
     }
+    return;
+  }
+  const int64_t item = static_cast<int64_t>(blockIdx.x) - row_blocks, begin = item / p.tiles * kRun;
+  const int tile = static_cast<int>(item % p.tiles), total = p.first[p.src.V];
+  if (begin >= total) return;
+  // the token that holds the run's last row, if it is common and begins in the run
+  const int end = min(static_cast<int>(begin) + kRun, total);
+  const int32_t token = p.keys[p.sorted[end - 1]];
+  const int from = p.first[token], to = p.first[token + 1];
+  if (to - from <= kRun || from < begin) return;
+  // its sums: the last token of this run (the first one where it begins with the run), the first of the runs behind
+  const int c = group_start(tile * p.lanes + (lane & (p.lanes - 1)), VEC, p.D);
+  const int64_t r0 = begin / kRun, r1 = (static_cast<int64_t>(to) - 1) / kRun;
+  const float* sums = p.sums + r0 * 2 * p.D;
+  // runs r0 + 1 .. r1 in four stretches
+  const int more = static_cast<int>(r1 - r0), stretch = (more + 3) / 4;
+  const int s0 = min(wave * stretch, more), s1 = min(s0 + stretch, more);
+  sum_rows<float, VEC>(sums + static_cast<int64_t>(1 + s0) * 2 * p.D, 2 * static_cast<int64_t>(p.D), nullptr, s1 - s0, p.lanes, c, sum);
+  if (lane < p.lanes) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) parts[wave][j * 64 + lane] = sum[j];
+  }
+  __syncthreads();
+  if (wave == 0 && lane < p.lanes) {
+    Pack<float, VEC> first;
+    first.load(sums + (from == begin ? 0 : p.D) + c);
+    first.get(sum);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) sum[j] += parts[w][j * 64 + lane];
+      sum[j] *= p.scale;
+    }
+    Pack<T, VEC> k;
+    k.set(sum);
+    k.store(static_cast<T*>(p.dweight) + static_cast<int64_t>(token) * p.D + c);
   }
 }
 
@@ -124,15 +334,31 @@ rnnt_status_t check(const int32_t* labels, const rnnt_embedding_shape_t& s, Toke
   return RNNT_OK;
 }
 
-// rows that start on 16 bytes take 16-byte accesses
-bool wide_rows(int D, rnnt_dtype_t dt, const void* a, const void* b) {
-  return D * net_elem_bytes(dt) % 16 == 0 && multiple_of(16, a) && multiple_of(16, b);
+int lanes_for(int groups, int most) {
+  int n = 1;
+  while (n < most && n < groups) n *= 2;
+  return n;
 }
 
-int lanes_for(int chunks) {
-  int n = 1;
-  while (n < 256 && n < chunks) n *= 2;
-  return n;
+// Workspace of the gradient, 256-byte aligned pieces.
+struct GradLayout {
+  size_t keys, sorted, first, sums, total;
+};
+
+GradLayout grad_layout(const rnnt_embedding_shape_t& s, int64_t rows) {
+  GradLayout L{};
+  const size_t runs = static_cast<size_t>((rows + kRun - 1) / kRun);
+  size_t o = 0;
+  L.keys = o;
+  o = net_align256(o + static_cast<size_t>(rows) * sizeof(int32_t));
+  L.sorted = o;
+  o = net_align256(o + static_cast<size_t>(rows) * sizeof(int32_t));
+  L.first = o;
+  o = net_align256(o + (static_cast<size_t>(s.V) + 1) * sizeof(int32_t));
+  L.sums = o;
+  o = net_align256(o + runs * 2 * s.D * sizeof(float));
+  L.total = o;
+  return L;
 }
 
 }  // namespace
@@ -156,13 +382,14 @@ rnnt_status_t rnnt_label_embedding(const int32_t* labels, const int32_t* lens, r
   p.out = out;
   p.scale = scale;
   p.D = shape.D;
-  const bool wide = wide_rows(shape.D, shape.dtype, weight, out);
   return with_dtype(shape.dtype, [&](auto t) {
     using T = decltype(t);
     constexpr int VEC = 16 / sizeof(T);
-    p.lanes = lanes_for(wide ? shape.D / VEC : shape.D);
-    const int per = 256 / p.lanes;
-    const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(p.rows) + per - 1) / per));
+    const bool wide = shape.D >= VEC;
+    p.groups = wide ? (shape.D + VEC - 1) / VEC : shape.D;
+    p.lanes = lanes_for(p.groups, 256);
+    const int64_t per = 256 / p.lanes, blocks = (p.rows + per - 1) / per;
+    const dim3 grid(static_cast<uint32_t>(blocks < kMaxRows / 256 ? blocks : kMaxRows / 256));
     if (wide) hipLaunchKernelGGL((net_embedding<T, VEC>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((net_embedding<T, 1>), grid, dim3(256), 0, stream, p);
     return launched();
@@ -172,7 +399,8 @@ rnnt_status_t rnnt_label_embedding(const int32_t* labels, const int32_t* lens, r
 size_t rnnt_label_embedding_grad_workspace_bytes(rnnt_embedding_shape_t shape) {
   TokenSource src;
   int32_t any;
-  return check(&any, shape, &src, nullptr) == RNNT_OK ? 256 : 0;
+  if (check(&any, shape, &src, nullptr) != RNNT_OK) return 0;
+  return grad_layout(shape, static_cast<int64_t>(src.n1) * shape.B).total;
 }
 
 rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* lens, rnnt_embedding_shape_t shape,
@@ -185,20 +413,50 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   if (!dweight || (!dout && p.rows > 0)) return RNNT_ERR_NULL_PTR;
   const int64_t e = net_elem_bytes(shape.dtype);
   if (!multiple_of(e, dout) || !multiple_of(e, dweight)) return RNNT_ERR_ALIGNMENT;
+  const GradLayout L = grad_layout(shape, p.rows);
   NetWorkspace ws;
-  st = ws.take(workspace, workspace_bytes, rnnt_label_embedding_grad_workspace_bytes(shape), stream);
+  st = ws.take(workspace, workspace_bytes, L.total, stream);
   if (st != RNNT_OK) return st;
   p.dout = dout;
   p.dweight = dweight;
   p.scale = scale;
   p.D = shape.D;
-  const bool wide = wide_rows(shape.D, shape.dtype, dout, dweight);
+  p.keys = reinterpret_cast<int32_t*>(ws.ptr + L.keys);
+  p.sorted = reinterpret_cast<int32_t*>(ws.ptr + L.sorted);
+  p.first = reinterpret_cast<int32_t*>(ws.ptr + L.first);
+  p.sums = reinterpret_cast<float*>(ws.ptr + L.sums);
+  p.runs = static_cast<int32_t>((static_cast<int64_t>(p.rows) + kRun - 1) / kRun);
+  const int64_t shares = (static_cast<int64_t>(shape.V) + kSortBlocks - 1) / kSortBlocks;
+  p.per_block = static_cast<int32_t>(shares < kSortTokens ? shares : kSortTokens);
+  const dim3 sort_grid(static_cast<uint32_t>((static_cast<int64_t>(shape.V) + p.per_block - 1) / p.per_block));
+  const size_t counters = static_cast<size_t>(kSortWaves) * p.per_block * sizeof(int32_t);
+  if (p.rows > 0) {
+    const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(p.rows) + 255) / 256));
+    hipLaunchKernelGGL(net_embedding_keys, grid, dim3(256), 0, stream, p);
+    if (launched() != RNNT_OK) return RNNT_ERR_HIP;
+  }
+  hipLaunchKernelGGL(net_embedding_sort, sort_grid, dim3(64 * kSortWaves), counters, stream, p);
+  if (launched() != RNNT_OK) return RNNT_ERR_HIP;
   return with_dtype(shape.dtype, [&](auto t) {
     using T = decltype(t);
-    constexpr int VEC = 16 / sizeof(T);
-    if (wide) hipLaunchKernelGGL((net_embedding_grad<T, VEC>), dim3(shape.V), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((net_embedding_grad<T, 1>), dim3(shape.V), dim3(256), 0, stream, p);
-    return launched();
+    const auto rest = [&](auto vec) {
+      constexpr int VEC = decltype(vec)::value;
+      const int groups = (shape.D + VEC - 1) / VEC;
+      p.lanes = lanes_for(groups, 64);
+      p.tiles = (groups + p.lanes - 1) / p.lanes;
+      const int64_t run_items = static_cast<int64_t>(p.runs) * 2 * p.tiles, starts = static_cast<int64_t>(p.runs) * p.tiles;
+      const int64_t row_blocks = (static_cast<int64_t>(shape.V) * p.tiles + 3) / 4;
+      if ((run_items + 3) / 4 > kMaxRows / 256 || row_blocks + starts > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
+      if (run_items > 0) {
+        hipLaunchKernelGGL((net_embedding_runs<T, VEC>), dim3(static_cast<uint32_t>((run_items + 3) / 4)), dim3(256), 0, stream, p);
+        if (launched() != RNNT_OK) return RNNT_ERR_HIP;
+      }
+      hipLaunchKernelGGL((net_embedding_rows<T, VEC>), dim3(static_cast<uint32_t>(row_blocks + starts)), dim3(256), 0, stream, p,
+                         static_cast<int32_t>(row_blocks));
+      return launched();
+    };
+    constexpr int WIDE = 16 / sizeof(T);
+    return shape.D >= WIDE ? rest(std::integral_constant<int, WIDE>{}) : rest(std::integral_constant<int, 1>{});
   });
 }
 
