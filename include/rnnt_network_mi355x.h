@@ -85,8 +85,9 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
  * (dlast where lens[b] = 0).  dx, dz (B, L, D); dh0 (B, D) float32 or NULL.
  *
  * RNNT_ERR_BAD_SHAPE: B < 1, L < 0, D < 1, or a stride below 0.
+ * RNNT_ERR_UNSUPPORTED: L > 2^30, D > 2^21, or B * ceil(D / 64) of 2^21 or more.
  */
-#define RNNT_RECURRENCE_STATE_STEPS 16
+#define RNNT_RECURRENCE_STATE_STEPS 8
 
 typedef struct {
   int32_t B, L, D;

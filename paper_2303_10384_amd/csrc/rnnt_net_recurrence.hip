@@ -8,7 +8,15 @@
 namespace rnnt {
 namespace {
 
-constexpr int kStateSteps = RNNT_RECURRENCE_STATE_STEPS;
+// A block takes a tile of channels of one sequence and goes over its steps kTileSteps at a time, kSteps of them to
+// a wave: a wave scans its steps from a zero state and multiplies their gates up, the waves' (product, state) pairs
+// meet in LDS, and every wave adds the state that arrives at its first step, h_j = S_j + P_j h_in.  x and z are
+// read once, the next tile's while this one is computed.
+// Where sequences and channel tiles are too few to fill the chip, the steps are cut into segments: a first kernel
+// finds each segment's pair, the second one begins each block at the state that the pairs before it give.
+constexpr int kSteps = RNNT_RECURRENCE_STATE_STEPS;
+constexpr int kWaves = 16;
+constexpr int kTileSteps = kSteps * kWaves;
 
 struct RecurrenceParams {
   const void *x, *z;
@@ -17,103 +25,451 @@ struct RecurrenceParams {
   const float* h0;
   void* h;
   float* last;
-  float* states;  // (B, ceil(L / kStateSteps), D), or null
-  int32_t B, L, D, n_states;
-};
-
-__device__ __forceinline__ int length_of(const int32_t* lens, int b, int L) { return lens ? lens[b] : L; }
-
-// One thread to a channel, step by step.
-template <typename T>
-__global__ __launch_bounds__(64) void net_recurrence(RecurrenceParams p) {
-  const int c = static_cast<int>(blockIdx.x) * 64 + static_cast<int>(threadIdx.x), b = static_cast<int>(blockIdx.y);
-  if (c >= p.D) return;
-  const int len = length_of(p.lens, b, p.L);
-  const bool bad = len < 0 || len > p.L;
-  const T* x = static_cast<const T*>(p.x) + b * p.x_sb + c;
-  const T* z = static_cast<const T*>(p.z) + b * p.z_sb + c;
-  T* h = static_cast<T*>(p.h) + static_cast<int64_t>(b) * p.L * p.D + c;
-  const int64_t bc = static_cast<int64_t>(b) * p.D + c;
-  float* st = p.states ? p.states + static_cast<int64_t>(b) * p.n_states * p.D + c : nullptr;
-  float s = bad ? __builtin_nanf("") : p.h0 ? p.h0[bc] : 0.f;
-  for (int t = 0; t < p.L; ++t) {
-    if (st && t % kStateSteps == 0) st[static_cast<int64_t>(t / kStateSteps) * p.D] = s;
-    float o = bad ? s : 0.f;
-    if (!bad && t < len) {
-      float a, g;
-      gate(ElemTraits<T>::load1(z + t * p.z_st), a, g);
-      s = __builtin_fmaf(g, ElemTraits<T>::load1(x + t * p.x_st) - s, s);
-      o = s;
-    }
-    ElemTraits<T>::store1(h + static_cast<int64_t>(t) * p.D, o);
-  }
-  p.last[bc] = s;
-}
-
-struct RecurrenceGradParams {
-  const void *x, *z;
-  int64_t x_sb, x_st, z_sb, z_st;
-  const int32_t* lens;
-  const float* states;
+  float* states;  // (B, n_states, D), or null
+  // backward
   const void* dh;
   const float* dlast;
   void *dx, *dz;
   float* dh0;
-  int32_t B, L, D, n_states;
+  float2* pairs;  // (B, segments, D) of the segments
+  int32_t B, L, D, n_states, tiles, segments, seg_steps;
 };
 
-template <typename T>
-__global__ __launch_bounds__(64) void net_recurrence_grad(RecurrenceGradParams p) {
-  const int c = static_cast<int>(blockIdx.x) * 64 + static_cast<int>(threadIdx.x), b = static_cast<int>(blockIdx.y);
-  if (c >= p.D) return;
-  int len = length_of(p.lens, b, p.L);
-  const bool bad = len < 0 || len > p.L;
-  if (bad) len = 0;
-  const T* x = static_cast<const T*>(p.x) + b * p.x_sb + c;
-  const T* z = static_cast<const T*>(p.z) + b * p.z_sb + c;
-  const int64_t base = static_cast<int64_t>(b) * p.L * p.D + c, bc = static_cast<int64_t>(b) * p.D + c;
-  const T* dh = p.dh ? static_cast<const T*>(p.dh) + base : nullptr;
-  T *dx = static_cast<T*>(p.dx) + base, *dz = static_cast<T*>(p.dz) + base;
-  float d = bad || !p.dlast ? 0.f : p.dlast[bc];
-  for (int t0 = (p.L - 1) / kStateSteps * kStateSteps; t0 >= 0 && p.L > 0; t0 -= kStateSteps) {
-    float before[kStateSteps], xs[kStateSteps], as[kStateSteps], gs[kStateSteps];
-    float s = p.states[(static_cast<int64_t>(b) * p.n_states + t0 / kStateSteps) * p.D + c];
+// The part of the work that a block has, and its sequence's length.
+struct Place {
+  int b, tile, segment, begin, end, len;  // steps [begin, end) of the segment
+  bool bad;
+
+  __device__ __forceinline__ explicit Place(const RecurrenceParams& p) {
+    const int i = static_cast<int>(blockIdx.x);
+    tile = i % p.tiles;
+    segment = i / p.tiles % p.segments;
+    b = i / p.tiles / p.segments;
+    len = p.lens ? p.lens[b] : p.L;
+    bad = len < 0 || len > p.L;
+    if (bad) len = 0;
+    begin = segment * p.seg_steps;
+    end = min(p.L - begin, p.seg_steps) + begin;
+  }
+};
+
+template <typename T, int VEC>
+struct Rows {
+  Pack<T, VEC> r[kSteps];
+
+  // rows t .. t + kSteps - 1, the last valid one in the place of those past it
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int t, int len, int c) {
 #pragma unroll
-    for (int j = 0; j < kStateSteps; ++j) {
-      before[j] = s;
-      if (t0 + j < len) {
-        gate(ElemTraits<T>::load1(z + (t0 + j) * p.z_st), as[j], gs[j]);
-        xs[j] = ElemTraits<T>::load1(x + (t0 + j) * p.x_st);
-        s = __builtin_fmaf(gs[j], xs[j] - s, s);
-      }
-    }
+    for (int j = 0; j < kSteps; ++j) r[j].load(base + min(t + j, len - 1) * stride + c);
+  }
+};
+
+// rows t + j of an output of D channels, those from `end` on left out (an offset past the buffer)
+template <typename T, int VEC>
+struct RowStore {
+  __amdgpu_buffer_rsrc_t r;
+  int left;   // steps from the buffer's first row to the end of the segment
+  int D, c;
+
+  // base: row `first` of a dense output, of which `left` steps belong to the segment
+  __device__ __forceinline__ RowStore(T* base, int64_t first, int left_, int D_, int c_)
+      : r(make_buffer(base + first * D_, static_cast<int64_t>(min(left_, kTileSteps)) * D_ * static_cast<int64_t>(sizeof(T)))),
+        left(left_), D(D_), c(c_) {}
+  __device__ __forceinline__ void put(int row, const float* f) const {
+    Pack<T, VEC> k;
+    k.set(f);
+    const int off = row < left ? (row * D + c) * static_cast<int>(sizeof(T)) : kOutOfRange;
+    if constexpr (Pack<T, VEC>::kBytes == 2)
+      __builtin_amdgcn_raw_buffer_store_b16(static_cast<uint16_t>(k.w[0]), r, off, 0, 0);
+    else
+      __builtin_amdgcn_raw_buffer_store_b32(k.w[0], r, off, 0, 0);
+  }
+};
+
+// The (product, state) pairs of a block's waves, two sets of them in turn.
+template <int VEC>
+struct PairBoard {
+  float2 at[2][kWaves][VEC][64];
+
+  __device__ __forceinline__ void put(int set, int wave, int lane, const float* A, const float* S) {
 #pragma unroll
-    for (int j = kStateSteps - 1; j >= 0; --j) {
-      const int t = t0 + j;
-      if (t >= p.L) continue;
-      float ox = 0.f, oz = 0.f;
-      if (t < len) {
-        const float total = d + (dh ? ElemTraits<T>::load1(dh + static_cast<int64_t>(t) * p.D) : 0.f);
-        ox = gs[j] * total;
-        oz = total * (before[j] - xs[j]) * (as[j] * gs[j]);
-        d = as[j] * total;
+    for (int v = 0; v < VEC; ++v) at[set][wave][v][lane] = make_float2(A[v], S[v]);
+  }
+  // carry through all waves' pairs, in order or backwards; `mine` is what arrives at `wave`
+  template <bool BACK>
+  __device__ __forceinline__ void compose(int set, int wave, int lane, float* carry, float* mine) const {
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const int w = BACK ? kWaves - 1 - i : i;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float2 k = at[set][w][v][lane];
+        if (w == wave) mine[v] = carry[v];
+        carry[v] = __builtin_fmaf(k.x, carry[v], k.y);
       }
-      ElemTraits<T>::store1(dx + static_cast<int64_t>(t) * p.D, ox);
-      ElemTraits<T>::store1(dz + static_cast<int64_t>(t) * p.D, oz);
     }
   }
-  if (p.dh0) p.dh0[bc] = d;
+};
+
+// carry through the pairs of the segments before (BACK: behind) a block's, the waves a stretch each
+template <int VEC, bool BACK>
+__device__ __forceinline__ void carry_in(const RecurrenceParams& p, const Place& at, int c, int wave, int lane, PairBoard<VEC>& board,
+                                         float* carry) {
+  const int n = BACK ? p.segments - 1 - at.segment : at.segment;
+  if (n == 0) return;
+  const int share = (n + kWaves - 1) / kWaves, from = min(wave * share, n), to = min(from + share, n);
+  const float2* pairs = p.pairs + (static_cast<int64_t>(at.b) * p.segments + (BACK ? at.segment + 1 : 0)) * p.D + c;
+  float A[VEC], S[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    A[v] = 1.f;
+    S[v] = 0.f;
+  }
+#pragma unroll 4
+  for (int i = from; i < to; ++i) {
+    const int seg = BACK ? to - 1 - (i - from) : i;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float2 k = pairs[static_cast<int64_t>(seg) * p.D + v];
+      S[v] = __builtin_fmaf(k.x, S[v], k.y);
+      A[v] *= k.x;
+    }
+  }
+  board.put(1, wave, lane, A, S);
+  __syncthreads();
+  float none[VEC];
+  board.template compose<BACK>(1, wave, lane, carry, none);
+}
+
+template <typename T, int VEC>
+__global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p) {
+  __shared__ PairBoard<VEC> board;
+  const Place at(p);
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  const int c = min((at.tile * 64 + lane) * VEC, p.D - VEC);
+  const int64_t bc = static_cast<int64_t>(at.b) * p.D + c;
+  float carry[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) carry[v] = at.bad ? __builtin_nanf("") : p.h0 ? p.h0[bc + v] : 0.f;
+  carry_in<VEC, false>(p, at, c, wave, lane, board, carry);
+  T* h = static_cast<T*>(p.h);
+  const int64_t row0 = static_cast<int64_t>(at.b) * p.L;
+  int t0 = at.begin;
+  if (t0 < at.len) {
+    const T* x = static_cast<const T*>(p.x) + at.b * p.x_sb;
+    const T* z = static_cast<const T*>(p.z) + at.b * p.z_sb;
+    Rows<T, VEC> xs, zs;
+    xs.load(x, p.x_st, t0 + wave * kSteps, at.len, c);
+    zs.load(z, p.z_st, t0 + wave * kSteps, at.len, c);
+    for (int set = 0; t0 < min(at.end, at.len); t0 += kTileSteps, set ^= 1) {
+      const int t = t0 + wave * kSteps, live = at.len - t;
+      float S[kSteps][VEC], P[kSteps][VEC], s[VEC], q[VEC];
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        s[v] = 0.f;
+        q[v] = 1.f;
+      }
+      const bool whole = live >= kSteps;
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        float xf[VEC], zf[VEC];
+        xs.r[j].get(xf);
+        zs.r[j].get(zf);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          float a, g;
+          gate(zf[v], a, g);
+          const float next = __builtin_fmaf(g, xf[v] - s[v], s[v]);
+          s[v] = whole || j < live ? next : s[v];
+          q[v] = whole || j < live ? a * q[v] : q[v];
+          S[j][v] = s[v];
+          P[j][v] = q[v];
+        }
+      }
+      // the next tile's rows, on their way during the rest
+      xs.load(x, p.x_st, t + kTileSteps, at.len, c);
+      zs.load(z, p.z_st, t + kTileSteps, at.len, c);
+      board.put(set, wave, lane, q, s);
+      __syncthreads();  // one to a tile: the other set is written before the next
+      float in[VEC];
+      board.template compose<false>(set, wave, lane, carry, in);
+      if (p.states && t < at.end) {
+        Pack<float, VEC> k;
+        k.set(in);
+        k.store(p.states + (static_cast<int64_t>(at.b) * p.n_states + t / kSteps) * p.D + c);
+      }
+      const RowStore<T, VEC> out(h, row0 + t0, at.end - t0, p.D, c);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        float f[VEC];
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) f[v] = whole || j < live ? __builtin_fmaf(P[j][v], in[v], S[j][v]) : 0.f;
+        out.put(wave * kSteps + j, f);
+      }
+    }
+  }
+  for (; t0 < at.end; t0 += kTileSteps) {  // behind the sequence
+    const RowStore<T, VEC> out(h, row0 + t0, at.end - t0, p.D, c);
+    float f[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) f[v] = at.bad ? __builtin_nanf("") : 0.f;
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) out.put(wave * kSteps + j, f);
+  }
+  if (at.segment == p.segments - 1 && wave == 0) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) p.last[bc + v] = carry[v];
+  }
+}
+
+// A segment's pair: forward (BACK false) of h, backward of the gradient's sums.  A wave streams a stretch of its
+// steps; nothing is exchanged before the end.
+template <typename T, int VEC, bool BACK>
+__global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrenceParams p) {
+  __shared__ PairBoard<VEC> board;
+  const Place at(p);
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  const int c = min((at.tile * 64 + lane) * VEC, p.D - VEC);
+  // its steps [from, to), whole batches of kSteps but for the sequence's end
+  const int share = (p.seg_steps / kSteps + kWaves - 1) / kWaves * kSteps;
+  const int stop = min(at.end, at.len);
+  const int from = min(at.begin + wave * share, stop), to = min(from + share, stop);
+  float A[VEC], S[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    A[v] = 1.f;
+    S[v] = 0.f;
+  }
+  const int batches = max(0, (to - from + kSteps - 1) / kSteps);
+  if (batches > 0) {
+    const T* z = static_cast<const T*>(p.z) + at.b * p.z_sb;
+    const T* x = BACK ? static_cast<const T*>(p.dh) + static_cast<int64_t>(at.b) * p.L * p.D : static_cast<const T*>(p.x) + at.b * p.x_sb;
+    const int64_t x_st = BACK ? p.D : p.x_st;
+    const bool with_x = !BACK || p.dh != nullptr;
+    Rows<T, VEC> xs, zs;
+    if (!with_x) {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) xs.r[j].zero();
+    }
+    const auto step_of = [&](int i) { return from + (BACK ? batches - 1 - i : i) * kSteps; };
+    if (with_x) xs.load(x, x_st, step_of(0), to, c);
+    zs.load(z, p.z_st, step_of(0), to, c);
+    for (int i = 0; i < batches; ++i) {
+      const Rows<T, VEC> xn = xs, zn = zs;
+      const int live = to - step_of(i);
+      if (i + 1 < batches) {
+        if (with_x) xs.load(x, x_st, step_of(i + 1), to, c);
+        zs.load(z, p.z_st, step_of(i + 1), to, c);
+      }
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) {
+        const int j = BACK ? kSteps - 1 - k : k;
+        float xf[VEC], zf[VEC];
+        xn.r[j].get(xf);
+        zn.r[j].get(zf);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          float a, g;
+          gate(zf[v], a, g);
+          const float next = BACK ? a * (S[v] + xf[v]) : __builtin_fmaf(g, xf[v] - S[v], S[v]);
+          S[v] = j < live ? next : S[v];
+          A[v] = j < live ? a * A[v] : A[v];
+        }
+      }
+    }
+  }
+  board.put(0, wave, lane, A, S);
+  __syncthreads();
+  if (wave != 0) return;
+  // the waves' pairs into one: the state from zero, and the product
+  float2* out = p.pairs + (static_cast<int64_t>(at.b) * p.segments + at.segment) * p.D + c;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    float prod = 1.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float2 k = board.at[0][BACK ? kWaves - 1 - i : i][v][lane];
+      sum = __builtin_fmaf(k.x, sum, k.y);
+      prod *= k.x;
+    }
+    out[v] = make_float2(prod, sum);
+  }
+}
+
+// The gradient goes the other way: s_t = dh_t + a_{t+1} s_{t+1}, tile by tile from the end, its carry d = a s.  The
+// states that dz needs are formed again from the one stored before the wave's first step.
+template <typename T, int VEC>
+__global__ __launch_bounds__(64 * kWaves) void net_recurrence_grad(RecurrenceParams p) {
+  __shared__ PairBoard<VEC> board;
+  const Place at(p);
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  const int c = min((at.tile * 64 + lane) * VEC, p.D - VEC);
+  const int64_t bc = static_cast<int64_t>(at.b) * p.D + c, row0 = static_cast<int64_t>(at.b) * p.L;
+  T *dx = static_cast<T*>(p.dx), *dz = static_cast<T*>(p.dz);
+  float carry[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) carry[v] = at.bad || !p.dlast ? 0.f : p.dlast[bc + v];
+  carry_in<VEC, true>(p, at, c, wave, lane, board, carry);
+  const int tiles = (at.end - at.begin + kTileSteps - 1) / kTileSteps;
+  // tiles that hold steps of the sequence; the ones behind it are zero
+  const int live_tiles = max(0, min(tiles, (at.len - at.begin + kTileSteps - 1) / kTileSteps));
+  float zero[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) zero[v] = 0.f;
+  for (int i = live_tiles; i < tiles; ++i) {
+    const int t0 = at.begin + i * kTileSteps;
+    const RowStore<T, VEC> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      ox.put(wave * kSteps + j, zero);
+      oz.put(wave * kSteps + j, zero);
+    }
+  }
+  if (live_tiles > 0) {
+    const T* x = static_cast<const T*>(p.x) + at.b * p.x_sb;
+    const T* z = static_cast<const T*>(p.z) + at.b * p.z_sb;
+    const T* dh = static_cast<const T*>(p.dh) + row0 * p.D;
+    const float* states = p.states + static_cast<int64_t>(at.b) * p.n_states * p.D + c;
+    const bool with_dh = p.dh != nullptr;
+    Rows<T, VEC> xs, zs, ds;
+    if (!with_dh) {
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) ds.r[j].zero();
+    }
+    Pack<float, VEC> st;
+    const auto load = [&](int i) {
+      const int t = at.begin + i * kTileSteps + wave * kSteps;
+      xs.load(x, p.x_st, t, at.len, c);
+      zs.load(z, p.z_st, t, at.len, c);
+      if (with_dh) ds.load(dh, p.D, t, at.len, c);
+      st.load(states + static_cast<int64_t>(min(t, at.len - 1) / kSteps) * p.D);
+    };
+    load(live_tiles - 1);
+    for (int i = live_tiles - 1, set = 0; i >= 0; --i, set ^= 1) {
+      const int t0 = at.begin + i * kTileSteps, live = at.len - t0 - wave * kSteps;
+      const bool whole = live >= kSteps;
+      float a[kSteps][VEC], g[kSteps][VEC], w[kSteps][VEC], s[VEC], A[VEC], S[VEC];
+      st.get(s);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        float xf[VEC], zf[VEC];
+        xs.r[j].get(xf);
+        zs.r[j].get(zf);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          gate(zf[v], a[j][v], g[j][v]);
+          const float off = xf[v] - s[v];
+          w[j][v] = -off * (a[j][v] * g[j][v]);
+          s[v] = __builtin_fmaf(g[j][v], off, s[v]);
+        }
+      }
+      Rows<T, VEC> d = ds;
+      if (i > 0) load(i - 1);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        A[v] = 1.f;
+        S[v] = 0.f;
+      }
+#pragma unroll
+      for (int j = kSteps - 1; j >= 0; --j) {
+        float df[VEC];
+        d.r[j].get(df);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          const float next = a[j][v] * (S[v] + df[v]);
+          S[v] = whole || j < live ? next : S[v];
+          A[v] = whole || j < live ? a[j][v] * A[v] : A[v];
+        }
+      }
+      board.put(set, wave, lane, A, S);
+      __syncthreads();  // one to a tile: the other set is written before the next
+      float in[VEC];
+      board.template compose<true>(set, wave, lane, carry, in);
+      const RowStore<T, VEC> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
+#pragma unroll
+      for (int j = kSteps - 1; j >= 0; --j) {
+        float df[VEC], fx[VEC], fz[VEC];
+        d.r[j].get(df);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          const bool on = whole || j < live;
+          const float total = in[v] + df[v];
+          fx[v] = on ? g[j][v] * total : 0.f;
+          fz[v] = on ? w[j][v] * total : 0.f;
+          in[v] = on ? a[j][v] * total : in[v];
+        }
+        ox.put(wave * kSteps + j, fx);
+        oz.put(wave * kSteps + j, fz);
+      }
+    }
+  }
+  if (p.dh0 && at.segment == 0 && wave == 0) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) p.dh0[bc + v] = at.bad ? 0.f : carry[v];
+  }
 }
 
 rnnt_status_t check(const rnnt_recurrence_shape_t& s) {
   if (s.B < 1 || s.L < 0 || s.D < 1 || s.x_stride_b < 0 || s.x_stride_t < 0 || s.z_stride_b < 0 || s.z_stride_t < 0)
     return RNNT_ERR_BAD_SHAPE;
   if (!net_dtype_known(s.dtype)) return RNNT_ERR_BAD_DTYPE;
-  if (s.B > 65535) return RNNT_ERR_UNSUPPORTED;
+  // a tile's rows are one buffer of less than 2^31 bytes; threads of a launch are a 32-bit count
+  if (s.D > (1 << 21) || s.L > (1 << 30) || static_cast<int64_t>(s.B) * ((s.D + 63) / 64) > kMaxRows / (64 * kWaves))
+    return RNNT_ERR_UNSUPPORTED;
   return RNNT_OK;
 }
 
-int state_count(int L) { return (L + kStateSteps - 1) / kStateSteps; }
+int state_count(int L) { return static_cast<int>((static_cast<int64_t>(L) + kSteps - 1) / kSteps); }
+
+// Blocks to a sequence: one, or as many segments of at least two tiles as give the chip two blocks to a CU.
+// Segments read x and z twice (5/3 of the bytes forward, 7/5 backward), which pays below about 3/5 of a chip.
+void segments_of(const rnnt_recurrence_shape_t& s, RecurrenceParams* p) {
+  const int vec = s.dtype == RNNT_DTYPE_F32 || s.D < 2 ? 1 : 2;
+  p->tiles = (s.D + 64 * vec - 1) / (64 * vec);
+  const int64_t blocks = static_cast<int64_t>(s.B) * p->tiles, steps = (static_cast<int64_t>(s.L) + kTileSteps - 1) / kTileSteps;
+  p->segments = 1;
+  p->seg_steps = s.L;
+  if (blocks < 150 && steps >= 4) {
+    int64_t want = (512 + blocks - 1) / blocks;
+    if (want > steps / 2) want = steps / 2;
+    const int64_t per = (steps + want - 1) / want;
+    p->segments = static_cast<int32_t>((steps + per - 1) / per);
+    p->seg_steps = static_cast<int32_t>(per * kTileSteps);
+  }
+}
+
+size_t pair_bytes(const rnnt_recurrence_shape_t& s) {
+  RecurrenceParams p{};
+  segments_of(s, &p);
+  return net_align256(p.segments > 1 ? static_cast<size_t>(s.B) * p.segments * s.D * sizeof(float2) : 256);
+}
+
+template <typename F>
+rnnt_status_t with_vector(const rnnt_recurrence_shape_t& s, F&& f) {
+  return with_dtype(s.dtype, [&](auto t) {
+    using T = decltype(t);
+    if constexpr (sizeof(T) == 4) return f(t, std::integral_constant<int, 1>{});
+    else return s.D < 2 ? f(t, std::integral_constant<int, 1>{}) : f(t, std::integral_constant<int, 2>{});
+  });
+}
+
+RecurrenceParams params_of(const void* x, const void* z, const rnnt_recurrence_shape_t& s, const int32_t* lens, char* ws) {
+  RecurrenceParams p{};
+  p.x = x;
+  p.z = z;
+  p.x_sb = s.x_stride_b;
+  p.x_st = s.x_stride_t;
+  p.z_sb = s.z_stride_b;
+  p.z_st = s.z_stride_t;
+  p.lens = lens;
+  p.B = s.B;
+  p.L = s.L;
+  p.D = s.D;
+  p.n_states = state_count(s.L);
+  p.pairs = reinterpret_cast<float2*>(ws);
+  segments_of(s, &p);
+  return p;
+}
 
 }  // namespace
 }  // namespace rnnt
@@ -127,7 +483,7 @@ size_t rnnt_recurrence_states_bytes(rnnt_recurrence_shape_t shape) {
   return static_cast<size_t>(shape.B) * state_count(shape.L) * shape.D * sizeof(float);
 }
 
-size_t rnnt_recurrence_workspace_bytes(rnnt_recurrence_shape_t shape) { return check(shape) == RNNT_OK ? 256 : 0; }
+size_t rnnt_recurrence_workspace_bytes(rnnt_recurrence_shape_t shape) { return check(shape) == RNNT_OK ? pair_bytes(shape) : 0; }
 
 rnnt_status_t rnnt_recurrence(const void* x, const void* z, rnnt_recurrence_shape_t shape, const int32_t* lens,
                               const float* h0, void* h_out, float* last_out, void* states_out, void* workspace,
@@ -142,11 +498,20 @@ rnnt_status_t rnnt_recurrence(const void* x, const void* z, rnnt_recurrence_shap
   NetWorkspace ws;
   st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
-  RecurrenceParams p{x, z, shape.x_stride_b, shape.x_stride_t, shape.z_stride_b, shape.z_stride_t, lens, h0, h_out,
-                     last_out, static_cast<float*>(states_out), shape.B, shape.L, shape.D, state_count(shape.L)};
-  return with_dtype(shape.dtype, [&](auto t) {
+  RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);
+  p.h0 = h0;
+  p.h = h_out;
+  p.last = last_out;
+  p.states = static_cast<float*>(states_out);
+  const dim3 grid(static_cast<uint32_t>(p.B * p.tiles * p.segments));
+  return with_vector(shape, [&](auto t, auto vec) {
     using T = decltype(t);
-    hipLaunchKernelGGL((net_recurrence<T>), dim3((shape.D + 63) / 64, shape.B), dim3(64), 0, stream, p);
+    constexpr int VEC = decltype(vec)::value;
+    if (p.segments > 1) {
+      hipLaunchKernelGGL((net_recurrence_pairs<T, VEC, false>), grid, dim3(64 * kWaves), 0, stream, p);
+      if (launched() != RNNT_OK) return RNNT_ERR_HIP;
+    }
+    hipLaunchKernelGGL((net_recurrence<T, VEC>), grid, dim3(64 * kWaves), 0, stream, p);
     return launched();
   });
 }
@@ -164,12 +529,22 @@ rnnt_status_t rnnt_recurrence_grad(const void* x, const void* z, rnnt_recurrence
   NetWorkspace ws;
   st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
-  RecurrenceGradParams p{x, z, shape.x_stride_b, shape.x_stride_t, shape.z_stride_b, shape.z_stride_t, lens,
-                         static_cast<const float*>(states), dh, dlast, dx, dz, dh0, shape.B, shape.L, shape.D,
-                         state_count(shape.L)};
-  return with_dtype(shape.dtype, [&](auto t) {
+  RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);
+  p.states = const_cast<float*>(static_cast<const float*>(states));
+  p.dh = dh;
+  p.dlast = dlast;
+  p.dx = dx;
+  p.dz = dz;
+  p.dh0 = dh0;
+  const dim3 grid(static_cast<uint32_t>(p.B * p.tiles * p.segments));
+  return with_vector(shape, [&](auto t, auto vec) {
     using T = decltype(t);
-    hipLaunchKernelGGL((net_recurrence_grad<T>), dim3((shape.D + 63) / 64, shape.B), dim3(64), 0, stream, p);
+    constexpr int VEC = decltype(vec)::value;
+    if (p.segments > 1) {
+      hipLaunchKernelGGL((net_recurrence_pairs<T, VEC, true>), grid, dim3(64 * kWaves), 0, stream, p);
+      if (launched() != RNNT_OK) return RNNT_ERR_HIP;
+    }
+    hipLaunchKernelGGL((net_recurrence_grad<T, VEC>), grid, dim3(64 * kWaves), 0, stream, p);
     return launched();
   });
 }

@@ -23,7 +23,7 @@ from torch.autograd.function import once_differentiable
 from .binding import RNNT_OK, RNNTError, _call_workspace, _ptr, _stream_handle, _workspace_args, dtype_code, load_library
 
 ACTIVATIONS = {"relu": 0, "tanh": 1}
-STATE_STEPS = 16  # RNNT_RECURRENCE_STATE_STEPS
+STATE_STEPS = 8  # RNNT_RECURRENCE_STATE_STEPS
 
 # every symbol declared in include/rnnt_network_mi355x.h
 EXPORTED = ("rnnt_label_embedding", "rnnt_label_embedding_grad_workspace_bytes", "rnnt_label_embedding_grad",
