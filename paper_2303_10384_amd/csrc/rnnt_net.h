@@ -133,9 +133,11 @@ __device__ __forceinline__ float exp_neg(float y) {
 }
 
 // a = sigmoid(z) and g = 1 - a = sigmoid(-z), each to float32's relative accuracy (1 - a as a
-// difference would lose it where the gate is nearly open).
+// difference would lose it where the gate is nearly open).  For z of 16 bits the exponent's own rounding,
+// |z| 2^-24 of the small one of the two, is left in: z is known to 2^-12 of itself at best.
+template <typename T>
 __device__ __forceinline__ void gate(float z, float& a, float& g) {
-  const float e = exp_neg(__builtin_fabsf(z));
+  const float y = __builtin_fabsf(z), e = sizeof(T) == 4 ? exp_neg(y) : fast_exp2(y * -kLog2eF);
   const float big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
   a = z < 0.f ? small : big;
   g = z < 0.f ? big : small;

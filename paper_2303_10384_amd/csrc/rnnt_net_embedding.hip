@@ -41,29 +41,35 @@ struct EmbeddingParams {
   int32_t D, rows, lanes, groups;  // lanes: threads to a row, a power of two; groups: of VEC elements in a row
 };
 
+// Four rows to a thread: a row's label, then its weights, then the store wait for one another, the rows do not.
+constexpr int kRowsAtOnce = 4;
+
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void net_embedding(EmbeddingParams p) {
-  const int per = 256 / p.lanes, step = static_cast<int>(gridDim.x) * per;
-  for (int64_t r = static_cast<int64_t>(blockIdx.x) * per + static_cast<int>(threadIdx.x) / p.lanes; r < p.rows; r += step) {
-    const int row = static_cast<int>(r);
-    const int32_t v = token_at(p.src, row);
-    const T* w = static_cast<const T*>(p.weight) + static_cast<int64_t>(v) * p.D;
-    T* o = static_cast<T*>(p.out) + static_cast<int64_t>(row) * p.D;
+  const int per = 256 / p.lanes;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * per * kRowsAtOnce;
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * per * kRowsAtOnce + static_cast<int>(threadIdx.x) / p.lanes; r0 < p.rows; r0 += step) {
+    int32_t v[kRowsAtOnce], row[kRowsAtOnce];
+#pragma unroll
+    for (int i = 0; i < kRowsAtOnce; ++i) {  // a row past the last one is the last one again
+      row[i] = static_cast<int32_t>(min(r0 + i * per, static_cast<int64_t>(p.rows) - 1));
+      v[i] = token_at(p.src, row[i]);
+    }
     for (int g = static_cast<int>(threadIdx.x) & (p.lanes - 1); g < p.groups; g += p.lanes) {
       const int c = group_start(g, VEC, p.D);
-      float f[VEC];
-      Pack<T, VEC> k;
-      if (v >= 0) {
-        k.load(w + c);
-        k.get(f);
+      Pack<T, VEC> k[kRowsAtOnce];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) f[j] *= p.scale;
-      } else {
+      for (int i = 0; i < kRowsAtOnce; ++i)
+        k[i].load(static_cast<const T*>(p.weight) + static_cast<int64_t>(max(v[i], 0)) * p.D + c);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) f[j] = v == kBadRow ? __builtin_nanf("") : 0.f;
+      for (int i = 0; i < kRowsAtOnce; ++i) {
+        float f[VEC];
+        k[i].get(f);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) f[j] = v[i] >= 0 ? f[j] * p.scale : v[i] == kBadRow ? __builtin_nanf("") : 0.f;
+        k[i].set(f);
+        k[i].store(static_cast<T*>(p.out) + static_cast<int64_t>(row[i]) * p.D + c);
       }
-      k.set(f);
-      k.store(o + c);
     }
   }
 }
@@ -75,7 +81,8 @@ __global__ __launch_bounds__(256) void net_embedding(EmbeddingParams p) {
 
 constexpr int32_t kNoKey = 0x7fffffff;  // a row without a token, past every token
 constexpr int kSortWaves = 16;
-constexpr int kSortTokens = 960;   // most tokens of a sorting block: 16 x 960 counters in LDS, a thread to a token
+constexpr int kSortTokens = 384;   // most tokens of a sorting block (a thread to a token)
+constexpr int kSortFound = 384;    // rows that a wave keeps
 constexpr int kSortBlocks = 256;   // one to a CU, each looks at every row
 constexpr int kRun = 64;
 
@@ -100,24 +107,22 @@ __global__ __launch_bounds__(256) void net_embedding_keys(EmbeddingGradParams p)
   p.keys[r] = v < 0 ? kNoKey : v;
 }
 
-// A counting sort in which every block looks at all rows and places those of its own few tokens: no pass over a
-// table of counters between blocks, one launch, and the rows of a token in order (a wave takes a stretch of the rows
-// and knows from the first look how many of each token the waves before it have).  The rows are read from L2:
-// 131072 of them are 0.5 MB to a block.
-__global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingGradParams p) {
-  extern __shared__ int32_t count[];  // [kSortWaves][per_block], then where a wave's next row of a token goes
-  __shared__ int32_t below[kSortWaves], wave_sum[kSortWaves];
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
-  const int64_t lo64 = static_cast<int64_t>(blockIdx.x) * p.per_block;
-  if (lo64 >= p.src.V) return;
-  const int lo = static_cast<int>(lo64), n = min(p.per_block, p.src.V - lo);
-  for (int i = threadIdx.x; i < kSortWaves * p.per_block; i += 64 * kSortWaves) count[i] = 0;
-  __syncthreads();
-  const int64_t stretch = ((static_cast<int64_t>(p.rows) + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-  const int64_t begin = wave * stretch, end = min(begin + stretch, static_cast<int64_t>(p.rows));
-  int32_t* mine = count + wave * p.per_block;
+// A counting sort in which every block looks at all rows and places those of its own few tokens: no table of
+// counters between blocks, one launch, and the rows of a token in order (a wave takes a stretch of the rows and
+// learns how many of each token the waves before it have).  The rows are read from L2: 131072 of them are 0.5 MB
+// to a block.  What a wave finds it keeps in LDS, and looks at the rows again only where that overflows (a
+// token with many rows).
+struct SortBoard {
+  int32_t place[kSortWaves][kSortTokens];   // rows of a token in a wave's stretch, then where its next one goes
+  int32_t found[kSortWaves][kSortFound];    // rows of this block's tokens, in order
+  uint16_t token[kSortWaves][kSortFound];   // their tokens, less the block's first
+  int32_t below[kSortWaves], sum[kSortWaves];
+};
+
+// f(row, key - lo) for the 64 rows of every group of a stretch, the keys of eight groups on their way at once
+template <typename F>
+__device__ __forceinline__ void for_rows(const EmbeddingGradParams& p, int64_t begin, int64_t end, int lane, F&& f) {
   constexpr int BATCH = 8;
-  int less = 0;
   for (int64_t r = begin + lane; r < end + lane; r += 64 * BATCH) {
     int32_t key[BATCH];
 #pragma unroll
@@ -127,168 +132,207 @@ __global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingG
       key[i] = at < end ? key[i] : kNoKey;
     }
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-      less += __popcll(__ballot(key[i] < lo));
-      const uint32_t d = static_cast<uint32_t>(key[i]) - static_cast<uint32_t>(lo);
-      if (d < static_cast<uint32_t>(n)) atomicAdd(&mine[d], 1);
-    }
-  }
-  if (lane == 0) below[wave] = less;
-  __syncthreads();
-  // exclusive sums over (token, wave)
-  int base = 0;
-#pragma unroll
-  for (int w = 0; w < kSortWaves; ++w) base += below[w];
-  {
-    const int t = static_cast<int>(threadIdx.x);  // per_block is at most the block's threads
-    int total = 0;
-    if (t < n) {
-#pragma unroll
-      for (int w = 0; w < kSortWaves; ++w) total += count[w * p.per_block + t];
-    }
-    int upto = total;  // inclusive over the wave
-    for (int off = 1; off < 64; off <<= 1) {
-      const int v = __shfl_up(upto, off);
-      if (lane >= off) upto += v;
-    }
-    if (lane == 63) wave_sum[wave] = upto;
-    __syncthreads();
-    int at = base + upto - total;
-    for (int w = 0; w < wave; ++w) at += wave_sum[w];
-    if (t < n) {
-      p.first[lo + t] = at;
-      if (lo + t == p.src.V - 1) p.first[p.src.V] = at + total;
-#pragma unroll
-      for (int w = 0; w < kSortWaves; ++w) {
-        const int c = count[w * p.per_block + t];
-        count[w * p.per_block + t] = at;
-        at += c;
-      }
-    }
-  }
-  __syncthreads();
-  for (int64_t r = begin + lane; r < end + lane; r += 64 * BATCH) {
-    int32_t key[BATCH];
-#pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-      const int64_t at = r + 64 * i;
-      key[i] = p.keys[min(at, static_cast<int64_t>(p.rows) - 1)];
-      key[i] = at < end ? key[i] : kNoKey;
-    }
-#pragma unroll 1
-    for (int i = 0; i < BATCH; ++i) {
-      const uint32_t d = static_cast<uint32_t>(key[0]) - static_cast<uint32_t>(lo);
-      uint64_t left = __ballot(d < static_cast<uint32_t>(n));
-      while (left) {  // the group's tokens one by one, each with all its rows
-        const int leader = __builtin_ctzll(left);
-        const uint32_t token = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(d), leader));
-        const uint64_t same = __ballot(d == token);
-        const int at = mine[token];
-        if (d == token) p.sorted[at + __popcll(same & ((uint64_t{1} << lane) - 1))] = static_cast<int32_t>(r + 64 * i);
-        if (lane == leader) mine[token] = at + __popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next look at the counter sees it
-        left &= ~same;
-      }
-#pragma unroll
-      for (int j = 0; j + 1 < BATCH; ++j) key[j] = key[j + 1];
-    }
+    for (int i = 0; i < BATCH; ++i) f(static_cast<int32_t>(r + 64 * i), key[i]);
   }
 }
 
-// The sum of rows list[0 .. n) of a tile's columns (list null: rows 0 .. n of float32 sums), shared out to the
-// wave's groups of lanes.  Every lane gets the sum of its columns, the same in every group.
-template <typename T, int VEC>
-__device__ __forceinline__ void sum_rows(const T* rows, int64_t stride, const int32_t* list, int n, int lanes, int c, float* sum) {
-  const int lane = static_cast<int>(threadIdx.x) & 63, group = lane / lanes, groups = 64 / lanes;
+__global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingGradParams p) {
+  __shared__ SortBoard s;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  const int lo = static_cast<int>(blockIdx.x) * p.per_block, n = min(p.per_block, p.src.V - lo);
+  for (int i = threadIdx.x; i < kSortWaves * kSortTokens; i += 64 * kSortWaves) (&s.place[0][0])[i] = 0;
+  __syncthreads();
+  const int64_t stretch = ((static_cast<int64_t>(p.rows) + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+  const int64_t begin = wave * stretch, end = min(begin + stretch, static_cast<int64_t>(p.rows));
+  int32_t* mine = s.place[wave];
+  const uint64_t before = (uint64_t{1} << lane) - 1;
+  int less = 0, kept = 0;
+  for_rows(p, begin, end, lane, [&](int32_t row, int32_t key) {
+    less += __popcll(__ballot(key < lo));
+    const uint32_t d = static_cast<uint32_t>(key) - static_cast<uint32_t>(lo);
+    const bool here = d < static_cast<uint32_t>(n);
+    const uint64_t votes = __ballot(here);
+    if (votes) {
+      if (here) {
+        atomicAdd(&mine[d], 1);
+        const int at = kept + __popcll(votes & before);
+        if (at < kSortFound) {
+          s.found[wave][at] = row;
+          s.token[wave][at] = static_cast<uint16_t>(d);
+        }
+      }
+      kept += __popcll(votes);
+    }
+  });
+  if (lane == 0) s.below[wave] = less;
+  __syncthreads();
+  // exclusive sums over (token, wave): a thread to a token
+  int base = 0;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
-  constexpr int BATCH = 8;
-  int i = group;
-  for (; i + (BATCH - 1) * groups < n; i += BATCH * groups) {
-    Pack<T, VEC> k[BATCH];
+  for (int w = 0; w < kSortWaves; ++w) base += s.below[w];
+  const int t = static_cast<int>(threadIdx.x);
+  int total = 0;
+  if (t < n) {
 #pragma unroll
-    for (int q = 0; q < BATCH; ++q) k[q].load(rows + (list ? list[i + q * groups] : i + q * groups) * stride + c);
+    for (int w = 0; w < kSortWaves; ++w) total += s.place[w][t];
+  }
+  int upto = total;  // inclusive over the wave
+  for (int off = 1; off < 64; off <<= 1) {
+    const int v = __shfl_up(upto, off);
+    if (lane >= off) upto += v;
+  }
+  if (lane == 63) s.sum[wave] = upto;
+  __syncthreads();
+  int at = base + upto - total;
+  for (int w = 0; w < wave; ++w) at += s.sum[w];
+  if (t < n) {
+    p.first[lo + t] = at;
+    if (lo + t == p.src.V - 1) p.first[p.src.V] = at + total;
 #pragma unroll
-    for (int q = 0; q < BATCH; ++q) {
-      float f[VEC];
-      k[q].get(f);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[j] += f[j];
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = s.place[w][t];
+      s.place[w][t] = at;
+      at += c;
     }
   }
-  for (; i < n; i += 2 * groups) {
-    Pack<T, VEC> k[2];
-    const int i1 = min(i + groups, n - 1);
-    k[0].load(rows + (list ? list[i] : i) * stride + c);
-    k[1].load(rows + (list ? list[i1] : i1) * stride + c);
-    float f[VEC];
-    k[0].get(f);
+  __syncthreads();
+  // 64 rows at a time, their tokens one by one, each with all its rows
+  const auto put = [&](int32_t row, uint32_t d) {
+    uint64_t left = __ballot(d < static_cast<uint32_t>(n));
+    while (left) {
+      const int leader = __builtin_ctzll(left);
+      const uint32_t token = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(d), leader));
+      const uint64_t same = __ballot(d == token);
+      const int to = mine[token];
+      if (d == token) p.sorted[to + __popcll(same & before)] = row;
+      if (lane == leader) mine[token] = to + __popcll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next look at the counter sees it
+      left &= ~same;
+    }
+  };
+  if (kept <= kSortFound) {
+    for (int i = 0; i < kept; i += 64) {
+      const int at_i = min(i + lane, kept - 1);
+      put(s.found[wave][at_i], i + lane < kept ? s.token[wave][at_i] : static_cast<uint32_t>(kNoKey));
+    }
+  } else {
+    for_rows(p, begin, end, lane, [&](int32_t row, int32_t key) { put(row, static_cast<uint32_t>(key) - static_cast<uint32_t>(lo)); });
+  }
+}
+
+// The sum of rows list[0 .. n) (list null: rows 0 .. n of float32 sums) in the columns of a lane, CH groups of VEC
+// that begin at c[], shared out to the wave's groups of lanes.  Every lane gets the sum of its columns.
+template <typename T, int VEC, int CH>
+__device__ __forceinline__ void sum_rows(const T* rows, int64_t stride, const int32_t* list, int n, int lanes, const int (&c)[CH],
+                                         float (&sum)[CH][VEC]) {
+  const int lane = static_cast<int>(threadIdx.x) & 63, group = lane / lanes, groups = 64 / lanes;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[j] += f[j];
-    k[1].get(f);
+  for (int q = 0; q < CH; ++q)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[j] += i + groups < n ? f[j] : 0.f;
+    for (int j = 0; j < VEC; ++j) sum[q][j] = 0.f;
+  constexpr int BATCH = 8;
+  // a row past the last one is the last one again, and not added
+  for (int i = 0; i < n; i += BATCH * groups) {
+    Pack<T, VEC> k[BATCH][CH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (i + b * groups < n) {  // the same for the whole wave
+        const int at = min(i + b * groups + group, n - 1);
+        const T* row = rows + (list ? list[at] : at) * stride;
+#pragma unroll
+        for (int q = 0; q < CH; ++q) k[b][q].load(row + c[q]);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (i + b * groups < n) {
+        const bool on = i + b * groups + group < n;
+#pragma unroll
+        for (int q = 0; q < CH; ++q) {
+          float f[VEC];
+          k[b][q].get(f);
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) sum[q][j] += on ? f[j] : 0.f;
+        }
+      }
+    }
   }
   for (int off = lanes; off < 64; off <<= 1) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[j] += __shfl_xor(sum[j], off);
+    for (int q = 0; q < CH; ++q)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[q][j] += __shfl_xor(sum[q][j], off);
   }
+}
+
+// The columns of a lane in a tile: CH groups, `lanes` groups apart.
+template <int VEC, int CH>
+__device__ __forceinline__ void columns_of(const EmbeddingGradParams& p, int tile, int (&c)[CH]) {
+  const int lane = static_cast<int>(threadIdx.x) & (p.lanes - 1);
+#pragma unroll
+  for (int q = 0; q < CH; ++q) c[q] = group_start((tile * CH + q) * p.lanes + lane, VEC, p.D);
 }
 
 // A wave to the first or the last token of a run of sorted rows (a token of more than kRun rows: at most
 // two of them meet a run), and a tile of columns.
-template <typename T, int VEC>
+template <typename T, int VEC, int CH>
 __global__ __launch_bounds__(256) void net_embedding_runs(EmbeddingGradParams p) {
   const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int tile = static_cast<int>(item % p.tiles), last = static_cast<int>(item / p.tiles) & 1;
   const int64_t run = item / p.tiles / 2;
   if (run >= p.runs) return;
-  const int lane = static_cast<int>(threadIdx.x) & 63;
   const int total = p.first[p.src.V];
   const int64_t begin64 = run * kRun;
   if (begin64 >= total) return;
   const int begin = static_cast<int>(begin64), end = min(begin + kRun, total);
-  const int32_t head = p.keys[p.sorted[begin]], token = last ? p.keys[p.sorted[end - 1]] : head;
-  if (last && token == head) return;
+  const int32_t head = p.keys[p.sorted[begin]], tail = p.keys[p.sorted[end - 1]], token = last ? tail : head;
+  if (last && tail == head) return;
   const int from = p.first[token], to = p.first[token + 1];
   if (to - from <= kRun) return;
   const int a = max(from, begin), n = min(to, end) - a;
-  const int c = group_start(tile * p.lanes + (lane & (p.lanes - 1)), VEC, p.D);
-  float sum[VEC];
-  sum_rows<T, VEC>(static_cast<const T*>(p.dout), p.D, p.sorted + a, n, p.lanes, c, sum);
-  if (lane < p.lanes) {
-    Pack<float, VEC> k;
-    k.set(sum);
-    k.store(p.sums + (run * 2 + last) * p.D + c);
+  int c[CH];
+  columns_of<VEC, CH>(p, tile, c);
+  float sum[CH][VEC];
+  sum_rows<T, VEC, CH>(static_cast<const T*>(p.dout), p.D, p.sorted + a, n, p.lanes, c, sum);
+  if ((static_cast<int>(threadIdx.x) & 63) < p.lanes) {
+#pragma unroll
+    for (int q = 0; q < CH; ++q) {
+      Pack<float, VEC> k;
+      k.set(sum[q]);
+      k.store(p.sums + (run * 2 + last) * p.D + c[q]);
+    }
   }
 }
 
 // A wave to a weight row and a tile of columns; behind them, a block to a run in which a common token begins.
-template <typename T, int VEC>
+template <typename T, int VEC, int CH>
 __global__ __launch_bounds__(256) void net_embedding_rows(EmbeddingGradParams p, int32_t row_blocks) {
-  __shared__ float parts[4][64 * VEC];
+  __shared__ float parts[4][CH * VEC * 64];
   const int wave = static_cast<int>(threadIdx.x) >> 6, lane = static_cast<int>(threadIdx.x) & 63;
-  float sum[VEC];
+  float sum[CH][VEC];
+  int c[CH];
   if (static_cast<int>(blockIdx.x) < row_blocks) {
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-    const int tile = static_cast<int>(item % p.tiles);
     const int64_t v = item / p.tiles;
     if (v >= p.src.V) return;
     const int from = p.first[v], n = p.first[v + 1] - from;
     if (n > kRun) return;
-    const int c = group_start(tile * p.lanes + (lane & (p.lanes - 1)), VEC, p.D);
-    sum_rows<T, VEC>(static_cast<const T*>(p.dout), p.D, p.sorted + from, n, p.lanes, c, sum);
+    columns_of<VEC, CH>(p, static_cast<int>(item % p.tiles), c);
+    sum_rows<T, VEC, CH>(static_cast<const T*>(p.dout), p.D, p.sorted + from, n, p.lanes, c, sum);
     if (lane < p.lanes) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[j] *= p.scale;
-      Pack<T, VEC> k;
-      k.set(sum);
-      k.store(static_cast<T*>(p.dweight) + v * p.D + c);
+      for (int q = 0; q < CH; ++q) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum[q][j] *= p.scale;
+        Pack<T, VEC> k;
+        k.set(sum[q]);
+        k.store(static_cast<T*>(p.dweight) + v * p.D + c[q]);
+      }
     }
     return;
   }
   const int64_t item = static_cast<int64_t>(blockIdx.x) - row_blocks, begin = item / p.tiles * kRun;
-  const int tile = static_cast<int>(item % p.tiles), total = p.first[p.src.V];
+  const int total = p.first[p.src.V];
   if (begin >= total) return;
   // the token that holds the run's last row, if it is common and begins in the run
   const int end = min(static_cast<int>(begin) + kRun, total);
@@ -296,31 +340,36 @@ __global__ __launch_bounds__(256) void net_embedding_rows(EmbeddingGradParams p,
   const int from = p.first[token], to = p.first[token + 1];
   if (to - from <= kRun || from < begin) return;
   // its sums: the last token of this run (the first one where it begins with the run), the first of the runs behind
-  const int c = group_start(tile * p.lanes + (lane & (p.lanes - 1)), VEC, p.D);
+  columns_of<VEC, CH>(p, static_cast<int>(item % p.tiles), c);
   const int64_t r0 = begin / kRun, r1 = (static_cast<int64_t>(to) - 1) / kRun;
   const float* sums = p.sums + r0 * 2 * p.D;
   // runs r0 + 1 .. r1 in four stretches
   const int more = static_cast<int>(r1 - r0), stretch = (more + 3) / 4;
   const int s0 = min(wave * stretch, more), s1 = min(s0 + stretch, more);
-  sum_rows<float, VEC>(sums + static_cast<int64_t>(1 + s0) * 2 * p.D, 2 * static_cast<int64_t>(p.D), nullptr, s1 - s0, p.lanes, c, sum);
+  sum_rows<float, VEC, CH>(sums + static_cast<int64_t>(1 + s0) * 2 * p.D, 2 * static_cast<int64_t>(p.D), nullptr, s1 - s0, p.lanes, c, sum);
   if (lane < p.lanes) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) parts[wave][j * 64 + lane] = sum[j];
+    for (int q = 0; q < CH; ++q)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) parts[wave][(q * VEC + j) * 64 + lane] = sum[q][j];
   }
   __syncthreads();
   if (wave == 0 && lane < p.lanes) {
-    Pack<float, VEC> first;
-    first.load(sums + (from == begin ? 0 : p.D) + c);
-    first.get(sum);
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
+    for (int q = 0; q < CH; ++q) {
+      Pack<float, VEC> first;
+      first.load(sums + (from == begin ? 0 : p.D) + c[q]);
+      first.get(sum[q]);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) sum[j] += parts[w][j * 64 + lane];
-      sum[j] *= p.scale;
+      for (int j = 0; j < VEC; ++j) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sum[q][j] += parts[w][(q * VEC + j) * 64 + lane];
+        sum[q][j] *= p.scale;
+      }
+      Pack<T, VEC> k;
+      k.set(sum[q]);
+      k.store(static_cast<T*>(p.dweight) + static_cast<int64_t>(token) * p.D + c[q]);
     }
-    Pack<T, VEC> k;
-    k.set(sum);
-    k.store(static_cast<T*>(p.dweight) + static_cast<int64_t>(token) * p.D + c);
   }
 }
 
@@ -388,7 +437,7 @@ rnnt_status_t rnnt_label_embedding(const int32_t* labels, const int32_t* lens, r
     const bool wide = shape.D >= VEC;
     p.groups = wide ? (shape.D + VEC - 1) / VEC : shape.D;
     p.lanes = lanes_for(p.groups, 256);
-    const int64_t per = 256 / p.lanes, blocks = (p.rows + per - 1) / per;
+    const int64_t per = 256 / p.lanes * kRowsAtOnce, blocks = (p.rows + per - 1) / per;
     const dim3 grid(static_cast<uint32_t>(blocks < kMaxRows / 256 ? blocks : kMaxRows / 256));
     if (wide) hipLaunchKernelGGL((net_embedding<T, VEC>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((net_embedding<T, 1>), grid, dim3(256), 0, stream, p);
@@ -429,34 +478,37 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   const int64_t shares = (static_cast<int64_t>(shape.V) + kSortBlocks - 1) / kSortBlocks;
   p.per_block = static_cast<int32_t>(shares < kSortTokens ? shares : kSortTokens);
   const dim3 sort_grid(static_cast<uint32_t>((static_cast<int64_t>(shape.V) + p.per_block - 1) / p.per_block));
-  const size_t counters = static_cast<size_t>(kSortWaves) * p.per_block * sizeof(int32_t);
   if (p.rows > 0) {
     const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(p.rows) + 255) / 256));
     hipLaunchKernelGGL(net_embedding_keys, grid, dim3(256), 0, stream, p);
     if (launched() != RNNT_OK) return RNNT_ERR_HIP;
   }
-  hipLaunchKernelGGL(net_embedding_sort, sort_grid, dim3(64 * kSortWaves), counters, stream, p);
+  hipLaunchKernelGGL(net_embedding_sort, sort_grid, dim3(64 * kSortWaves), 0, stream, p);
   if (launched() != RNNT_OK) return RNNT_ERR_HIP;
   return with_dtype(shape.dtype, [&](auto t) {
     using T = decltype(t);
-    const auto rest = [&](auto vec) {
-      constexpr int VEC = decltype(vec)::value;
+    const auto rest = [&](auto vec, auto chunks) {
+      constexpr int VEC = decltype(vec)::value, CH = decltype(chunks)::value;
       const int groups = (shape.D + VEC - 1) / VEC;
-      p.lanes = lanes_for(groups, 64);
-      p.tiles = (groups + p.lanes - 1) / p.lanes;
+      p.lanes = lanes_for((groups + CH - 1) / CH, 64);
+      p.tiles = (groups + p.lanes * CH - 1) / (p.lanes * CH);
       const int64_t run_items = static_cast<int64_t>(p.runs) * 2 * p.tiles, starts = static_cast<int64_t>(p.runs) * p.tiles;
       const int64_t row_blocks = (static_cast<int64_t>(shape.V) * p.tiles + 3) / 4;
       if ((run_items + 3) / 4 > kMaxRows / 256 || row_blocks + starts > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
       if (run_items > 0) {
-        hipLaunchKernelGGL((net_embedding_runs<T, VEC>), dim3(static_cast<uint32_t>((run_items + 3) / 4)), dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((net_embedding_runs<T, VEC, CH>), dim3(static_cast<uint32_t>((run_items + 3) / 4)), dim3(256), 0, stream, p);
         if (launched() != RNNT_OK) return RNNT_ERR_HIP;
       }
-      hipLaunchKernelGGL((net_embedding_rows<T, VEC>), dim3(static_cast<uint32_t>(row_blocks + starts)), dim3(256), 0, stream, p,
+      hipLaunchKernelGGL((net_embedding_rows<T, VEC, CH>), dim3(static_cast<uint32_t>(row_blocks + starts)), dim3(256), 0, stream, p,
                          static_cast<int32_t>(row_blocks));
       return launched();
     };
     constexpr int WIDE = 16 / sizeof(T);
-    return shape.D >= WIDE ? rest(std::integral_constant<int, WIDE>{}) : rest(std::integral_constant<int, 1>{});
+    const std::integral_constant<int, 1> one{};
+    const std::integral_constant<int, 2> two{};
+    const std::integral_constant<int, WIDE> wide{};
+    if (shape.D < WIDE) return rest(one, one);
+    return shape.D > 64 * WIDE ? rest(wide, two) : rest(wide, one);  // two groups to a lane where one is not the row
   });
 }
 

@@ -170,22 +170,26 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p
         q[v] = 1.f;
       }
       const bool whole = live >= kSteps;
+      const auto scan = [&](auto all) {
 #pragma unroll
-      for (int j = 0; j < kSteps; ++j) {
-        float xf[VEC], zf[VEC];
-        xs.r[j].get(xf);
-        zs.r[j].get(zf);
+        for (int j = 0; j < kSteps; ++j) {
+          float xf[VEC], zf[VEC];
+          xs.r[j].get(xf);
+          zs.r[j].get(zf);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          float a, g;
-          gate(zf[v], a, g);
-          const float next = __builtin_fmaf(g, xf[v] - s[v], s[v]);
-          s[v] = whole || j < live ? next : s[v];
-          q[v] = whole || j < live ? a * q[v] : q[v];
-          S[j][v] = s[v];
-          P[j][v] = q[v];
+          for (int v = 0; v < VEC; ++v) {
+            float a, g;
+            gate<T>(zf[v], a, g);
+            const float next = __builtin_fmaf(g, xf[v] - s[v], s[v]);
+            s[v] = all || j < live ? next : s[v];
+            q[v] = all || j < live ? a * q[v] : q[v];
+            S[j][v] = s[v];
+            P[j][v] = q[v];
+          }
         }
-      }
+      };
+      if (whole) scan(std::true_type{});
+      else scan(std::false_type{});
       // the next tile's rows, on their way during the rest
       xs.load(x, p.x_st, t + kTileSteps, at.len, c);
       zs.load(z, p.z_st, t + kTileSteps, at.len, c);
@@ -270,7 +274,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
           float a, g;
-          gate(zf[v], a, g);
+          gate<T>(zf[v], a, g);
           const float next = BACK ? a * (S[v] + xf[v]) : __builtin_fmaf(g, xf[v] - S[v], S[v]);
           S[v] = j < live ? next : S[v];
           A[v] = j < live ? a * A[v] : A[v];
@@ -357,7 +361,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_grad(RecurrencePar
         zs.r[j].get(zf);
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-          gate(zf[v], a[j][v], g[j][v]);
+          gate<T>(zf[v], a[j][v], g[j][v]);
           const float off = xf[v] - s[v];
           w[j][v] = -off * (a[j][v] * g[j][v]);
           s[v] = __builtin_fmaf(g[j][v], off, s[v]);
@@ -421,7 +425,7 @@ rnnt_status_t check(const rnnt_recurrence_shape_t& s) {
 
 int state_count(int L) { return static_cast<int>((static_cast<int64_t>(L) + kSteps - 1) / kSteps); }
 
-// Blocks to a sequence: one, or as many segments of at least two tiles as give the chip two blocks to a CU.
+// Blocks to a sequence: one, or as many segments of at least two tiles as give the chip a block to a CU.
 // Segments read x and z twice (5/3 of the bytes forward, 7/5 backward), which pays below about 3/5 of a chip.
 void segments_of(const rnnt_recurrence_shape_t& s, RecurrenceParams* p) {
   const int vec = s.dtype == RNNT_DTYPE_F32 || s.D < 2 ? 1 : 2;
@@ -430,7 +434,7 @@ void segments_of(const rnnt_recurrence_shape_t& s, RecurrenceParams* p) {
   p->segments = 1;
   p->seg_steps = s.L;
   if (blocks < 150 && steps >= 4) {
-    int64_t want = (512 + blocks - 1) / blocks;
+    int64_t want = 256 / blocks;
     if (want > steps / 2) want = steps / 2;
     const int64_t per = (steps + want - 1) / want;
     p->segments = static_cast<int32_t>((steps + per - 1) / per);
