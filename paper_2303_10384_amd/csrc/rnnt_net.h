@@ -51,7 +51,7 @@ struct Pack {
   }
   // a load of what is read once: it does not push lines out that are still to be written or read
   __device__ __forceinline__ void load_once(const T* p) {
-    static_assert(kBytes % 16 == 0, "vectors of 16 bytes");
+    if constexpr (kBytes % 16 != 0) return load(p);
     using loose = LooseVector<sizeof(T)>;
 #pragma unroll
     for (int i = 0; i < kBytes / 16; ++i) {

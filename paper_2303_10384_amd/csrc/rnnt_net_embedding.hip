@@ -75,29 +75,31 @@ __global__ __launch_bounds__(256) void net_embedding(EmbeddingParams p) {
 }
 
 // ---- the gradient ---------------------------------------------------------------
-// Four launches: the rows' tokens; the rows sorted by token (and by position within one); sums of the runs of
-// common tokens, kRun sorted rows at a time; every weight row from its rows or, if it has more than kRun, from
-// those sums.  A row of dout is read once, and every sum has one order.
+// Four launches: the rows' tokens; the rows sorted by token (and by position within one); the sums of kRun sorted
+// rows at a time, token by token; the tokens that lie in several runs, and the rows without a token.  A row of dout
+// is read once, and every sum has one order.
 
 constexpr int32_t kNoKey = 0x7fffffff;  // a row without a token, past every token
 constexpr int kSortWaves = 16;
 constexpr int kSortTokens = 384;   // most tokens of a sorting block (a thread to a token)
 constexpr int kSortFound = 384;    // rows that a wave keeps
 constexpr int kSortBlocks = 256;   // one to a CU, each looks at every row
-constexpr int kRun = 64;
+constexpr int kRun = 32;
+constexpr int kManyRuns = 32;  // a token of more runs is added up by four waves
 
 struct EmbeddingGradParams {
   TokenSource src;
   const void* dout;
   void* dweight;
   float scale;
-  int32_t D, rows, lanes, tiles;    // lanes: of a wave to a row of a tile, a power of two
+  int32_t D, rows, tiles;           // tiles: of 64 groups of columns
   int32_t per_block;                // tokens of a sorting block
   int32_t runs;                     // ceil(rows / kRun)
   int32_t* keys;                    // (rows)
   int32_t* sorted;                  // (rows) positions, by token
+  int32_t* tokens;                  // (rows) their tokens
   int32_t* first;                   // (V + 1) where a token's rows begin in `sorted`
-  float* sums;                      // (runs, 2, D): of the run's first token, of its last one
+  float* sums;                      // (runs, 2, D): of a token of the run before, of one of the next run too
 };
 
 __global__ __launch_bounds__(256) void net_embedding_keys(EmbeddingGradParams p) {
@@ -204,7 +206,11 @@ __global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingG
       const uint32_t token = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(d), leader));
       const uint64_t same = __ballot(d == token);
       const int to = mine[token];
-      if (d == token) p.sorted[to + __popcll(same & before)] = row;
+      if (d == token) {
+        const int at = to + __popcll(same & before);
+        p.sorted[at] = row;
+        p.tokens[at] = lo + static_cast<int32_t>(token);
+      }
       if (lane == leader) mine[token] = to + __popcll(same);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next look at the counter sees it
       left &= ~same;
@@ -220,156 +226,140 @@ __global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingG
   }
 }
 
-// The sum of rows list[0 .. n) (list null: rows 0 .. n of float32 sums) in the columns of a lane, CH groups of VEC
-// that begin at c[], shared out to the wave's groups of lanes.  Every lane gets the sum of its columns.
-template <typename T, int VEC, int CH>
-__device__ __forceinline__ void sum_rows(const T* rows, int64_t stride, const int32_t* list, int n, int lanes, const int (&c)[CH],
-                                         float (&sum)[CH][VEC]) {
-  const int lane = static_cast<int>(threadIdx.x) & 63, group = lane / lanes, groups = 64 / lanes;
-#pragma unroll
-  for (int q = 0; q < CH; ++q)
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) sum[q][j] = 0.f;
-  constexpr int BATCH = 8;
-  // a row past the last one is the last one again, and not added
-  for (int i = 0; i < n; i += BATCH * groups) {
-    Pack<T, VEC> k[BATCH][CH];
-#pragma unroll
-    for (int b = 0; b < BATCH; ++b) {
-      if (i + b * groups < n) {  // the same for the whole wave
-        const int at = min(i + b * groups + group, n - 1);
-        const T* row = rows + (list ? list[at] : at) * stride;
-#pragma unroll
-        for (int q = 0; q < CH; ++q) k[b][q].load(row + c[q]);
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < BATCH; ++b) {
-      if (i + b * groups < n) {
-        const bool on = i + b * groups + group < n;
-#pragma unroll
-        for (int q = 0; q < CH; ++q) {
-          float f[VEC];
-          k[b][q].get(f);
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) sum[q][j] += on ? f[j] : 0.f;
-        }
-      }
-    }
-  }
-  for (int off = lanes; off < 64; off <<= 1) {
-#pragma unroll
-    for (int q = 0; q < CH; ++q)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) sum[q][j] += __shfl_xor(sum[q][j], off);
-  }
-}
-
-// The columns of a lane in a tile: CH groups, `lanes` groups apart.
-template <int VEC, int CH>
-__device__ __forceinline__ void columns_of(const EmbeddingGradParams& p, int tile, int (&c)[CH]) {
-  const int lane = static_cast<int>(threadIdx.x) & (p.lanes - 1);
-#pragma unroll
-  for (int q = 0; q < CH; ++q) c[q] = group_start((tile * CH + q) * p.lanes + lane, VEC, p.D);
-}
-
-// A wave to the first or the last token of a run of sorted rows (a token of more than kRun rows: at most
-// two of them meet a run), and a tile of columns.
-template <typename T, int VEC, int CH>
+// A wave to a run of kRun sorted rows and a tile of 64 groups of columns: the same work whatever the tokens are, its rows
+// loaded eight at a time.  A token whose rows all lie in the run is finished here; the sums of one that comes from
+// the run before go to the run's first slot, of one that only goes on in the next run to its second.
+template <typename T, int VEC>
 __global__ __launch_bounds__(256) void net_embedding_runs(EmbeddingGradParams p) {
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int tile = static_cast<int>(item % p.tiles), last = static_cast<int>(item / p.tiles) & 1;
-  const int64_t run = item / p.tiles / 2;
-  if (run >= p.runs) return;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int64_t run = item / p.tiles, begin64 = run * kRun;
   const int total = p.first[p.src.V];
-  const int64_t begin64 = run * kRun;
   if (begin64 >= total) return;
-  const int begin = static_cast<int>(begin64), end = min(begin + kRun, total);
-  const int32_t head = p.keys[p.sorted[begin]], tail = p.keys[p.sorted[end - 1]], token = last ? tail : head;
-  if (last && tail == head) return;
-  const int from = p.first[token], to = p.first[token + 1];
-  if (to - from <= kRun) return;
-  const int a = max(from, begin), n = min(to, end) - a;
-  int c[CH];
-  columns_of<VEC, CH>(p, tile, c);
-  float sum[CH][VEC];
-  sum_rows<T, VEC, CH>(static_cast<const T*>(p.dout), p.D, p.sorted + a, n, p.lanes, c, sum);
-  if ((static_cast<int>(threadIdx.x) & 63) < p.lanes) {
+  const int begin = static_cast<int>(begin64), n = min(kRun, total - begin), lane = static_cast<int>(threadIdx.x) & 63;
+  const int c = group_start(static_cast<int>(item - run * p.tiles) * 64 + lane, VEC, p.D);
+  // lane i: row and token i of the run; lanes kRun and kRun + 1: the tokens around it
+  const int at = lane < kRun ? begin + min(lane, n - 1) : lane == kRun ? max(begin - 1, 0) : min(begin + n, total - 1);
+  const int my_row = p.sorted[at], my_token = p.tokens[at];
+  const auto token_of = [&](int i) { return __builtin_amdgcn_readlane(my_token, i); };
+  const bool from_before = begin > 0 && token_of(kRun) == token_of(0);
+  const bool goes_on = begin + n < total && token_of(kRun + 1) == token_of(n - 1);
+  float sum[VEC];
 #pragma unroll
-    for (int q = 0; q < CH; ++q) {
+  for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+  int32_t token = token_of(0);
+  bool first = true;
+  const auto flush = [&](bool at_end) {
+    if ((first && from_before) || (at_end && goes_on)) {
       Pack<float, VEC> k;
-      k.set(sum[q]);
-      k.store(p.sums + (run * 2 + last) * p.D + c[q]);
+      k.set(sum);
+      k.store(p.sums + (run * 2 + (first && from_before ? 0 : 1)) * p.D + c);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[j] *= p.scale;
+      Pack<T, VEC> k;
+      k.set(sum);
+      k.store(static_cast<T*>(p.dweight) + static_cast<int64_t>(token) * p.D + c);
     }
+  };
+  constexpr int BATCH = 8;
+  for (int i = 0; i < n; i += BATCH) {
+    Pack<T, VEC> k[BATCH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b)  // past the run's end its last row again
+      k[b].load_once(static_cast<const T*>(p.dout) + static_cast<int64_t>(__builtin_amdgcn_readlane(my_row, min(i + b, n - 1))) * p.D + c);
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (i + b < n) {
+        const int32_t t = token_of(i + b);
+        if (t != token) {
+          flush(false);
+          first = false;
+          token = t;
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+        }
+        float f[VEC];
+        k[b].get(f);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum[j] += f[j];
+      }
+    }
+  }
+  flush(true);
+}
+
+// The sums of a token in runs r0 .. r1 (r0's second slot, the others' first), from run r0 + 1 + s0 to s1.
+template <int VEC>
+__device__ __forceinline__ void add_runs(const EmbeddingGradParams& p, int64_t r0, int s0, int s1, int c, float* sum) {
+  const float* sums = p.sums + (r0 + 1) * 2 * p.D + c;
+#pragma unroll 4
+  for (int i = s0; i < s1; ++i) {
+    Pack<float, VEC> k;
+    float f[VEC];
+    k.load(sums + static_cast<int64_t>(i) * 2 * p.D);
+    k.get(f);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] += f[j];
   }
 }
 
-// A wave to a weight row and a tile of columns; behind them, a block to a run in which a common token begins.
-template <typename T, int VEC, int CH>
+// What the runs left: a wave to a weight row and a tile, for the rows that no token has and the tokens of several
+// runs; behind them a block to every run in which a token of more than kManyRuns begins.
+template <typename T, int VEC>
 __global__ __launch_bounds__(256) void net_embedding_rows(EmbeddingGradParams p, int32_t row_blocks) {
-  __shared__ float parts[4][CH * VEC * 64];
-  const int wave = static_cast<int>(threadIdx.x) >> 6, lane = static_cast<int>(threadIdx.x) & 63;
-  float sum[CH][VEC];
-  int c[CH];
+  __shared__ float parts[4][VEC * 64];
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
+  float sum[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+  const auto begin_sums = [&](int64_t r0, int c) {
+    Pack<float, VEC> k;
+    k.load(p.sums + (r0 * 2 + 1) * p.D + c);
+    k.get(sum);
+  };
+  const auto finish = [&](int64_t v, int c) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] *= p.scale;
+    Pack<T, VEC> k;
+    k.set(sum);
+    k.store(static_cast<T*>(p.dweight) + v * p.D + c);
+  };
   if (static_cast<int>(blockIdx.x) < row_blocks) {
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + wave;
     const int64_t v = item / p.tiles;
     if (v >= p.src.V) return;
-    const int from = p.first[v], n = p.first[v + 1] - from;
-    if (n > kRun) return;
-    columns_of<VEC, CH>(p, static_cast<int>(item % p.tiles), c);
-    sum_rows<T, VEC, CH>(static_cast<const T*>(p.dout), p.D, p.sorted + from, n, p.lanes, c, sum);
-    if (lane < p.lanes) {
-#pragma unroll
-      for (int q = 0; q < CH; ++q) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) sum[q][j] *= p.scale;
-        Pack<T, VEC> k;
-        k.set(sum[q]);
-        k.store(static_cast<T*>(p.dweight) + v * p.D + c[q]);
-      }
+    const int from = p.first[v], to = p.first[v + 1], c = group_start(static_cast<int>(item - v * p.tiles) * 64 + lane, VEC, p.D);
+    if (from < to) {
+      const int r0 = from / kRun, more = (to - 1) / kRun - r0;
+      if (more == 0 || more > kManyRuns) return;
+      begin_sums(r0, c);
+      add_runs<VEC>(p, r0, 0, more, c, sum);
     }
+    finish(v, c);
     return;
   }
-  const int64_t item = static_cast<int64_t>(blockIdx.x) - row_blocks, begin = item / p.tiles * kRun;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) - row_blocks, r0 = item / p.tiles;
   const int total = p.first[p.src.V];
-  if (begin >= total) return;
-  // the token that holds the run's last row, if it is common and begins in the run
-  const int end = min(static_cast<int>(begin) + kRun, total);
-  const int32_t token = p.keys[p.sorted[end - 1]];
-  const int from = p.first[token], to = p.first[token + 1];
-  if (to - from <= kRun || from < begin) return;
-  // its sums: the last token of this run (the first one where it begins with the run), the first of the runs behind
-  columns_of<VEC, CH>(p, static_cast<int>(item % p.tiles), c);
-  const int64_t r0 = begin / kRun, r1 = (static_cast<int64_t>(to) - 1) / kRun;
-  const float* sums = p.sums + r0 * 2 * p.D;
-  // runs r0 + 1 .. r1 in four stretches
-  const int more = static_cast<int>(r1 - r0), stretch = (more + 3) / 4;
-  const int s0 = min(wave * stretch, more), s1 = min(s0 + stretch, more);
-  sum_rows<float, VEC, CH>(sums + static_cast<int64_t>(1 + s0) * 2 * p.D, 2 * static_cast<int64_t>(p.D), nullptr, s1 - s0, p.lanes, c, sum);
-  if (lane < p.lanes) {
+  const int64_t begin = r0 * kRun;
+  if (begin + kRun >= total) return;
+  const int32_t token = p.tokens[begin + kRun - 1];
+  const int from = p.first[token], more = static_cast<int>((p.first[token + 1] - 1) / kRun - r0);
+  if (from < begin || more <= kManyRuns) return;
+  const int c = group_start(static_cast<int>(item - r0 * p.tiles) * 64 + lane, VEC, p.D);
+  const int stretch = (more + 3) / 4, s0 = min(wave * stretch, more), s1 = min(s0 + stretch, more);
+  if (wave == 0) begin_sums(r0, c);
+  add_runs<VEC>(p, r0, s0, s1, c, sum);
 #pragma unroll
-    for (int q = 0; q < CH; ++q)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) parts[wave][(q * VEC + j) * 64 + lane] = sum[q][j];
-  }
+  for (int j = 0; j < VEC; ++j) parts[wave][j * 64 + lane] = sum[j];
   __syncthreads();
-  if (wave == 0 && lane < p.lanes) {
+  if (wave == 0) {
 #pragma unroll
-    for (int q = 0; q < CH; ++q) {
-      Pack<float, VEC> first;
-      first.load(sums + (from == begin ? 0 : p.D) + c[q]);
-      first.get(sum[q]);
+    for (int j = 0; j < VEC; ++j) {
+      sum[j] = 0.f;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) sum[q][j] += parts[w][(q * VEC + j) * 64 + lane];
-        sum[q][j] *= p.scale;
-      }
-      Pack<T, VEC> k;
-      k.set(sum[q]);
-      k.store(static_cast<T*>(p.dweight) + static_cast<int64_t>(token) * p.D + c[q]);
+      for (int w = 0; w < 4; ++w) sum[j] += parts[w][j * 64 + lane];
     }
+    finish(token, c);
   }
 }
 
@@ -383,15 +373,15 @@ rnnt_status_t check(const int32_t* labels, const rnnt_embedding_shape_t& s, Toke
   return RNNT_OK;
 }
 
-int lanes_for(int groups, int most) {
+int lanes_for(int groups) {
   int n = 1;
-  while (n < most && n < groups) n *= 2;
+  while (n < 256 && n < groups) n *= 2;
   return n;
 }
 
 // Workspace of the gradient, 256-byte aligned pieces.
 struct GradLayout {
-  size_t keys, sorted, first, sums, total;
+  size_t keys, sorted, tokens, first, sums, total;
 };
 
 GradLayout grad_layout(const rnnt_embedding_shape_t& s, int64_t rows) {
@@ -401,6 +391,8 @@ GradLayout grad_layout(const rnnt_embedding_shape_t& s, int64_t rows) {
   L.keys = o;
   o = net_align256(o + static_cast<size_t>(rows) * sizeof(int32_t));
   L.sorted = o;
+  o = net_align256(o + static_cast<size_t>(rows) * sizeof(int32_t));
+  L.tokens = o;
   o = net_align256(o + static_cast<size_t>(rows) * sizeof(int32_t));
   L.first = o;
   o = net_align256(o + (static_cast<size_t>(s.V) + 1) * sizeof(int32_t));
@@ -436,7 +428,7 @@ rnnt_status_t rnnt_label_embedding(const int32_t* labels, const int32_t* lens, r
     constexpr int VEC = 16 / sizeof(T);
     const bool wide = shape.D >= VEC;
     p.groups = wide ? (shape.D + VEC - 1) / VEC : shape.D;
-    p.lanes = lanes_for(p.groups, 256);
+    p.lanes = lanes_for(p.groups);
     const int64_t per = 256 / p.lanes * kRowsAtOnce, blocks = (p.rows + per - 1) / per;
     const dim3 grid(static_cast<uint32_t>(blocks < kMaxRows / 256 ? blocks : kMaxRows / 256));
     if (wide) hipLaunchKernelGGL((net_embedding<T, VEC>), grid, dim3(256), 0, stream, p);
@@ -472,6 +464,7 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   p.D = shape.D;
   p.keys = reinterpret_cast<int32_t*>(ws.ptr + L.keys);
   p.sorted = reinterpret_cast<int32_t*>(ws.ptr + L.sorted);
+  p.tokens = reinterpret_cast<int32_t*>(ws.ptr + L.tokens);
   p.first = reinterpret_cast<int32_t*>(ws.ptr + L.first);
   p.sums = reinterpret_cast<float*>(ws.ptr + L.sums);
   p.runs = static_cast<int32_t>((static_cast<int64_t>(p.rows) + kRun - 1) / kRun);
@@ -487,28 +480,23 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   if (launched() != RNNT_OK) return RNNT_ERR_HIP;
   return with_dtype(shape.dtype, [&](auto t) {
     using T = decltype(t);
-    const auto rest = [&](auto vec, auto chunks) {
-      constexpr int VEC = decltype(vec)::value, CH = decltype(chunks)::value;
+    const auto rest = [&](auto vec) {
+      constexpr int VEC = decltype(vec)::value;
       const int groups = (shape.D + VEC - 1) / VEC;
-      p.lanes = lanes_for((groups + CH - 1) / CH, 64);
-      p.tiles = (groups + p.lanes * CH - 1) / (p.lanes * CH);
-      const int64_t run_items = static_cast<int64_t>(p.runs) * 2 * p.tiles, starts = static_cast<int64_t>(p.runs) * p.tiles;
+      p.tiles = (groups + 63) / 64;
+      const int64_t run_items = static_cast<int64_t>(p.runs) * p.tiles;
       const int64_t row_blocks = (static_cast<int64_t>(shape.V) * p.tiles + 3) / 4;
-      if ((run_items + 3) / 4 > kMaxRows / 256 || row_blocks + starts > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
+      if (row_blocks + run_items > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
       if (run_items > 0) {
-        hipLaunchKernelGGL((net_embedding_runs<T, VEC, CH>), dim3(static_cast<uint32_t>((run_items + 3) / 4)), dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((net_embedding_runs<T, VEC>), dim3(static_cast<uint32_t>((run_items + 3) / 4)), dim3(256), 0, stream, p);
         if (launched() != RNNT_OK) return RNNT_ERR_HIP;
       }
-      hipLaunchKernelGGL((net_embedding_rows<T, VEC, CH>), dim3(static_cast<uint32_t>(row_blocks + starts)), dim3(256), 0, stream, p,
+      hipLaunchKernelGGL((net_embedding_rows<T, VEC>), dim3(static_cast<uint32_t>(row_blocks + run_items)), dim3(256), 0, stream, p,
                          static_cast<int32_t>(row_blocks));
       return launched();
     };
     constexpr int WIDE = 16 / sizeof(T);
-    const std::integral_constant<int, 1> one{};
-    const std::integral_constant<int, 2> two{};
-    const std::integral_constant<int, WIDE> wide{};
-    if (shape.D < WIDE) return rest(one, one);
-    return shape.D > 64 * WIDE ? rest(wide, two) : rest(wide, one);  // two groups to a lane where one is not the row
+    return shape.D >= WIDE ? rest(std::integral_constant<int, WIDE>{}) : rest(std::integral_constant<int, 1>{});
   });
 }
 
