@@ -38,6 +38,7 @@ struct EmbeddingParams {
   const void* weight;
   void* out;
   float scale;
+  bool away;  // store past the caches
   int32_t D, rows, lanes, groups;  // lanes: threads to a row, a power of two; groups: of VEC elements in a row
 };
 
@@ -68,7 +69,9 @@ __global__ __launch_bounds__(256) void net_embedding(EmbeddingParams p) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) f[j] = v[i] >= 0 ? f[j] * p.scale : v[i] == kBadRow ? __builtin_nanf("") : 0.f;
         k[i].set(f);
-        k[i].store(static_cast<T*>(p.out) + static_cast<int64_t>(row[i]) * p.D + c);
+        T* o = static_cast<T*>(p.out) + static_cast<int64_t>(row[i]) * p.D + c;
+        if (p.away) k[i].store_away(o);
+        else k[i].store(o);
       }
     }
   }
@@ -421,6 +424,7 @@ rnnt_status_t rnnt_label_embedding(const int32_t* labels, const int32_t* lens, r
   if (!multiple_of(e, weight) || !multiple_of(e, out)) return RNNT_ERR_ALIGNMENT;
   p.weight = weight;
   p.out = out;
+  p.away = static_cast<int64_t>(p.rows) * shape.D * e >= kStoreAway;
   p.scale = scale;
   p.D = shape.D;
   return with_dtype(shape.dtype, [&](auto t) {

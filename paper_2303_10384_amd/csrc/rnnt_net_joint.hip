@@ -60,12 +60,12 @@ struct JointParams {
   void* h;
   DropParams drop;
   int64_t* rng_out;
-  int32_t B, T, U1, H, t_blocks;
+  int32_t B, T, U1, H, t_blocks, block_frames;
 };
 
-constexpr int kJointFrames = 4;    // frames of a block of net_joint: pred is read once for all of them
+constexpr int kJointFrames = 4;    // frames of a block (net_joint reads pred once for all of them)
 constexpr int kJointRun = 8;       // groups of eight elements to a thread and frame
-constexpr int kJointLdsH = 4096;   // widest row that net_joint_odd keeps in LDS
+constexpr int kJointLdsBytes = 64000;  // rows that net_joint_odd keeps in LDS
 
 template <typename T, int ACT>
 __device__ __forceinline__ void joint_group(const float* e, const float* q, float scale, const Dropped& drop, Pack<T, 8>& out) {
@@ -97,13 +97,13 @@ __device__ __forceinline__ Pack<T, 8> nan_group() {
 template <typename T, int ACT>
 __global__ __launch_bounds__(256) void net_joint(JointParams p) {
   copy_rng(p.drop.rng, p.rng_out);
-  const int b = static_cast<int>(blockIdx.x) / p.t_blocks, t0 = static_cast<int>(blockIdx.x) % p.t_blocks * kJointFrames;
+  const int b = static_cast<int>(blockIdx.x) / p.t_blocks, t0 = static_cast<int>(blockIdx.x) % p.t_blocks * p.block_frames;
   const int64_t total = static_cast<int64_t>(p.U1) * p.H;
   int64_t j = (static_cast<int64_t>(blockIdx.y) * kJointRun * 256 + threadIdx.x) * 8;
   int col = static_cast<int>(j % p.H);
   const int col_step = 2048 % p.H;
   const int64_t valid0 = joint_valid(p, b, t0);
-  const int frames = min(kJointFrames, p.T - t0);
+  const int frames = min(p.block_frames, p.T - t0);
   const int tl = valid0 < 0 ? 0 : p.logit_lens[b];
   const int64_t valid = valid0 < 0 ? 0 : static_cast<int64_t>(p.label_lens[b] + 1) * p.H;
   Rng rng{};
@@ -142,81 +142,93 @@ __global__ __launch_bounds__(256) void net_joint(JointParams p) {
   }
 }
 
-// Any H: one frame to a block; groups are multiples of eight in h, where the random numbers are, so a
-// group may begin in one row of the run and end in the next (the frame's row, continued by its first
-// eight elements, is in LDS while it fits), and the run's first and last group may be partial.
+// Any H: groups are multiples of eight in h, where the random numbers are, so a group may begin in one row of
+// the run and end in the next (the frame's row, continued by its first eight elements, is in LDS while it fits),
+// and the run's first and last group may be partial.
+__device__ __forceinline__ int lds_at(int c) { return c + (c >> 3); }  // lanes read eight apart: nine words, no two in a bank
+
 template <typename T, int ACT, bool IN_LDS>
 __global__ __launch_bounds__(256) void net_joint_odd(JointParams p) {
   copy_rng(p.drop.rng, p.rng_out);
-  __shared__ float row[IN_LDS ? kJointLdsH + 8 : 1];
-  const int b = static_cast<int>(blockIdx.x) / p.T, t = static_cast<int>(blockIdx.x) % p.T;
-  const int64_t total = static_cast<int64_t>(p.U1) * p.H, run0 = static_cast<int64_t>(blockIdx.x) * total;
-  const int64_t valid = joint_valid(p, b, t);
-  const T* enc = static_cast<const T*>(p.enc) + static_cast<int64_t>(blockIdx.x) * p.H;
+  extern __shared__ float rows[];  // [block_frames][lds_at(H + 8)]
+  const int b = static_cast<int>(blockIdx.x) / p.t_blocks, t0 = static_cast<int>(blockIdx.x) % p.t_blocks * p.block_frames;
+  const int64_t total = static_cast<int64_t>(p.U1) * p.H;
+  const int frames = min(p.block_frames, p.T - t0), pitch = lds_at(p.H + 8);
   const T* pred = static_cast<const T*>(p.pred) + b * total;
-  T* h = static_cast<T*>(p.h) + run0;
   Rng rng{};
   if (p.drop.threshold) rng = load_rng(p.drop.rng);
-  if (IN_LDS && valid > 0) {
-    for (int c = threadIdx.x; c < p.H + 8; c += 256) row[c] = ElemTraits<T>::load1(enc + c % p.H);
+  if (IN_LDS) {
+    const T* enc = static_cast<const T*>(p.enc) + (static_cast<int64_t>(b) * p.T + t0) * p.H;
+    for (int i = 0; i < frames; ++i)
+      for (int c = threadIdx.x; c < p.H + 8; c += 256)
+        rows[i * pitch + lds_at(c)] = ElemTraits<T>::load1(enc + static_cast<int64_t>(i) * p.H + (c < p.H ? c : c % p.H));
     __syncthreads();
   }
-  int64_t j = (static_cast<int64_t>(blockIdx.y) * kJointRun * 256 + threadIdx.x) * 8 - (run0 & 7);
-  int col = static_cast<int>((j + p.H * static_cast<int64_t>(8)) % p.H);  // j > -8
+  const int64_t j_block = static_cast<int64_t>(blockIdx.y) * kJointRun * 2048;
+  const uint32_t col_block = static_cast<uint32_t>(j_block % p.H) + threadIdx.x * 8 + 8 * static_cast<uint32_t>(p.H);
   const int col_step = 2048 % p.H;
-  for (int it = 0; it < kJointRun && j < total; ++it, j += 2048) {
-    Pack<T, 8> k;
-    if (valid < 0) {
-      k = nan_group<T>();
-    } else if (j >= valid) {
-      k.zero();
-    } else {
-      float e[8], q[8];
-      const int first = j < 0 ? static_cast<int>(-j) : 0;
-      if (first == 0 && j + 8 <= total) k.load(pred + j);
-      else k.zero();
-      k.get(q);
-      if (first > 0 || j + 8 > total) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i >= first && j + i < total) q[i] = ElemTraits<T>::load1(pred + j + i);
-      }
-      if (IN_LDS) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = row[col + i];
-      } else if (col + 8 <= p.H) {
-        k.load(enc + col);
-        k.get(e);
+  for (int i = 0; i < frames; ++i) {
+    const int64_t frame = static_cast<int64_t>(b) * p.T + t0 + i, run0 = frame * total;
+    const int64_t valid = joint_valid(p, b, t0 + i);
+    const T* enc = static_cast<const T*>(p.enc) + frame * p.H;
+    T* h = static_cast<T*>(p.h) + run0;
+    const int shift = static_cast<int>(run0 & 7);
+    int64_t j = j_block + static_cast<int>(threadIdx.x) * 8 - shift;  // > -8
+    int col = static_cast<int>((col_block - static_cast<uint32_t>(shift)) % static_cast<uint32_t>(p.H));
+    for (int it = 0; it < kJointRun && j < total; ++it, j += 2048) {
+      Pack<T, 8> k;
+      if (j < 0 || j + 8 > total) {  // the run's first or last group, one element after the other
+        Dropped drop;
+        dropped_of(p.drop, rng, static_cast<uint64_t>(run0 + j) >> 3, drop);
+        const uint32_t dropped = drop.bits();
+        int cj = col;
+#pragma unroll 1
+        for (int q = 0; q < 8; ++q) {
+          if (j + q >= 0 && j + q < total) {
+            float v = valid < 0 ? __builtin_nanf("") : 0.f;
+            if (j + q < valid && !(dropped >> q & 1u))
+              v = Activation<ACT>::value(ElemTraits<T>::load1(enc + cj) + ElemTraits<T>::load1(pred + j + q)) * p.drop.scale;
+            ElemTraits<T>::store1(h + j + q, v);
+          }
+          if (++cj == p.H) cj = 0;
+        }
       } else {
+        if (valid < 0) {
+          k = nan_group<T>();
+        } else if (j >= valid) {
+          k.zero();
+        } else {
+          float e[8], q[8];
+          k.load(pred + j);
+          k.get(q);
+          if (IN_LDS) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = ElemTraits<T>::load1(enc + (col + i) % p.H);
-      }
-      Dropped drop;
-      dropped_of(p.drop, rng, static_cast<uint64_t>(run0 + j) >> 3, drop);
-      joint_group<T, ACT>(e, q, p.drop.scale, drop, k);
-      if (j + 8 > valid) {  // the valid rows end inside the group
+            for (int q8 = 0; q8 < 8; ++q8) e[q8] = rows[i * pitch + lds_at(col + q8)];
+          } else if (col + 8 <= p.H) {
+            k.load(enc + col);
+            k.get(e);
+          } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (j + i >= valid) {
-            if constexpr (sizeof(T) == 4) k.w[i] = 0;
-            else k.w[i / 2] &= (i & 1) ? 0x0000ffffu : 0xffff0000u;
+            for (int q8 = 0; q8 < 8; ++q8) e[q8] = ElemTraits<T>::load1(enc + (col + q8) % p.H);
+          }
+          Dropped drop;
+          dropped_of(p.drop, rng, static_cast<uint64_t>(run0 + j) >> 3, drop);
+          joint_group<T, ACT>(e, q, p.drop.scale, drop, k);
+          if (j + 8 > valid) {  // the valid rows end inside the group
+#pragma unroll
+            for (int q8 = 0; q8 < 8; ++q8) {
+              if (j + q8 >= valid) {
+                if constexpr (sizeof(T) == 4) k.w[q8] = 0;
+                else k.w[q8 / 2] &= (q8 & 1) ? 0x0000ffffu : 0xffff0000u;
+              }
+            }
           }
         }
+        k.store(h + j);
       }
+      col += col_step;
+      if (col >= p.H) col -= p.H;
     }
-    if (j >= 0 && j + 8 <= total) {
-      k.store(h + j);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (j + i >= 0 && j + i < total) {
-          if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(h + j + i) = k.w[i];
-          else *reinterpret_cast<uint16_t*>(h + j + i) = static_cast<uint16_t>(k.w[i / 2] >> (16 * (i & 1)));
-        }
-      }
-    }
-    col += col_step;
-    if (col >= p.H) col -= p.H;
   }
 }
 
@@ -234,13 +246,10 @@ struct JointGradParams {
   DropParams drop;
   float factor;  // of both sums: the dropout's scale, and 4 for tanh (its slope is 4u / (1 + u)^2)
   int32_t B, T, U1, H, t_blocks, slices, lanes;  // lanes: of a row, eight channels each (4, 8 or 16)
+  int32_t tile_frames;                           // frames of a block
 };
 
 constexpr int kGradWaves = 4;
-constexpr int wave_frames(int elem_bytes) { return elem_bytes == 4 ? 4 : 8; }
-constexpr int tile_frames(int elem_bytes) { return kGradWaves * wave_frames(elem_bytes); }  // of a block
-template <typename T>
-constexpr int kWaveT = wave_frames(sizeof(T));
 
 // Whether enc + pred > 0 for two 16-bit elements at a time, without the sums: the sum of two floats is
 // positive exactly when enc > -pred, and the bits of a float, its lower 15 flipped where the sign is set, are
@@ -344,17 +353,19 @@ __device__ __forceinline__ int longest_first(const int32_t* label_lens, int B, i
 // EIGHTS: rows are multiples of eight elements, so that a group's numbers are one block.  H is at least 8 here: the
 // last group of a row that is no multiple begins at H - 8, its first channels also the group's before it, which
 // computes and writes the same values.
-template <typename T, int ACT, bool EIGHTS, bool DROP>
+template <typename T, int ACT, bool EIGHTS, bool DROP, int FRAMES>
 __global__ __launch_bounds__(64 * kGradWaves) void net_joint_grad(JointGradParams p) {
   constexpr bool KEYS = ACT == RNNT_ACT_RELU && sizeof(T) == 2;
-  constexpr int WAVES = kGradWaves, FRAMES = kWaveT<T>;
+  constexpr int WAVES = kGradWaves;
   static_assert(WAVES == 4, "256 threads store a step's 512 sums");
   __shared__ __attribute__((aligned(16))) float sums[2][WAVES][512];
   const int slice = static_cast<int>(blockIdx.x) % p.slices, bt = static_cast<int>(blockIdx.x) / p.slices;
   const int tb = bt % p.t_blocks, b = longest_first(p.label_lens, p.B, bt / p.t_blocks);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
   const int sub = lane / p.lanes, rows = 64 / p.lanes;
-  const int c0 = slice * p.lanes * 8, c = min(c0 + (lane & (p.lanes - 1)) * 8, p.H - 8);
+  // groups of a slice: one fewer than the lanes where random numbers straddle groups (the blocks are one more)
+  const int wide = EIGHTS || !DROP ? p.lanes : p.lanes - 1;
+  const int c0 = slice * wide * 8, c = min(c0 + min(lane & (p.lanes - 1), wide - 1) * 8, p.H - 8);
   int tl = p.logit_lens[b];
   const int ul = p.label_lens[b];
   if (tl < 0 || tl > p.T || ul < 0 || ul >= p.U1) tl = 0;
@@ -397,7 +408,7 @@ __global__ __launch_bounds__(64 * kGradWaves) void net_joint_grad(JointGradParam
         make_buffer(p.part + (static_cast<int64_t>(b) * p.t_blocks + tb) * run, run * static_cast<int64_t>(sizeof(float)));
     const int from = static_cast<int>(threadIdx.x) >> 2, pair = static_cast<int>(threadIdx.x) & 3;
     const int sums_at = ((pair >> 1) * 64 + from) * 2 + (pair & 1);  // in float2
-    const int put_u = from / p.lanes, put_c = min(c0 + (from & (p.lanes - 1)) * 8, p.H - 8) + pair * 2;
+    const int put_u = from / p.lanes, put_c = min(c0 + min(from & (p.lanes - 1), wide - 1) * 8, p.H - 8) + pair * 2;
 
     auto step = [&](GradRows<T, FRAMES>& now, GradRows<T, FRAMES>& next, int u0, float (*lds)[512]) {
       const int u = u0 + sub;
@@ -418,14 +429,17 @@ __global__ __launch_bounds__(64 * kGradWaves) void net_joint_grad(JointGradParam
 #pragma unroll
       for (int i = 0; i < FRAMES; ++i) {
         Dropped signs;
-        if constexpr (DROP) {
-          const uint64_t n = number[i] + at;
-          signs.signs_below(random_block(rng, n >> 3), p.drop.threshold);
-          if constexpr (!EIGHTS) {
-            Dropped after;
-            after.signs_below(random_block(rng, (n >> 3) + 1), p.drop.threshold);
-            signs.shift(after, static_cast<int>(n & 7));
-          }
+        if constexpr (DROP && EIGHTS) {
+          signs.signs_below(random_block(rng, (number[i] + at) >> 3), p.drop.threshold);
+        } else if constexpr (DROP) {
+          // the row's lanes form the blocks that its slice meets, one each; an element's may be two of them
+          const uint64_t n = number[i] + at, n_row = number[i] + static_cast<uint32_t>(u * p.H + c0);
+          signs.signs_below(random_block(rng, (n_row >> 3) + (lane & (p.lanes - 1))), p.drop.threshold);
+          const uint32_t bits = signs.bits();
+          const int from_lane = (lane & ~(p.lanes - 1)) + static_cast<int>((n >> 3) - (n_row >> 3));
+          const uint32_t here = static_cast<uint32_t>(__shfl(static_cast<int>(bits), from_lane));
+          const uint32_t next = static_cast<uint32_t>(__shfl(static_cast<int>(bits), from_lane + 1));
+          signs.from_bits((here | next << 8) >> (n & 7));
         }
         if constexpr (!KEYS) {
           const uint32_t off = past | static_cast<uint32_t>((frames - 1 - i) >> 31);
@@ -521,7 +535,7 @@ __global__ __launch_bounds__(256) void net_joint_join(JointGradParams p) {
   const int tl = p.logit_lens[b], ul = p.label_lens[b];
   float f[4] = {};
   if (tl >= 0 && tl <= p.T && ul < p.U1 && u <= ul) {
-    const int n = (tl + tile_frames(sizeof(T)) - 1) / tile_frames(sizeof(T));
+    const int n = (tl + p.tile_frames - 1) / p.tile_frames;
     const float* part = p.part + (static_cast<int64_t>(b) * p.t_blocks * p.U1 + u) * p.H + c;
     const int64_t step = static_cast<int64_t>(p.U1) * p.H;
 #pragma unroll 4
@@ -556,13 +570,35 @@ rnnt_status_t check(const rnnt_joint_shape_t& s, rnnt_activation_t act, double p
   return RNNT_OK;
 }
 
-int tile_count(const rnnt_joint_shape_t& s) {
-  const int64_t n = tile_frames(static_cast<int>(net_elem_bytes(s.dtype)));
-  return static_cast<int>((s.T_max + n - 1) / n);
-}
+// Lanes to a row (eight channels each), and the slices of channels that blocks share a row out in.
+struct GradShape {
+  int lanes, slices, wave_frames, t_blocks;
+
+  // In float32 at most four frames to a wave, else eight, so that the block's float32 sums are a sixteenth of
+  // dh; half as many, for twice the blocks and sums, where the blocks would not be three to a CU (B=16 T=150
+  // U=40 H=321 f32 tanh, 480 blocks of four frames: 47 us, 912 of two: 37; B=32 T=250 U=80 H=640 bf16, 1280
+  // of eight: 133, 2520 of four: 138).
+  GradShape(const rnnt_joint_shape_t& s, bool dropping) {
+    lanes = s.H <= 32 ? 4 : s.H <= 64 ? 8 : 16;
+    const int wide = s.H % 8 == 0 || !dropping ? lanes : lanes - 1;
+    slices = (s.H + 8 * wide - 1) / (8 * wide);
+    wave_frames = s.dtype == RNNT_DTYPE_F32 ? 4 : 8;
+    count(s);
+    if (static_cast<int64_t>(s.B) * t_blocks * slices < 768) {
+      wave_frames /= 2;
+      count(s);
+    }
+  }
+  void count(const rnnt_joint_shape_t& s) {
+    const int64_t n = wave_frames * kGradWaves;
+    t_blocks = static_cast<int>((s.T_max + n - 1) / n);
+  }
+};
 
 size_t grad_bytes(const rnnt_joint_shape_t& s) {
-  return net_align256(static_cast<size_t>(s.B) * tile_count(s) * (static_cast<size_t>(s.U_max) + 1) * s.H * sizeof(float));
+  const GradShape with(s, true), without(s, false);  // the same call size whatever p is
+  const int64_t blocks = with.t_blocks > without.t_blocks ? with.t_blocks : without.t_blocks;
+  return net_align256(static_cast<size_t>(s.B) * blocks * (static_cast<size_t>(s.U_max) + 1) * s.H * sizeof(float));
 }
 
 template <typename F>
@@ -622,17 +658,22 @@ rnnt_status_t rnnt_joint_hidden(const void* enc, const void* pred, rnnt_joint_sh
   q.U1 = shape.U_max + 1;
   q.H = shape.H;
   const bool eights = shape.H % 8 == 0;
-  q.t_blocks = eights ? (shape.T_max + kJointFrames - 1) / kJointFrames : shape.T_max;
   const int64_t groups = (static_cast<int64_t>(q.U1) * shape.H + 7) / 8 + (eights ? 0 : 1);
-  const int64_t x = static_cast<int64_t>(shape.B) * q.t_blocks, y = (groups + 256 * kJointRun - 1) / (256 * kJointRun);
+  // a frame to a block where kJointFrames would leave the chip fewer than eight blocks to a CU
+  const int64_t y = (groups + 256 * kJointRun - 1) / (256 * kJointRun);
+  const int64_t full = (static_cast<int64_t>(shape.T_max) + kJointFrames - 1) / kJointFrames;
+  q.block_frames = full * shape.B * y >= 2048 ? kJointFrames : 1;
+  q.t_blocks = static_cast<int32_t>(q.block_frames == 1 ? shape.T_max : full);
+  const int64_t x = static_cast<int64_t>(shape.B) * q.t_blocks;
   if (x > kMaxRows / 256 || y > 65535) return RNNT_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<uint32_t>(x), static_cast<uint32_t>(y));
+  const int64_t lds = (static_cast<int64_t>(shape.H) + 8 + (shape.H + 8) / 8) * q.block_frames * static_cast<int64_t>(sizeof(float));
   return with_dtype(shape.dtype, [&](auto t) {
     return with_activation(act, [&](auto a) {
       using T = decltype(t);
       constexpr int A = decltype(a)::value;
       if (eights) hipLaunchKernelGGL((net_joint<T, A>), grid, dim3(256), 0, stream, q);
-      else if (shape.H <= kJointLdsH) hipLaunchKernelGGL((net_joint_odd<T, A, true>), grid, dim3(256), 0, stream, q);
+      else if (lds <= kJointLdsBytes) hipLaunchKernelGGL((net_joint_odd<T, A, true>), grid, dim3(256), static_cast<size_t>(lds), stream, q);
       else hipLaunchKernelGGL((net_joint_odd<T, A, false>), grid, dim3(256), 0, stream, q);
       return launched();
     });
@@ -672,9 +713,11 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
   q.H = shape.H;
   q.part = reinterpret_cast<float*>(ws.ptr);
   q.factor = q.drop.scale * (act == RNNT_ACT_TANH ? 4.f : 1.f);
-  q.t_blocks = tile_count(shape);
-  q.lanes = shape.H <= 32 ? 4 : shape.H <= 64 ? 8 : 16;
-  q.slices = (shape.H + 8 * q.lanes - 1) / (8 * q.lanes);
+  const GradShape cut(shape, q.drop.threshold != 0);
+  q.t_blocks = cut.t_blocks;
+  q.lanes = cut.lanes;
+  q.slices = cut.slices;
+  q.tile_frames = cut.wave_frames * kGradWaves;
   const int64_t x = static_cast<int64_t>(shape.B) * q.t_blocks * q.slices;
   const int64_t joins = (static_cast<int64_t>(shape.B) * q.U1 * ((shape.H + 3) / 4) + 255) / 256;
   // a block's sums are one buffer of less than 2^31 bytes
@@ -693,17 +736,17 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
       });
     }
     const rnnt_status_t done = with_activation(act, [&](auto a) {
-      constexpr int A = decltype(a)::value;
       const dim3 grid(static_cast<uint32_t>(x)), block(64 * kGradWaves);
       const bool drop = q.drop.threshold != 0;
-      if (shape.H % 8 == 0) {
-        if (drop) hipLaunchKernelGGL((net_joint_grad<T, A, true, true>), grid, block, 0, stream, q);
-        else hipLaunchKernelGGL((net_joint_grad<T, A, true, false>), grid, block, 0, stream, q);
-      } else {
-        if (drop) hipLaunchKernelGGL((net_joint_grad<T, A, false, true>), grid, block, 0, stream, q);
-        else hipLaunchKernelGGL((net_joint_grad<T, A, true, false>), grid, block, 0, stream, q);
-      }
-      return launched();
+      const auto run = [&](auto frames) {
+        constexpr int A = decltype(a)::value, F = decltype(frames)::value;
+        if (drop && shape.H % 8 != 0) hipLaunchKernelGGL((net_joint_grad<T, A, false, true, F>), grid, block, 0, stream, q);
+        else if (drop) hipLaunchKernelGGL((net_joint_grad<T, A, true, true, F>), grid, block, 0, stream, q);
+        else hipLaunchKernelGGL((net_joint_grad<T, A, true, false, F>), grid, block, 0, stream, q);
+        return launched();
+      };
+      constexpr int FULL = sizeof(T) == 4 ? 4 : 8;
+      return cut.wave_frames == FULL ? run(std::integral_constant<int, FULL>{}) : run(std::integral_constant<int, FULL / 2>{});
     });
     if (done != RNNT_OK) return done;
     hipLaunchKernelGGL((net_joint_join<T>), dim3(static_cast<uint32_t>(joins)), dim3(256), 0, stream, q);
