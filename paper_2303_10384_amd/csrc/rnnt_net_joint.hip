@@ -233,10 +233,10 @@ __global__ __launch_bounds__(256) void net_joint_odd(JointParams p) {
 }
 
 // ---- its gradient -------------------------------------------------------------
-// A block takes tile_frames() frames of an utterance and a slice of channels, and goes over the units: dh is
+// A block takes the frames of its waves, of one utterance, and a slice of channels, and goes over the units: dh is
 // read once.  A wave holds the sums over u of its frames in registers (denc is finished in the block); the sums
-// over its frames meet in LDS, and the block's go to the workspace, one float32 row for 32 rows of a 16-bit dh
-// or 16 of a float32 one (a sixteenth of the bytes), which net_joint_join adds up in the order of the frames.
+// over its frames meet in LDS, and the block's go to the workspace, one float32 row for 16 rows of a 16-bit dh
+// or 8 of a float32 one (an eighth of the bytes), which net_joint_join adds up in the order of the frames.
 
 struct JointGradParams {
   const void *enc, *pred, *dh;
@@ -250,6 +250,8 @@ struct JointGradParams {
 };
 
 constexpr int kGradWaves = 4;
+template <typename T>
+constexpr int kWaveFrames = sizeof(T) == 4 ? 2 : 4;  // frames of a wave (GradShape says why)
 
 // Whether enc + pred > 0 for two 16-bit elements at a time, without the sums: the sum of two floats is
 // positive exactly when enc > -pred, and the bits of a float, its lower 15 flipped where the sign is set, are
@@ -353,10 +355,10 @@ __device__ __forceinline__ int longest_first(const int32_t* label_lens, int B, i
 // EIGHTS: rows are multiples of eight elements, so that a group's numbers are one block.  H is at least 8 here: the
 // last group of a row that is no multiple begins at H - 8, its first channels also the group's before it, which
 // computes and writes the same values.
-template <typename T, int ACT, bool EIGHTS, bool DROP, int FRAMES>
+template <typename T, int ACT, bool EIGHTS, bool DROP>
 __global__ __launch_bounds__(64 * kGradWaves) void net_joint_grad(JointGradParams p) {
   constexpr bool KEYS = ACT == RNNT_ACT_RELU && sizeof(T) == 2;
-  constexpr int WAVES = kGradWaves;
+  constexpr int WAVES = kGradWaves, FRAMES = kWaveFrames<T>;
   static_assert(WAVES == 4, "256 threads store a step's 512 sums");
   __shared__ __attribute__((aligned(16))) float sums[2][WAVES][512];
   const int slice = static_cast<int>(blockIdx.x) % p.slices, bt = static_cast<int>(blockIdx.x) / p.slices;
@@ -570,35 +572,26 @@ rnnt_status_t check(const rnnt_joint_shape_t& s, rnnt_activation_t act, double p
   return RNNT_OK;
 }
 
-// Lanes to a row (eight channels each), and the slices of channels that blocks share a row out in.
+// Lanes to a row (eight channels each), the slices of channels that blocks share a row out in, and their tiles of
+// frames.  Few frames to a wave leave room for twice the waves, which counts for more than the float32 sums
+// (an eighth of dh): eight or four frames of bfloat16 to a wave, B=32 T=250 U=80, H=320: 72 + 4 us (gradient and
+// join) or 65 + 6, H=640: 110 + 7 or 101 + 10, H=1024: 176 + 9 or 159 + 14; four or two of float32,
+// B=16 T=150 U=40 H=321 tanh: 46 + 4 or 40 + 6.
 struct GradShape {
-  int lanes, slices, wave_frames, t_blocks;
+  int lanes, slices, tile_frames, t_blocks;
 
-  // In float32 at most four frames to a wave, else eight, so that the block's float32 sums are a sixteenth of
-  // dh; half as many, for twice the blocks and sums, where the blocks would not be three to a CU (B=16 T=150
-  // U=40 H=321 f32 tanh, 480 blocks of four frames: 47 us, 912 of two: 37; B=32 T=250 U=80 H=640 bf16, 1280
-  // of eight: 133, 2520 of four: 138).
   GradShape(const rnnt_joint_shape_t& s, bool dropping) {
     lanes = s.H <= 32 ? 4 : s.H <= 64 ? 8 : 16;
     const int wide = s.H % 8 == 0 || !dropping ? lanes : lanes - 1;
     slices = (s.H + 8 * wide - 1) / (8 * wide);
-    wave_frames = s.dtype == RNNT_DTYPE_F32 ? 4 : 8;
-    count(s);
-    if (static_cast<int64_t>(s.B) * t_blocks * slices < 768) {
-      wave_frames /= 2;
-      count(s);
-    }
-  }
-  void count(const rnnt_joint_shape_t& s) {
-    const int64_t n = wave_frames * kGradWaves;
-    t_blocks = static_cast<int>((s.T_max + n - 1) / n);
+    tile_frames = kGradWaves * (s.dtype == RNNT_DTYPE_F32 ? kWaveFrames<float> : kWaveFrames<bf16_t>);
+    t_blocks = static_cast<int>((static_cast<int64_t>(s.T_max) + tile_frames - 1) / tile_frames);
   }
 };
 
 size_t grad_bytes(const rnnt_joint_shape_t& s) {
-  const GradShape with(s, true), without(s, false);  // the same call size whatever p is
-  const int64_t blocks = with.t_blocks > without.t_blocks ? with.t_blocks : without.t_blocks;
-  return net_align256(static_cast<size_t>(s.B) * blocks * (static_cast<size_t>(s.U_max) + 1) * s.H * sizeof(float));
+  const GradShape cut(s, true);  // the same whatever p is
+  return net_align256(static_cast<size_t>(s.B) * cut.t_blocks * (static_cast<size_t>(s.U_max) + 1) * s.H * sizeof(float));
 }
 
 template <typename F>
@@ -717,7 +710,7 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
   q.t_blocks = cut.t_blocks;
   q.lanes = cut.lanes;
   q.slices = cut.slices;
-  q.tile_frames = cut.wave_frames * kGradWaves;
+  q.tile_frames = cut.tile_frames;
   const int64_t x = static_cast<int64_t>(shape.B) * q.t_blocks * q.slices;
   const int64_t joins = (static_cast<int64_t>(shape.B) * q.U1 * ((shape.H + 3) / 4) + 255) / 256;
   // a block's sums are one buffer of less than 2^31 bytes
@@ -738,15 +731,11 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
     const rnnt_status_t done = with_activation(act, [&](auto a) {
       const dim3 grid(static_cast<uint32_t>(x)), block(64 * kGradWaves);
       const bool drop = q.drop.threshold != 0;
-      const auto run = [&](auto frames) {
-        constexpr int A = decltype(a)::value, F = decltype(frames)::value;
-        if (drop && shape.H % 8 != 0) hipLaunchKernelGGL((net_joint_grad<T, A, false, true, F>), grid, block, 0, stream, q);
-        else if (drop) hipLaunchKernelGGL((net_joint_grad<T, A, true, true, F>), grid, block, 0, stream, q);
-        else hipLaunchKernelGGL((net_joint_grad<T, A, true, false, F>), grid, block, 0, stream, q);
-        return launched();
-      };
-      constexpr int FULL = sizeof(T) == 4 ? 4 : 8;
-      return cut.wave_frames == FULL ? run(std::integral_constant<int, FULL>{}) : run(std::integral_constant<int, FULL / 2>{});
+      constexpr int A = decltype(a)::value;
+      if (drop && shape.H % 8 != 0) hipLaunchKernelGGL((net_joint_grad<T, A, false, true>), grid, block, 0, stream, q);
+      else if (drop) hipLaunchKernelGGL((net_joint_grad<T, A, true, true>), grid, block, 0, stream, q);
+      else hipLaunchKernelGGL((net_joint_grad<T, A, true, false>), grid, block, 0, stream, q);
+      return launched();
     });
     if (done != RNNT_OK) return done;
     hipLaunchKernelGGL((net_joint_join<T>), dim3(static_cast<uint32_t>(joins)), dim3(256), 0, stream, q);
