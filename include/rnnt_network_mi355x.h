@@ -84,6 +84,8 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
  *   dx_t = (1 - a_t) s_t,  dz_t = s_t (h_{t-1} - x_t) a_t (1 - a_t),  dh0 = a_0 s_0
  * (dlast where lens[b] = 0).  dx, dz (B, L, D); dh0 (B, D) float32 or NULL.
  *
+ * Only long sequences that are few need a workspace (0 bytes: none).
+ *
  * RNNT_ERR_BAD_SHAPE: B < 1, L < 0, D < 1, or a stride below 0.
  * RNNT_ERR_UNSUPPORTED: L > 2^30, D > 2^21, or B * ceil(D / 64) of 2^21 or more.
  */

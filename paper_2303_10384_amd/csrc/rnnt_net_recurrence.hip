@@ -445,7 +445,7 @@ void segments_of(const rnnt_recurrence_shape_t& s, RecurrenceParams* p) {
 size_t pair_bytes(const rnnt_recurrence_shape_t& s) {
   RecurrenceParams p{};
   segments_of(s, &p);
-  return net_align256(p.segments > 1 ? static_cast<size_t>(s.B) * p.segments * s.D * sizeof(float2) : 256);
+  return p.segments > 1 ? net_align256(static_cast<size_t>(s.B) * p.segments * s.D * sizeof(float2)) : 0;
 }
 
 template <typename F>

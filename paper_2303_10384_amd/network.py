@@ -68,9 +68,16 @@ def _library():
     return lib
 
 
+# A call's descriptor and the bytes of its workspace; a program makes the same few again and again.
+@functools.lru_cache(maxsize=1024)
+def _shape(kind, size_of, *fields):
+    shape = kind(*fields)
+    return shape, getattr(_library(), size_of)(shape)
+
+
 def _call(fn, device, *args):
     """fn(*args, stream) with the tensors' GPU current; its status as an RNNTError."""
-    if device.index == torch.cuda.current_device():
+    if device.index == torch._C._cuda_getDevice():
         st = fn(*args, _stream_handle(device))
     else:
         with torch.cuda.device(device):
@@ -89,19 +96,10 @@ def _check(name, t, device=None, dtype=None, shape=None, contiguous=True):
         raise ValueError("%s must be on %s, got %s" % (name, device, t.device))
     if dtype is not None and t.dtype != dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if shape is not None and tuple(t.shape) != shape:
-        raise ValueError("%s must have shape %s, got %s" % (name, shape, tuple(t.shape)))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     if contiguous and not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-
-
-def _check_lens(name, lens, device, B):
-    if lens is not None:
-        _check(name, lens, device, torch.int32, (B,))
-
-
-def _check_rng(rng, device):
-    _check("rng", rng, device, torch.int64, (2,))
 
 
 def _check_p(p):
@@ -112,14 +110,16 @@ def _check_p(p):
 
 
 def _result(shape, dtype, device, nbytes):
-    """A result tensor and the workspace of the call that fills it: (tensor, workspace arguments).
+    """A result tensor and the workspace of the call that fills it, or None.
 
     Under a stream capture the workspace is the rest of the result's memory, so that it belongs
     to the graph for as long as the program holds what the graph computes, whoever began the
     capture; else it is a block of torch's allocator, free again behind the call's kernels (None
     where torch has no memory left: the library then takes its own)."""
-    if not nbytes or not torch.cuda.is_current_stream_capturing():
-        return torch.empty(shape, dtype=dtype, device=device), _call_workspace(nbytes, device) if nbytes else None
+    if not nbytes:
+        return torch.empty(shape, dtype=dtype, device=device), None
+    if not torch.cuda.is_current_stream_capturing():
+        return torch.empty(shape, dtype=dtype, device=device), _call_workspace(nbytes, device)
     size = -(-math.prod(shape) * dtype.itemsize // 256) * 256
     both = torch.empty(size + nbytes, dtype=torch.uint8, device=device)
     return torch.empty(0, dtype=dtype, device=device).set_(both.untyped_storage(), 0, shape), both[size:]
@@ -130,9 +130,10 @@ def _result(shape, dtype, device, nbytes):
 def _embedding_forward(labels, weight, lens, scale, start):
     B, N = labels.shape
     V, D = weight.shape
-    shape = EmbeddingShape(B, N, V, D, start, dtype_code(weight.dtype))
+    shape = _shape(EmbeddingShape, "rnnt_label_embedding_grad_workspace_bytes", B, N, V, D, start, dtype_code(weight.dtype))
     out = torch.empty((B, N + (start >= 0), D), dtype=weight.dtype, device=weight.device)
-    _call(_library().rnnt_label_embedding, weight.device, _ptr(labels), _ptr(lens), shape, _ptr(weight), scale, _ptr(out))
+    _call(_library().rnnt_label_embedding, weight.device, _ptr(labels), _ptr(lens), shape[0], _ptr(weight), scale,
+          _ptr(out))
     return out, shape
 
 
@@ -148,10 +149,9 @@ class _LabelEmbedding(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dout):
         labels, lens = ctx.saved_tensors
-        lib, shape, dout = _library(), ctx.shape, dout.contiguous()
-        dw, ws = _result((shape.V, shape.D), dout.dtype, dout.device,
-                         lib.rnnt_label_embedding_grad_workspace_bytes(shape))
-        _call(lib.rnnt_label_embedding_grad, dout.device, _ptr(labels), _ptr(lens), shape, _ptr(dout), ctx.scale,
+        (shape, nbytes), dout = ctx.shape, dout.contiguous()
+        dw, ws = _result((shape.V, shape.D), dout.dtype, dout.device, nbytes)
+        _call(_library().rnnt_label_embedding_grad, dout.device, _ptr(labels), _ptr(lens), shape, _ptr(dout), ctx.scale,
               _ptr(dw), *_workspace_args(ws))
         return None, dw, None, None, None
 
@@ -168,7 +168,8 @@ def label_embedding(labels, weight, lens=None, scale=1.0, start=None):
     _check("labels", labels, weight.device, torch.int32)
     if labels.dim() != 2 or weight.dim() != 2:
         raise ValueError("labels must be (B, N) and weight (V, D)")
-    _check_lens("lens", lens, weight.device, labels.shape[0])
+    if lens is not None:
+        _check("lens", lens, weight.device, torch.int32, labels.shape[:1])
     dtype_code(weight.dtype)
     if start is not None and not 0 <= start < weight.shape[0]:
         raise ValueError("start must be None or a row of weight, got %r" % (start,))
@@ -183,14 +184,14 @@ def label_embedding(labels, weight, lens=None, scale=1.0, start=None):
 def _recurrence_forward(x, z, h0, lens, with_states):
     B, L, D = x.shape
     dev = x.device
-    lib = _library()
-    shape = RecurrenceShape(B, L, D, dtype_code(x.dtype), x.stride(0), x.stride(1), z.stride(0), z.stride(1))
-    h, ws = _result((B, L, D), x.dtype, dev, lib.rnnt_recurrence_workspace_bytes(shape))
+    shape, nbytes = both = _shape(RecurrenceShape, "rnnt_recurrence_workspace_bytes", B, L, D, dtype_code(x.dtype),
+                                  *x.stride()[:2], *z.stride()[:2])
+    h, ws = _result((B, L, D), x.dtype, dev, nbytes)
     last = torch.empty((B, D), dtype=torch.float32, device=dev)
     states = torch.empty((B, -(-L // STATE_STEPS), D), dtype=torch.float32, device=dev) if with_states else None
-    _call(lib.rnnt_recurrence, dev, _ptr(x), _ptr(z), shape, _ptr(lens), _ptr(h0), _ptr(h), _ptr(last), _ptr(states),
+    _call(_library().rnnt_recurrence, dev, _ptr(x), _ptr(z), shape, _ptr(lens), _ptr(h0), _ptr(h), _ptr(last), _ptr(states),
           *_workspace_args(ws))
-    return h, last, states, shape
+    return h, last, states, both
 
 
 class _GatedRecurrence(torch.autograd.Function):
@@ -205,13 +206,13 @@ class _GatedRecurrence(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dh, dlast):
         x, z, lens, states = ctx.saved_tensors
-        lib, shape, dev = _library(), ctx.shape, x.device
+        (shape, nbytes), dev = ctx.shape, x.device
         dh = None if dh is None else dh.contiguous()
         dlast = None if dlast is None else dlast.contiguous()
-        dx, ws = _result(tuple(x.shape), x.dtype, dev, lib.rnnt_recurrence_workspace_bytes(shape))
+        dx, ws = _result(x.shape, x.dtype, dev, nbytes)
         dz = torch.empty(x.shape, dtype=x.dtype, device=dev)
         dh0 = torch.empty((shape.B, shape.D), dtype=torch.float32, device=dev) if ctx.needs_input_grad[2] else None
-        _call(lib.rnnt_recurrence_grad, dev, _ptr(x), _ptr(z), shape, _ptr(lens), _ptr(states), _ptr(dh), _ptr(dlast),
+        _call(_library().rnnt_recurrence_grad, dev, _ptr(x), _ptr(z), shape, _ptr(lens), _ptr(states), _ptr(dh), _ptr(dlast),
               _ptr(dx), _ptr(dz), _ptr(dh0), *_workspace_args(ws))
         return dx, dz, dh0, None
 
@@ -229,13 +230,14 @@ def gated_recurrence(x, z, h0=None, lens=None):
     if x.dim() != 3:
         raise ValueError("x must be (B, L, D)")
     dtype_code(x.dtype)
-    _check("z", z, x.device, x.dtype, tuple(x.shape), contiguous=False)
+    _check("z", z, x.device, x.dtype, x.shape, contiguous=False)
     for name, t in (("x", x), ("z", z)):
         if t.numel() > 0 and t.shape[2] > 1 and t.stride(2) != 1:
             raise ValueError("%s must have contiguous channels" % name)
     if h0 is not None:
         _check("h0", h0, x.device, torch.float32, (x.shape[0], x.shape[2]))
-    _check_lens("lens", lens, x.device, x.shape[0])
+    if lens is not None:
+        _check("lens", lens, x.device, torch.int32, x.shape[:1])
     if torch.is_grad_enabled() and (x.requires_grad or z.requires_grad or (h0 is not None and h0.requires_grad)):
         return _GatedRecurrence.apply(x, z, h0, lens)
     return _recurrence_forward(x, z, h0, lens, False)[:2]
@@ -275,7 +277,7 @@ def dropout(x, p, rng):
     _check("x", x)
     dtype_code(x.dtype)
     p = _check_p(p)
-    _check_rng(rng, x.device)
+    _check("rng", rng, x.device, torch.int64, (2,))
     if x.requires_grad and torch.is_grad_enabled():
         return _Dropout.apply(x, p, rng)
     return _dropout_call(x, p, rng)
@@ -286,10 +288,10 @@ def dropout(x, p, rng):
 def _joint_forward(enc, pred, logit_lens, label_lens, act, p, rng, rng_out=None):
     B, T, H = enc.shape
     U1 = pred.shape[1]
-    shape = JointShape(B, T, U1 - 1, H, dtype_code(enc.dtype))
+    shape = _shape(JointShape, "rnnt_joint_hidden_grad_workspace_bytes", B, T, U1 - 1, H, dtype_code(enc.dtype))
     h = torch.empty((B, T, U1, H), dtype=enc.dtype, device=enc.device)
-    _call(_library().rnnt_joint_hidden, enc.device, _ptr(enc), _ptr(pred), shape, _ptr(logit_lens), _ptr(label_lens), act,
-          p, _ptr(rng), _ptr(rng_out), _ptr(h))
+    _call(_library().rnnt_joint_hidden, enc.device, _ptr(enc), _ptr(pred), shape[0], _ptr(logit_lens), _ptr(label_lens),
+          act, p, _ptr(rng), _ptr(rng_out), _ptr(h))
     return h, shape
 
 
@@ -306,10 +308,10 @@ class _JointHidden(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dh):
         enc, pred, logit_lens, label_lens, used = ctx.saved_tensors
-        lib, dh = _library(), dh.contiguous()
-        denc, ws = _result(tuple(enc.shape), enc.dtype, enc.device, lib.rnnt_joint_hidden_grad_workspace_bytes(ctx.shape))
+        (shape, nbytes), dh = ctx.shape, dh.contiguous()
+        denc, ws = _result(enc.shape, enc.dtype, enc.device, nbytes)
         dpred = torch.empty_like(pred)
-        _call(lib.rnnt_joint_hidden_grad, enc.device, _ptr(enc), _ptr(pred), ctx.shape, _ptr(logit_lens),
+        _call(_library().rnnt_joint_hidden_grad, enc.device, _ptr(enc), _ptr(pred), shape, _ptr(logit_lens),
               _ptr(label_lens), ctx.act, ctx.p, _ptr(used), _ptr(dh), _ptr(denc), _ptr(dpred), *_workspace_args(ws))
         return denc, dpred, None, None, None, None, None
 
@@ -337,7 +339,7 @@ def joint_hidden(enc, pred, logit_lens, label_lens, activation="relu", p=0.0, rn
     if p > 0.0 and rng is None:
         raise ValueError("dropout needs rng")
     if rng is not None:
-        _check_rng(rng, enc.device)
+        _check("rng", rng, enc.device, torch.int64, (2,))
     args = (enc, pred, logit_lens, label_lens, ACTIVATIONS[activation], p, rng)
     if torch.is_grad_enabled() and (enc.requires_grad or pred.requires_grad):
         return _JointHidden.apply(*args)

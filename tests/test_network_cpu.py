@@ -65,10 +65,11 @@ def test_embedding_refusals(net):
 
 def test_recurrence_refusals(net):
     lib, S = net._library(), net.RecurrenceShape
-    ok = S(2, 40, 5, 0, 200, 5, 200, 5)
+    assert lib.rnnt_recurrence_workspace_bytes(S(2, 40, 5, 0, 200, 5, 200, 5)) == 0  # one block to a sequence
+    ok = S(2, 4000, 5, 0, 20000, 5, 20000, 5)
     need = lib.rnnt_recurrence_workspace_bytes(ok)
     assert need > 0 and need % 256 == 0
-    assert lib.rnnt_recurrence_states_bytes(ok) == 2 * -(-40 // net.STATE_STEPS) * 5 * 4
+    assert lib.rnnt_recurrence_states_bytes(ok) == 2 * -(-4000 // net.STATE_STEPS) * 5 * 4
     fwd = {"x": FAKE, "z": FAKE, "shape": ok, "lens": FAKE, "h0": FAKE, "h": FAKE, "last": FAKE, "states": FAKE,
            "ws": FAKE, "bytes": need - 1, "stream": None}
     bwd = {"x": FAKE, "z": FAKE, "shape": ok, "lens": FAKE, "states": FAKE, "dh": FAKE, "dlast": FAKE, "dx": FAKE,
