@@ -434,8 +434,9 @@ __global__ __launch_bounds__(64 * kGradWaves) void net_joint_grad(JointGradParam
         if constexpr (DROP && EIGHTS) {
           signs.signs_below(random_block(rng, (number[i] + at) >> 3), p.drop.threshold);
         } else if constexpr (DROP) {
-          // the row's lanes form the blocks that its slice meets, one each; an element's may be two of them
-          const uint64_t n = number[i] + at, n_row = number[i] + static_cast<uint32_t>(u * p.H + c0);
+          // the row's lanes form the blocks that its slice meets, one each, from the one of its first channel on
+          // (H - 8 where the slice has fewer than eight); a group's numbers may be of two of them
+          const uint64_t n = number[i] + at, n_row = number[i] + static_cast<uint32_t>(u * p.H + min(c0, p.H - 8));
           signs.signs_below(random_block(rng, (n_row >> 3) + (lane & (p.lanes - 1))), p.drop.threshold);
           const uint32_t bits = signs.bits();
           const int from_lane = (lane & ~(p.lanes - 1)) + static_cast<int>((n >> 3) - (n_row >> 3));

@@ -333,6 +333,8 @@ JOINT = [  # B, T, U, H, lengths
     (1, 1, 0, 1, "full"), (16, 1, 0, 64, "full"), (2, 5, 3, 7, "any"), (3, 9, 4, 64, "any"), (2, 33, 2, 129, "any"),
     (1, 2, 40, 136, "any"), (2, 7, 6, 321, "any"), (4, 40, 1, 8, "any"), (1, 70, 70, 16, "any"), (2, 3, 2, 640, "zero"),
     (1, 17, 5, 520, "full"), (1, 130, 3, 24, "full")]
+# rows whose last slice of channels has one to seven (slices of 15, 7 and 3 groups with dropout, of 16, 8 and 4 without)
+JOINT_TAILS = [121, 125, 127, 131, 241, 247, 57, 61, 25, 31, 9, 15]
 
 
 def joint_case(torch, B, T, U, H, lengths, dtype, seed):  # noqa: F811
@@ -378,6 +380,20 @@ def test_joint(torch, pkg, case, p, dtype, act):  # noqa: F811
         if p:
             state -= 1
         assert torch.equal(h, pkg.joint_hidden(enc, pred, ints(torch, tl), ints(torch, ul), act, p, state))
+
+
+@pytest.mark.parametrize("act,dtype", [("relu", "bf16"), ("tanh", "f32")])
+@pytest.mark.parametrize("H", JOINT_TAILS)
+def test_joint_rows_with_a_short_last_slice(torch, pkg, H, act, dtype):  # noqa: F811
+    for p in (0.0, 0.4):
+        enc, pred, dh, encd, predd, dhd, tl, ul = joint_case(torch, 2, 6, 4, H, "any", dtype, 10 + H)
+        enc.requires_grad_(True)
+        pred.requires_grad_(True)
+        h = pkg.joint_hidden(enc, pred, ints(torch, tl), ints(torch, ul), act, p, rng_of(torch, 5, 6))
+        want, wenc, wpred, senc, spred = R.joint_hidden(encd, predd, tl, ul, act, p, 5, 6, dhd)
+        close(h, want, (HALF[dtype] + 2.0 ** -20 + 2 * ONE) * np.abs(want) + TINY[dtype], "h")
+        for got, w, size, n in zip(torch.autograd.grad(h, (enc, pred), dh), (wenc, wpred), (senc, spred), (5, 6)):
+            close(got, w, HALF[dtype] * np.abs(w) + (2.0 ** -20 + 10 * 2.0 ** -23 + (n + 3) * ONE) * size + TINY[dtype], "grad")
 
 
 def test_joint_bad_lengths(torch, pkg):  # noqa: F811
