@@ -48,7 +48,8 @@ extern "C" {
  * Every element of dweight (V, D) is written.
  *
  * RNNT_ERR_BAD_SHAPE: B < 1, N < 0, V < 1, D < 1 or start outside [-1, V).
- * RNNT_ERR_UNSUPPORTED: 2^31 or more rows in the output.
+ * RNNT_ERR_UNSUPPORTED: more than 2^31 - 2^16 - 1 rows in the output, or 2^25 or more
+ * of V * ceil(D / (64 groups of 16 bytes)) in the gradient.
  */
 typedef struct {
   int32_t B, N, V, D;

@@ -124,21 +124,20 @@ struct SortBoard {
   int32_t below[kSortWaves], sum[kSortWaves];
 };
 
-// f(row, key - lo) for the 64 rows of every group of a stretch, the keys of eight groups on their way at once
+// f(row, key) for the 64 rows of every group of a stretch, the keys of eight groups on their way at once
 template <typename F>
-__device__ __forceinline__ void for_rows(const EmbeddingGradParams& p, int64_t begin, int64_t end, int lane, F&& f) {
+__device__ __forceinline__ void for_rows(const EmbeddingGradParams& p, int begin, int end, int lane, F&& f) {
   constexpr int BATCH = 8;
-  for (int64_t r = begin + lane; r < end + lane; r += 64 * BATCH) {
+  int r = begin;
+  for (; r + 64 * BATCH <= end; r += 64 * BATCH) {  // whole batches: nothing to check
+    const int32_t* keys = p.keys + r + lane;
     int32_t key[BATCH];
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-      const int64_t at = r + 64 * i;
-      key[i] = p.keys[min(at, static_cast<int64_t>(p.rows) - 1)];
-      key[i] = at < end ? key[i] : kNoKey;
-    }
+    for (int i = 0; i < BATCH; ++i) key[i] = keys[64 * i];
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) f(static_cast<int32_t>(r + 64 * i), key[i]);
+    for (int i = 0; i < BATCH; ++i) f(r + 64 * i + lane, key[i]);
   }
+  for (; r < end; r += 64) f(r + lane, r + lane < end ? p.keys[r + lane] : kNoKey);
 }
 
 __global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingGradParams p) {
@@ -148,7 +147,8 @@ __global__ __launch_bounds__(64 * kSortWaves) void net_embedding_sort(EmbeddingG
   for (int i = threadIdx.x; i < kSortWaves * kSortTokens; i += 64 * kSortWaves) (&s.place[0][0])[i] = 0;
   __syncthreads();
   const int64_t stretch = ((static_cast<int64_t>(p.rows) + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-  const int64_t begin = wave * stretch, end = min(begin + stretch, static_cast<int64_t>(p.rows));
+  const int begin = static_cast<int>(min(wave * stretch, static_cast<int64_t>(p.rows)));
+  const int end = static_cast<int>(min(begin + stretch, static_cast<int64_t>(p.rows)));
   int32_t* mine = s.place[wave];
   const uint64_t before = (uint64_t{1} << lane) - 1;
   int less = 0, kept = 0;
@@ -370,7 +370,7 @@ rnnt_status_t check(const int32_t* labels, const rnnt_embedding_shape_t& s, Toke
   if (s.B < 1 || s.N < 0 || s.V < 1 || s.D < 1 || s.start < -1 || s.start >= s.V) return RNNT_ERR_BAD_SHAPE;
   if (!net_dtype_known(s.dtype)) return RNNT_ERR_BAD_DTYPE;
   const int64_t n1 = static_cast<int64_t>(s.N) + (s.start >= 0);
-  if (n1 * s.B > kMaxRows) return RNNT_ERR_UNSUPPORTED;
+  if (n1 * s.B > kMaxRows - (1 << 16)) return RNNT_ERR_UNSUPPORTED;
   if (!labels && s.N > 0) return RNNT_ERR_NULL_PTR;
   *src = TokenSource{labels, lens, s.B, s.N, static_cast<int32_t>(n1), s.V, s.start};
   return RNNT_OK;

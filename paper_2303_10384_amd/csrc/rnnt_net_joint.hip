@@ -34,8 +34,9 @@ __global__ __launch_bounds__(256) void net_dropout(DropoutParams p) {
   const T* x = static_cast<const T*>(p.x) + n0;
   T* y = static_cast<T*>(p.y) + n0;
   Pack<T, 8> k;
-  const bool whole = n0 + 8 <= p.n;
-  if (whole) k.load(x);
+  const bool whole = n0 + 8 <= p.n, pair = (block | 1) * 8 + 8 <= p.n;  // the neighbour's group too
+  if (pair) load_pair(k, x);
+  else if (whole) k.load(x);
   else k.load_part(x, static_cast<int>(p.n - n0));
   Dropped drop;
   dropped_of(p.drop, load_rng(p.drop.rng), static_cast<uint64_t>(block), drop);
@@ -45,7 +46,8 @@ __global__ __launch_bounds__(256) void net_dropout(DropoutParams p) {
   for (int j = 0; j < 8; ++j) f[j] *= p.drop.scale;
   k.set(f);
   drop.clear(k);
-  if (whole) k.store(y);
+  if (pair) store_pair(k, y);
+  else if (whole) k.store(y);
   else k.store_part(y, static_cast<int>(p.n - n0));
 }
 
