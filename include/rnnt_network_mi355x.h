@@ -48,8 +48,8 @@ extern "C" {
  * Every element of dweight (V, D) is written.
  *
  * RNNT_ERR_BAD_SHAPE: B < 1, N < 0, V < 1, D < 1 or start outside [-1, V).
- * RNNT_ERR_UNSUPPORTED: more than 2^31 - 2^16 - 1 rows in the output, or 2^25 or more
- * of V * ceil(D / (64 groups of 16 bytes)) in the gradient.
+ * RNNT_ERR_UNSUPPORTED: more than 2^31 - 2^16 - 1 rows in the output; in the gradient,
+ * 8 rows + V of 2^25 or more per KB of a row.
  */
 typedef struct {
   int32_t B, N, V, D;
@@ -122,6 +122,7 @@ rnnt_status_t rnnt_recurrence_grad(const void* x, const void* z, rnnt_recurrence
  * rng_out (two int64, or NULL) receives the numbers used.  The gradient is the
  * same call on dy with those numbers.  In place (y = x) is allowed.
  * RNNT_ERR_BAD_SHAPE: n < 0.  RNNT_ERR_BAD_VARIANT: p outside [0, 1).
+ * RNNT_ERR_UNSUPPORTED: n of 2^34 - 2^12 or more.
  */
 rnnt_status_t rnnt_dropout(const void* x, int64_t n, rnnt_dtype_t dtype, double p, const int64_t* rng,
                            int64_t* rng_out, void* y, hipStream_t stream);
@@ -141,6 +142,8 @@ rnnt_status_t rnnt_dropout(const void* x, int64_t n, rnnt_dtype_t dtype, double 
  * logit_lens outside [0, T_max] or label_lens outside [0, U_max] is a bad length.
  * RNNT_ERR_BAD_SHAPE: B < 1, T_max < 1, U_max < 0, H < 1 (or 2^31 or more rows of
  * an utterance).  RNNT_ERR_BAD_VARIANT: unknown activation, p outside [0, 1).
+ * RNNT_ERR_UNSUPPORTED: B * T_max or B * (U_max+1) of about 2^23 or more, or 2^29 or
+ * more elements of an utterance's pred.
  */
 typedef enum { RNNT_ACT_RELU = 0, RNNT_ACT_TANH = 1 } rnnt_activation_t;
 

@@ -8,15 +8,19 @@
 namespace rnnt {
 namespace {
 
-// A block takes a tile of channels of one sequence and goes over its steps kTileSteps at a time, kSteps of them to
-// a wave: a wave scans its steps from a zero state and multiplies their gates up, the waves' (product, state) pairs
+// A block of W waves takes a tile of channels of one sequence and goes over its steps W * kSteps at a time, kSteps of
+// them to a wave: a wave scans its steps from a zero state and multiplies their gates up, the waves' (product, state) pairs
 // meet in LDS, and every wave adds the state that arrives at its first step, h_j = S_j + P_j h_in.  x and z are
 // read once, the next tile's while this one is computed.
 // Where sequences and channel tiles are too few to fill the chip, the steps are cut into segments: a first kernel
 // finds each segment's pair, the second one begins each block at the state that the pairs before it give.
+// Bound by the bytes of x, z and h, twice x and z in segments (L=60013 D=640 bf16, one sequence: 27 us at 5.6 TB/s for
+// the pairs, 47 us at 4.9 TB/s for the states).  One pass in which a block waits for the blocks before it would read
+// them once; not built: 469 tiles of that sequence, about a hundred of them on the chip at a time, would each look back
+// over those through the memory-side cache, an estimated 6 to 12 us a tile, which is what the second read costs.
 constexpr int kSteps = RNNT_RECURRENCE_STATE_STEPS;
-constexpr int kWaves = 16;
-constexpr int kTileSteps = kSteps * kWaves;
+constexpr int kWaves = 16;                     // of a block where sequences are few: as many as it can have
+constexpr int kTileSteps = kSteps * kWaves;    // segments are multiples of it
 
 struct RecurrenceParams {
   const void *x, *z;
@@ -65,7 +69,7 @@ struct Rows {
 };
 
 // rows t + j of an output of D channels, those from `end` on left out (an offset past the buffer)
-template <typename T, int VEC>
+template <typename T, int VEC, int W>
 struct RowStore {
   __amdgpu_buffer_rsrc_t r;
   int left;   // steps from the buffer's first row to the end of the segment
@@ -73,7 +77,7 @@ struct RowStore {
 
   // base: row `first` of a dense output, of which `left` steps belong to the segment
   __device__ __forceinline__ RowStore(T* base, int64_t first, int left_, int D_, int c_)
-      : r(make_buffer(base + first * D_, static_cast<int64_t>(min(left_, kTileSteps)) * D_ * static_cast<int64_t>(sizeof(T)))),
+      : r(make_buffer(base + first * D_, static_cast<int64_t>(min(left_, W * kSteps)) * D_ * static_cast<int64_t>(sizeof(T)))),
         left(left_), D(D_), c(c_) {}
   __device__ __forceinline__ void put(int row, const float* f) const {
     Pack<T, VEC> k;
@@ -87,9 +91,9 @@ struct RowStore {
 };
 
 // The (product, state) pairs of a block's waves, two sets of them in turn.
-template <int VEC>
+template <int VEC, int W>
 struct PairBoard {
-  float2 at[2][kWaves][VEC][64];
+  float2 at[2][W][VEC][64];
 
   __device__ __forceinline__ void put(int set, int wave, int lane, const float* A, const float* S) {
 #pragma unroll
@@ -99,8 +103,8 @@ struct PairBoard {
   template <bool BACK>
   __device__ __forceinline__ void compose(int set, int wave, int lane, float* carry, float* mine) const {
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      const int w = BACK ? kWaves - 1 - i : i;
+    for (int i = 0; i < W; ++i) {
+      const int w = BACK ? W - 1 - i : i;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         const float2 k = at[set][w][v][lane];
@@ -112,12 +116,12 @@ struct PairBoard {
 };
 
 // carry through the pairs of the segments before (BACK: behind) a block's, the waves a stretch each
-template <int VEC, bool BACK>
-__device__ __forceinline__ void carry_in(const RecurrenceParams& p, const Place& at, int c, int wave, int lane, PairBoard<VEC>& board,
-                                         float* carry) {
+template <int VEC, bool BACK, int W>
+__device__ __forceinline__ void carry_in(const RecurrenceParams& p, const Place& at, int c, int wave, int lane,
+                                         PairBoard<VEC, W>& board, float* carry) {
   const int n = BACK ? p.segments - 1 - at.segment : at.segment;
   if (n == 0) return;
-  const int share = (n + kWaves - 1) / kWaves, from = min(wave * share, n), to = min(from + share, n);
+  const int share = (n + W - 1) / W, from = min(wave * share, n), to = min(from + share, n);
   const float2* pairs = p.pairs + (static_cast<int64_t>(at.b) * p.segments + (BACK ? at.segment + 1 : 0)) * p.D + c;
   float A[VEC], S[VEC];
 #pragma unroll
@@ -141,9 +145,10 @@ __device__ __forceinline__ void carry_in(const RecurrenceParams& p, const Place&
   board.template compose<BACK>(1, wave, lane, carry, none);
 }
 
-template <typename T, int VEC>
-__global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p) {
-  __shared__ PairBoard<VEC> board;
+template <typename T, int VEC, int W>
+__global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
+  constexpr int TILE = W * kSteps;
+  __shared__ PairBoard<VEC, W> board;
   const Place at(p);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
   const int c = min((at.tile * 64 + lane) * VEC, p.D - VEC);
@@ -151,7 +156,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p
   float carry[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = at.bad ? __builtin_nanf("") : p.h0 ? p.h0[bc + v] : 0.f;
-  carry_in<VEC, false>(p, at, c, wave, lane, board, carry);
+  carry_in<VEC, false, W>(p, at, c, wave, lane, board, carry);
   T* h = static_cast<T*>(p.h);
   const int64_t row0 = static_cast<int64_t>(at.b) * p.L;
   int t0 = at.begin;
@@ -161,7 +166,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p
     Rows<T, VEC> xs, zs;
     xs.load(x, p.x_st, t0 + wave * kSteps, at.len, c);
     zs.load(z, p.z_st, t0 + wave * kSteps, at.len, c);
-    for (int set = 0; t0 < min(at.end, at.len); t0 += kTileSteps, set ^= 1) {
+    for (int set = 0; t0 < min(at.end, at.len); t0 += TILE, set ^= 1) {
       const int t = t0 + wave * kSteps, live = at.len - t;
       float S[kSteps][VEC], P[kSteps][VEC], s[VEC], q[VEC];
 #pragma unroll
@@ -191,8 +196,8 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p
       if (whole) scan(std::true_type{});
       else scan(std::false_type{});
       // the next tile's rows, on their way during the rest
-      xs.load(x, p.x_st, t + kTileSteps, at.len, c);
-      zs.load(z, p.z_st, t + kTileSteps, at.len, c);
+      xs.load(x, p.x_st, t + TILE, at.len, c);
+      zs.load(z, p.z_st, t + TILE, at.len, c);
       board.put(set, wave, lane, q, s);
       __syncthreads();  // one to a tile: the other set is written before the next
       float in[VEC];
@@ -202,7 +207,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p
         k.set(in);
         k.store(p.states + (static_cast<int64_t>(at.b) * p.n_states + t / kSteps) * p.D + c);
       }
-      const RowStore<T, VEC> out(h, row0 + t0, at.end - t0, p.D, c);
+      const RowStore<T, VEC, W> out(h, row0 + t0, at.end - t0, p.D, c);
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {
         float f[VEC];
@@ -212,8 +217,8 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p
       }
     }
   }
-  for (; t0 < at.end; t0 += kTileSteps) {  // behind the sequence
-    const RowStore<T, VEC> out(h, row0 + t0, at.end - t0, p.D, c);
+  for (; t0 < at.end; t0 += TILE) {  // behind the sequence
+    const RowStore<T, VEC, W> out(h, row0 + t0, at.end - t0, p.D, c);
     float f[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) f[v] = at.bad ? __builtin_nanf("") : 0.f;
@@ -226,11 +231,57 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence(RecurrenceParams p
   }
 }
 
+// At most kSteps steps (one, for a streaming decoder): a thread to VEC channels, step by step, nothing to exchange.
+// 16 sequences of 640 float32 channels: one step 2.0 us and eight 3.3, where the tiles of sixteen waves take 5.9.
+template <typename T, int VEC>
+__global__ __launch_bounds__(64) void net_recurrence_short(RecurrenceParams p) {
+  const int b = static_cast<int>(blockIdx.x) / p.tiles, tile = static_cast<int>(blockIdx.x) % p.tiles;
+  const int c = min((tile * 64 + static_cast<int>(threadIdx.x)) * VEC, p.D - VEC);
+  int len = p.lens ? p.lens[b] : p.L;
+  const bool bad = len < 0 || len > p.L;
+  if (bad) len = 0;
+  const int64_t bc = static_cast<int64_t>(b) * p.D + c;
+  float s[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) s[v] = bad ? __builtin_nanf("") : p.h0 ? p.h0[bc + v] : 0.f;
+  if (p.states && p.L > 0) {
+    Pack<float, VEC> k;
+    k.set(s);
+    k.store(p.states + static_cast<int64_t>(b) * p.n_states * p.D + c);
+  }
+  const T* x = static_cast<const T*>(p.x) + b * p.x_sb + c;
+  const T* z = static_cast<const T*>(p.z) + b * p.z_sb + c;
+  T* h = static_cast<T*>(p.h) + static_cast<int64_t>(b) * p.L * p.D + c;
+  for (int t = 0; t < p.L; ++t) {
+    Pack<T, VEC> k;
+    float f[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) f[v] = bad ? s[v] : 0.f;
+    if (t < len) {
+      float xf[VEC], zf[VEC];
+      k.load(x + t * p.x_st);
+      k.get(xf);
+      k.load(z + t * p.z_st);
+      k.get(zf);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        float a, g;
+        gate<T>(zf[v], a, g);
+        f[v] = s[v] = __builtin_fmaf(g, xf[v] - s[v], s[v]);
+      }
+    }
+    k.set(f);
+    k.store(h + static_cast<int64_t>(t) * p.D);
+  }
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) p.last[bc + v] = s[v];
+}
+
 // A segment's pair: forward (BACK false) of h, backward of the gradient's sums.  A wave streams a stretch of its
 // steps; nothing is exchanged before the end.
 template <typename T, int VEC, bool BACK>
 __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrenceParams p) {
-  __shared__ PairBoard<VEC> board;
+  __shared__ PairBoard<VEC, kWaves> board;
   const Place at(p);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
   const int c = min((at.tile * 64 + lane) * VEC, p.D - VEC);
@@ -302,9 +353,10 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
 
 // The gradient goes the other way: s_t = dh_t + a_{t+1} s_{t+1}, tile by tile from the end, its carry d = a s.  The
 // states that dz needs are formed again from the one stored before the wave's first step.
-template <typename T, int VEC>
-__global__ __launch_bounds__(64 * kWaves) void net_recurrence_grad(RecurrenceParams p) {
-  __shared__ PairBoard<VEC> board;
+template <typename T, int VEC, int W>
+__global__ __launch_bounds__(64 * W) void net_recurrence_grad(RecurrenceParams p) {
+  constexpr int TILE = W * kSteps;
+  __shared__ PairBoard<VEC, W> board;
   const Place at(p);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6), lane = static_cast<int>(threadIdx.x) & 63;
   const int c = min((at.tile * 64 + lane) * VEC, p.D - VEC);
@@ -313,16 +365,16 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_grad(RecurrencePar
   float carry[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = at.bad || !p.dlast ? 0.f : p.dlast[bc + v];
-  carry_in<VEC, true>(p, at, c, wave, lane, board, carry);
-  const int tiles = (at.end - at.begin + kTileSteps - 1) / kTileSteps;
+  carry_in<VEC, true, W>(p, at, c, wave, lane, board, carry);
+  const int tiles = (at.end - at.begin + TILE - 1) / TILE;
   // tiles that hold steps of the sequence; the ones behind it are zero
-  const int live_tiles = max(0, min(tiles, (at.len - at.begin + kTileSteps - 1) / kTileSteps));
+  const int live_tiles = max(0, min(tiles, (at.len - at.begin + TILE - 1) / TILE));
   float zero[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) zero[v] = 0.f;
   for (int i = live_tiles; i < tiles; ++i) {
-    const int t0 = at.begin + i * kTileSteps;
-    const RowStore<T, VEC> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
+    const int t0 = at.begin + i * TILE;
+    const RowStore<T, VEC, W> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
       ox.put(wave * kSteps + j, zero);
@@ -342,7 +394,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_grad(RecurrencePar
     }
     Pack<float, VEC> st;
     const auto load = [&](int i) {
-      const int t = at.begin + i * kTileSteps + wave * kSteps;
+      const int t = at.begin + i * TILE + wave * kSteps;
       xs.load(x, p.x_st, t, at.len, c);
       zs.load(z, p.z_st, t, at.len, c);
       if (with_dh) ds.load(dh, p.D, t, at.len, c);
@@ -350,7 +402,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_grad(RecurrencePar
     };
     load(live_tiles - 1);
     for (int i = live_tiles - 1, set = 0; i >= 0; --i, set ^= 1) {
-      const int t0 = at.begin + i * kTileSteps, live = at.len - t0 - wave * kSteps;
+      const int t0 = at.begin + i * TILE, live = at.len - t0 - wave * kSteps;
       const bool whole = live >= kSteps;
       float a[kSteps][VEC], g[kSteps][VEC], w[kSteps][VEC], s[VEC], A[VEC], S[VEC];
       st.get(s);
@@ -389,7 +441,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_grad(RecurrencePar
       __syncthreads();  // one to a tile: the other set is written before the next
       float in[VEC];
       board.template compose<true>(set, wave, lane, carry, in);
-      const RowStore<T, VEC> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
+      const RowStore<T, VEC, W> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
 #pragma unroll
       for (int j = kSteps - 1; j >= 0; --j) {
         float df[VEC], fx[VEC], fz[VEC];
@@ -446,6 +498,17 @@ size_t pair_bytes(const rnnt_recurrence_shape_t& s) {
   RecurrenceParams p{};
   segments_of(s, &p);
   return p.segments > 1 ? net_align256(static_cast<size_t>(s.B) * p.segments * s.D * sizeof(float2)) : 0;
+}
+
+// Waves of a block: sixteen while channel tiles are few, then four or one, no more than the steps have use for
+// (forward, sixteen waves and these: B=8 L=20 D=640 bf16 6.9 and 5.2 us, B=64 L=81 D=1024 bf16 14.5 and 9.8,
+// B=600 L=60 D=512 bf16 59 and 24, B=256 L=81 D=1024 f32 78 and 41, 6.3 TB/s).
+template <typename F>
+rnnt_status_t with_waves(const RecurrenceParams& p, F&& f) {
+  const int64_t blocks = static_cast<int64_t>(p.B) * p.tiles * p.segments;
+  if (blocks >= 2048) return f(std::integral_constant<int, 1>{});
+  if (blocks >= 512 || p.L <= 4 * kSteps) return f(std::integral_constant<int, 4>{});
+  return f(std::integral_constant<int, kWaves>{});
 }
 
 template <typename F>
@@ -511,12 +574,19 @@ rnnt_status_t rnnt_recurrence(const void* x, const void* z, rnnt_recurrence_shap
   return with_vector(shape, [&](auto t, auto vec) {
     using T = decltype(t);
     constexpr int VEC = decltype(vec)::value;
+    if (p.L <= kSteps) {
+      hipLaunchKernelGGL((net_recurrence_short<T, VEC>), grid, dim3(64), 0, stream, p);
+      return launched();
+    }
     if (p.segments > 1) {
       hipLaunchKernelGGL((net_recurrence_pairs<T, VEC, false>), grid, dim3(64 * kWaves), 0, stream, p);
       if (launched() != RNNT_OK) return RNNT_ERR_HIP;
     }
-    hipLaunchKernelGGL((net_recurrence<T, VEC>), grid, dim3(64 * kWaves), 0, stream, p);
-    return launched();
+    return with_waves(p, [&](auto w) {
+      constexpr int W = decltype(w)::value;
+      hipLaunchKernelGGL((net_recurrence<T, VEC, W>), grid, dim3(64 * W), 0, stream, p);
+      return launched();
+    });
   });
 }
 
@@ -548,8 +618,11 @@ rnnt_status_t rnnt_recurrence_grad(const void* x, const void* z, rnnt_recurrence
       hipLaunchKernelGGL((net_recurrence_pairs<T, VEC, true>), grid, dim3(64 * kWaves), 0, stream, p);
       if (launched() != RNNT_OK) return RNNT_ERR_HIP;
     }
-    hipLaunchKernelGGL((net_recurrence_grad<T, VEC>), grid, dim3(64 * kWaves), 0, stream, p);
-    return launched();
+    return with_waves(p, [&](auto w) {
+      constexpr int W = decltype(w)::value;
+      hipLaunchKernelGGL((net_recurrence_grad<T, VEC, W>), grid, dim3(64 * W), 0, stream, p);
+      return launched();
+    });
   });
 }
 

@@ -61,7 +61,8 @@ def close(got, want, tol, what):
 EMBEDDING = [  # B, N, V, D, lengths, start
     (1, 1, 1, 1, None, None), (2, 5, 7, 3, "any", 0), (3, 0, 4, 8, "any", 2), (16, 1, 40, 64, None, None),
     (4, 33, 29, 640, "any", 28), (5, 70, 300, 127, "any", 0), (2, 300, 3, 48, "full", 1), (1, 700, 2, 520, None, None),
-    (7, 20, 5000, 16, "any", 4999), (3, 11, 17, 1032, "zero", 5)]
+    (7, 20, 5000, 16, "any", 4999), (3, 11, 17, 1032, "zero", 5), (2, 0, 5, 16, None, None), (1, 40, 9, 1, "any", 3),
+    (3, 64, 1, 9, "any", 0), (2, 31, 600, 257, "full", None)]
 
 
 def embedding_case(B, N, V, D, lengths, seed):
@@ -145,7 +146,9 @@ RECURRENCE = [  # B, L, D, lengths, h0, layout
     (3, 17, 65, "any", True, "dense"), (2, 81, 40, "any", False, "halves"), (4, 16, 128, "full", True, "halves"),
     (1, 333, 130, None, True, "dense"), (5, 64, 8, "any", True, "steps first"), (2, 700, 7, "any", True, "halves"),
     (3, 250, 264, "any", False, "dense"), (2, 33, 96, "zero", True, "dense"), (2, 0, 6, None, True, "dense"),
-    (1, 2900, 24, "any", True, "dense"), (1, 5200, 136, None, True, "halves")]
+    (1, 2900, 24, "any", True, "dense"), (1, 5200, 136, None, True, "halves"), (3, 7, 66, "any", True, "dense"),
+    (5, 8, 129, "any", False, "halves"), (2, 9, 130, "any", True, "dense"), (3, 128, 2, "any", True, "dense"),
+    (2, 129, 1, "any", True, "dense"), (4, 600, 200, "zero", True, "dense"), (2, 1025, 65, "full", True, "steps first")]
 
 
 def recurrence_case(torch, B, L, D, lengths, with_h0, layout, dtype, seed):  # noqa: F811
@@ -423,6 +426,43 @@ def test_joint_of_tensors_off_16_bytes(torch, pkg, dtype):  # noqa: F811
     denc, dpred = torch.autograd.grad(h, (e, q), shifted(dh))
     for got, w, size in ((denc, wenc, senc), (dpred, wpred, spred)):
         close(got, w, HALF[dtype] * np.abs(w) + (2.0 ** -19 + 8 * ONE) * size, "grad")
+
+
+def test_joint_of_many_utterances(torch, pkg):  # noqa: F811
+    """More utterances than are put in order of their units, and fewer with equal lengths."""
+    for B in (64, 65, 150):
+        enc, pred, dh, encd, predd, dhd, tl, ul = joint_case(torch, B, 3, 4, 16, "any", "f32", B)
+        enc.requires_grad_(True)
+        pred.requires_grad_(True)
+        h = pkg.joint_hidden(enc, pred, ints(torch, tl), ints(torch, ul))
+        _, wenc, wpred, senc, spred = R.joint_hidden(encd, predd, tl, ul, "relu", dh=dhd)
+        for got, w, size in zip(torch.autograd.grad(h, (enc, pred), dh), (wenc, wpred), (senc, spred)):
+            close(got, w, 10 * ONE * size, "grad")
+
+
+def test_recurrence_of_many_sequences(torch, pkg):  # noqa: F811
+    """Enough channel tiles for blocks of four waves and of one, over several tiles of steps; the sequences of a
+    few, repeated, give the same bits."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for dtype, D in (("f32", 130), ("bf16", 264)):
+        x, z, dh = (torch.randn((4, 75, D), device="cuda", generator=g).to(td(torch, dtype)) for _ in range(3))
+        lens = ints(torch, [75, 74, 33, 0])
+
+        def both(n):
+            a, b = (t.repeat(n, 1, 1).requires_grad_(True) for t in (x, z))
+            h, last = pkg.gated_recurrence(a, b, None, lens.repeat(n))
+            return (h.detach(), last.detach()) + torch.autograd.grad(h, (a, b), dh.repeat(n, 1, 1))
+        few = both(1)
+        e = recurrence_bounds(*(t.double().cpu().numpy() for t in (x, z)), None, lens.cpu().numpy(), dh.double().cpu().numpy(),
+                              np.zeros((4, D)))
+        for n in (60, 400):
+            many = both(n)
+            for name, a, b in zip(("h", "last", "dx", "dz"), few, many):
+                b = b.view((n,) + a.shape)
+                assert torch.equal(b[0], b[-1])
+                want = a.double().cpu().numpy()
+                # two orders of one sum
+                close(b[0], want, 2 * e[name] + 2 * HALF[dtype if name != "last" else "f32"] * np.abs(want) + 2.0 ** -120, name)
 
 
 def test_joint_past_32_bits(torch, pkg):  # noqa: F811
