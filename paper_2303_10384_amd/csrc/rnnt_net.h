@@ -212,21 +212,21 @@ struct Activation<RNNT_ACT_RELU> {
   __device__ static __forceinline__ float slope(float s) { return s > 0.f ? 1.f : 0.f; }
 };
 
-// tanh s = (1 - u) / (1 + u) and 4u / (1 + u)^2 with u = e^-2|s|; below 0.3, where 1 - u
-// loses digits, the odd series through s^9 (the next term is 5e-8 of the value there).  The
-// rounding of the exponent, 2|s| 2^-24 of u, needs no correction: where it grows, u is small
-// in the value, and in the slope it is what the rounding of s itself costs.
+// tanh s = 1 - 2 / (1 + e^2s), which ends at -1 and 1 whatever overflows; below 0.3, where the
+// difference loses digits, the odd series through s^9 (the next term is 5e-8 of the value there).  Its slope
+// is 4u / (1 + u)^2 with u = e^-2|s|.  The rounding of the exponent, 2|s| 2^-24 of the exponential, needs no
+// correction: where it grows, little of the value is left to it, and in the slope it is what the rounding of s
+// itself costs.
 template <>
 struct Activation<RNNT_ACT_TANH> {
   __device__ static __forceinline__ float u_of(float s) { return fast_exp2(__builtin_fabsf(s) * (-2.f * kLog2eF)); }
   __device__ static __forceinline__ float value(float s) {
-    const float y = __builtin_fabsf(s), q = s * s;
-    const float u = u_of(s);
-    const float big = __builtin_copysignf((1.f - u) * __builtin_amdgcn_rcpf(1.f + u), s);
+    const float q = s * s;
+    const float big = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * (2.f * kLog2eF))), 1.f);
     float p = __builtin_fmaf(q, 62.f / 2835.f, -17.f / 315.f);
     p = __builtin_fmaf(q, p, 2.f / 15.f);
     p = __builtin_fmaf(q, p, -1.f / 3.f);
-    return y < 0.3f ? __builtin_fmaf(q * p, s, s) : big;
+    return __builtin_fabsf(s) < 0.3f ? __builtin_fmaf(q * p, s, s) : big;
   }
   __device__ static __forceinline__ float slope(float s) {
     const float u = u_of(s), r = __builtin_amdgcn_rcpf(1.f + u);

@@ -70,12 +70,11 @@ constexpr int kJointRun = 8;       // groups of eight elements to a thread and f
 constexpr int kJointLdsBytes = 64000;  // rows that net_joint_odd keeps in LDS
 
 template <typename T, int ACT>
-__device__ __forceinline__ void joint_group(const float* e, const float* q, float scale, const Dropped& drop, Pack<T, 8>& out) {
+__device__ __forceinline__ void joint_group(const float* e, const float* q, float scale, Pack<T, 8>& out) {
   float f[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = Activation<ACT>::value(e[i] + q[i]) * scale;
   out.set(f);
-  drop.clear(out);
 }
 
 // Elements of a run valid at frame t (-1: a bad length).
@@ -96,7 +95,7 @@ __device__ __forceinline__ Pack<T, 8> nan_group() {
 }
 
 // H a multiple of eight: groups lie in one row, and at the same place of the run for every frame.
-template <typename T, int ACT>
+template <typename T, int ACT, bool DROP>
 __global__ __launch_bounds__(256) void net_joint(JointParams p) {
   copy_rng(p.drop.rng, p.rng_out);
   const int b = static_cast<int>(blockIdx.x) / p.t_blocks, t0 = static_cast<int>(blockIdx.x) % p.t_blocks * p.block_frames;
@@ -109,7 +108,7 @@ __global__ __launch_bounds__(256) void net_joint(JointParams p) {
   const int tl = valid0 < 0 ? 0 : p.logit_lens[b];
   const int64_t valid = valid0 < 0 ? 0 : static_cast<int64_t>(p.label_lens[b] + 1) * p.H;
   Rng rng{};
-  if (p.drop.threshold) rng = load_rng(p.drop.rng);
+  if constexpr (DROP) rng = load_rng(p.drop.rng);
   const T* enc = static_cast<const T*>(p.enc) + (static_cast<int64_t>(b) * p.T + t0) * p.H;
   const T* pred = static_cast<const T*>(p.pred) + b * total;
   const int64_t run0 = (static_cast<int64_t>(b) * p.T + t0) * total;
@@ -130,9 +129,12 @@ __global__ __launch_bounds__(256) void net_joint(JointParams p) {
           float e[8];
           k.load(enc + i * p.H + col);
           k.get(e);
-          Dropped drop;
-          dropped_of(p.drop, rng, static_cast<uint64_t>(run0 + i * total + j) >> 3, drop);
-          joint_group<T, ACT>(e, q, p.drop.scale, drop, k);
+          joint_group<T, ACT>(e, q, p.drop.scale, k);
+          if constexpr (DROP) {
+            Dropped drop;
+            drop.below(random_block(rng, static_cast<uint64_t>(run0 + i * total + j) >> 3), p.drop.threshold);
+            drop.clear(k);
+          }
         } else {
           k.zero();
         }
@@ -215,7 +217,8 @@ __global__ __launch_bounds__(256) void net_joint_odd(JointParams p) {
           }
           Dropped drop;
           dropped_of(p.drop, rng, static_cast<uint64_t>(run0 + j) >> 3, drop);
-          joint_group<T, ACT>(e, q, p.drop.scale, drop, k);
+          joint_group<T, ACT>(e, q, p.drop.scale, k);
+          drop.clear(k);
           if (j + 8 > valid) {  // the valid rows end inside the group
 #pragma unroll
             for (int q8 = 0; q8 < 8; ++q8) {
@@ -668,7 +671,8 @@ rnnt_status_t rnnt_joint_hidden(const void* enc, const void* pred, rnnt_joint_sh
     return with_activation(act, [&](auto a) {
       using T = decltype(t);
       constexpr int A = decltype(a)::value;
-      if (eights) hipLaunchKernelGGL((net_joint<T, A>), grid, dim3(256), 0, stream, q);
+      if (eights && q.drop.threshold) hipLaunchKernelGGL((net_joint<T, A, true>), grid, dim3(256), 0, stream, q);
+      else if (eights) hipLaunchKernelGGL((net_joint<T, A, false>), grid, dim3(256), 0, stream, q);
       else if (lds <= kJointLdsBytes) hipLaunchKernelGGL((net_joint_odd<T, A, true>), grid, dim3(256), static_cast<size_t>(lds), stream, q);
       else hipLaunchKernelGGL((net_joint_odd<T, A, false>), grid, dim3(256), 0, stream, q);
       return launched();
