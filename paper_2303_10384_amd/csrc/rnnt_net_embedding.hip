@@ -88,6 +88,7 @@ constexpr int kSortTokens = 384;   // most tokens of a sorting block (a thread t
 constexpr int kSortFound = 384;    // rows that a wave keeps
 constexpr int kSortBlocks = 256;   // one to a CU, each looks at every row
 constexpr int kRun = 32;
+constexpr int kRowsToWave = 4;
 constexpr int kManyRuns = 32;  // a token of more runs is added up by four waves
 
 struct EmbeddingGradParams {
@@ -306,7 +307,7 @@ __device__ __forceinline__ void add_runs(const EmbeddingGradParams& p, int64_t r
   }
 }
 
-// What the runs left: a wave to a weight row and a tile, for the rows that no token has and the tokens of several
+// What the runs left: a wave to kRowsToWave weight rows and a tile, for the rows that no token has and the tokens of several
 // runs; behind them a block to every run in which a token of more than kManyRuns begins.
 template <typename T, int VEC>
 __global__ __launch_bounds__(256) void net_embedding_rows(EmbeddingGradParams p, int32_t row_blocks) {
@@ -329,16 +330,22 @@ __global__ __launch_bounds__(256) void net_embedding_rows(EmbeddingGradParams p,
   };
   if (static_cast<int>(blockIdx.x) < row_blocks) {
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-    const int64_t v = item / p.tiles;
-    if (v >= p.src.V) return;
-    const int from = p.first[v], to = p.first[v + 1], c = group_start(static_cast<int>(item - v * p.tiles) * 64 + lane, VEC, p.D);
-    if (from < to) {
-      const int r0 = from / kRun, more = (to - 1) / kRun - r0;
-      if (more == 0 || more > kManyRuns) return;
-      begin_sums(r0, c);
-      add_runs<VEC>(p, r0, 0, more, c, sum);
+    const int64_t v0 = item / p.tiles * kRowsToWave;
+    if (v0 >= p.src.V) return;
+    const int c = group_start(static_cast<int>(item % p.tiles) * 64 + lane, VEC, p.D);
+    const int bounds = p.first[min(v0 + lane, static_cast<int64_t>(p.src.V))];  // lanes 0 .. kRowsToWave: where the rows begin
+    for (int i = 0; i < kRowsToWave && v0 + i < p.src.V; ++i) {
+      const int from = __builtin_amdgcn_readlane(bounds, i), to = __builtin_amdgcn_readlane(bounds, i + 1);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) sum[j] = 0.f;
+      if (from < to) {
+        const int r0 = from / kRun, more = (to - 1) / kRun - r0;
+        if (more == 0 || more > kManyRuns) continue;
+        begin_sums(r0, c);
+        add_runs<VEC>(p, r0, 0, more, c, sum);
+      }
+      finish(v0 + i, c);
     }
-    finish(v, c);
     return;
   }
   const int64_t item = static_cast<int64_t>(blockIdx.x) - row_blocks, r0 = item / p.tiles;
@@ -489,7 +496,7 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
       const int groups = (shape.D + VEC - 1) / VEC;
       p.tiles = (groups + 63) / 64;
       const int64_t run_items = static_cast<int64_t>(p.runs) * p.tiles;
-      const int64_t row_blocks = (static_cast<int64_t>(shape.V) * p.tiles + 3) / 4;
+      const int64_t row_waves = (static_cast<int64_t>(shape.V) + kRowsToWave - 1) / kRowsToWave * p.tiles, row_blocks = (row_waves + 3) / 4;
       if (row_blocks + run_items > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
       if (run_items > 0) {
         hipLaunchKernelGGL((net_embedding_runs<T, VEC>), dim3(static_cast<uint32_t>((run_items + 3) / 4)), dim3(256), 0, stream, p);

@@ -11,7 +11,9 @@ A streaming decoder takes the same calls one step at a time: labels (B, 1), x an
 with h0 the state before, enc (B, 1, H) against pred (B, 1, H).
 
 Every tensor of a call is on one GPU, which need not be the current one; work is queued on
-that GPU's current stream.  A gradient of a gradient is not offered.
+that GPU's current stream.  A gradient of a gradient is not offered.  Calls may be captured
+into a graph, backward passes too (as with any operation, while no eager graph of the same
+leaves is alive); a captured loss call brings its workspace.
 """
 import ctypes
 import functools
