@@ -62,7 +62,7 @@ EMBEDDING = [  # B, N, V, D, lengths, start
     (1, 1, 1, 1, None, None), (2, 5, 7, 3, "any", 0), (3, 0, 4, 8, "any", 2), (16, 1, 40, 64, None, None),
     (4, 33, 29, 640, "any", 28), (5, 70, 300, 127, "any", 0), (2, 300, 3, 48, "full", 1), (1, 700, 2, 520, None, None),
     (7, 20, 5000, 16, "any", 4999), (3, 11, 17, 1032, "zero", 5), (2, 0, 5, 16, None, None), (1, 40, 9, 1, "any", 3),
-    (3, 64, 1, 9, "any", 0), (2, 31, 600, 257, "full", None)]
+    (3, 64, 1, 9, "any", 0), (2, 31, 600, 257, "full", None), (8, 1000, 1, 8, "full", None), (16, 1000, 2, 12, "any", 1)]
 
 
 def embedding_case(B, N, V, D, lengths, seed):
