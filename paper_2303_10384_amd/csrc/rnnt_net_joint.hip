@@ -658,7 +658,9 @@ rnnt_status_t rnnt_joint_hidden(const void* enc, const void* pred, rnnt_joint_sh
   q.H = shape.H;
   const bool eights = shape.H % 8 == 0;
   const int64_t groups = (static_cast<int64_t>(q.U1) * shape.H + 7) / 8 + (eights ? 0 : 1);
-  // a frame to a block where kJointFrames would leave the chip fewer than eight blocks to a CU
+  // a frame to a block where kJointFrames would leave the chip fewer than eight blocks to a CU (B=16 T=150 U=40, 600
+  // blocks of four frames and 2400 of one: H=320 bf16 tanh 29 and 20 us, f32 34 and 27; B=32 T=250 U=80 H=640 bf16
+  // of full lengths, 8064 blocks of four and 16000 of two: 179 and 211)
   const int64_t y = (groups + 256 * kJointRun - 1) / (256 * kJointRun);
   const int64_t full = (static_cast<int64_t>(shape.T_max) + kJointFrames - 1) / kJointFrames;
   q.block_frames = full * shape.B * y >= 2048 ? kJointFrames : 1;

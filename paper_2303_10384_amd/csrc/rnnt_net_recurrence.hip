@@ -15,7 +15,7 @@ namespace {
 // Where sequences and channel tiles are too few to fill the chip, the steps are cut into segments: a first kernel
 // finds each segment's pair, the second one begins each block at the state that the pairs before it give.
 // Bound by the bytes of x, z and h, twice x and z in segments (L=60013 D=640 bf16, one sequence: 27 us at 5.6 TB/s for
-// the pairs, 47 us at 4.9 TB/s for the states).  One pass in which a block waits for the blocks before it would read
+// the pairs, 41 us at 5.7 TB/s for the states).  One pass in which a block waits for the blocks before it would read
 // them once; not built: 469 tiles of that sequence, about a hundred of them on the chip at a time, would each look back
 // over those through the memory-side cache, an estimated 6 to 12 us a tile, which is what the second read costs.
 constexpr int kSteps = RNNT_RECURRENCE_STATE_STEPS;
@@ -93,11 +93,16 @@ struct RowStore {
 // The (product, state) pairs of a block's waves, two sets of them in turn.
 template <int VEC, int W>
 struct PairBoard {
-  float2 at[2][W][VEC][64];
+  struct __attribute__((aligned(8 * VEC))) Pairs {
+    float2 of[VEC];
+  };
+  Pairs at[2][W][64];
 
   __device__ __forceinline__ void put(int set, int wave, int lane, const float* A, const float* S) {
+    Pairs k;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) at[set][wave][v][lane] = make_float2(A[v], S[v]);
+    for (int v = 0; v < VEC; ++v) k.of[v] = make_float2(A[v], S[v]);
+    at[set][wave][lane] = k;
   }
   // carry through all waves' pairs, in order or backwards; `mine` is what arrives at `wave`
   template <bool BACK>
@@ -105,11 +110,11 @@ struct PairBoard {
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       const int w = BACK ? W - 1 - i : i;
+      const Pairs k = at[set][w][lane];
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const float2 k = at[set][w][v][lane];
         if (w == wave) mine[v] = carry[v];
-        carry[v] = __builtin_fmaf(k.x, carry[v], k.y);
+        carry[v] = __builtin_fmaf(k.of[v].x, carry[v], k.of[v].y);
       }
     }
   }
@@ -174,13 +179,20 @@ __global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
         s[v] = 0.f;
         q[v] = 1.f;
       }
+      // the next tile's rows, on their way while this one is computed
+      const Rows<T, VEC> xn = xs, zn = zs;
+      if (t0 + TILE < min(at.end, at.len)) {
+        xs.load(x, p.x_st, t + TILE, at.len, c);
+        zs.load(z, p.z_st, t + TILE, at.len, c);
+      }
+      __builtin_amdgcn_sched_barrier(0);
       const bool whole = live >= kSteps;
       const auto scan = [&](auto all) {
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
           float xf[VEC], zf[VEC];
-          xs.r[j].get(xf);
-          zs.r[j].get(zf);
+          xn.r[j].get(xf);
+          zn.r[j].get(zf);
 #pragma unroll
           for (int v = 0; v < VEC; ++v) {
             float a, g;
@@ -195,9 +207,6 @@ __global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
       };
       if (whole) scan(std::true_type{});
       else scan(std::false_type{});
-      // the next tile's rows, on their way during the rest
-      xs.load(x, p.x_st, t + TILE, at.len, c);
-      zs.load(z, p.z_st, t + TILE, at.len, c);
       board.put(set, wave, lane, q, s);
       __syncthreads();  // one to a tile: the other set is written before the next
       float in[VEC];
@@ -343,7 +352,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
     float prod = 1.f, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      const float2 k = board.at[0][BACK ? kWaves - 1 - i : i][v][lane];
+      const float2 k = board.at[0][BACK ? kWaves - 1 - i : i][lane].of[v];
       sum = __builtin_fmaf(k.x, sum, k.y);
       prod *= k.x;
     }
@@ -478,14 +487,17 @@ rnnt_status_t check(const rnnt_recurrence_shape_t& s) {
 int state_count(int L) { return static_cast<int>((static_cast<int64_t>(L) + kSteps - 1) / kSteps); }
 
 // Blocks to a sequence: one, or as many segments of at least two tiles as give the chip a block to a CU.
-// Segments read x and z twice (5/3 of the bytes forward, 7/5 backward), which pays below about 3/5 of a chip.
+// Segments read x and z twice (5/3 of the bytes forward, 7/5 backward), which pays up to half a chip of blocks: D=640
+// bf16 L=2000, forward and backward, one block and segments: 20 sequences (100 blocks) 63 + 82 us and 57 + 70,
+// 25 (125) 63 + 92 and 61 + 82, 32 (160) 63 + 102 and 104 + 133 (53 + 96 in one block with the pairs read 16 bytes at
+// a time, which the other figures came before).
 void segments_of(const rnnt_recurrence_shape_t& s, RecurrenceParams* p) {
   const int vec = s.dtype == RNNT_DTYPE_F32 || s.D < 2 ? 1 : 2;
   p->tiles = (s.D + 64 * vec - 1) / (64 * vec);
   const int64_t blocks = static_cast<int64_t>(s.B) * p->tiles, steps = (static_cast<int64_t>(s.L) + kTileSteps - 1) / kTileSteps;
   p->segments = 1;
   p->seg_steps = s.L;
-  if (blocks < 150 && steps >= 4) {
+  if (blocks <= 128 && steps >= 4) {
     int64_t want = 256 / blocks;
     if (want > steps / 2) want = steps / 2;
     const int64_t per = (steps + want - 1) / want;
