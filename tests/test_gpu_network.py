@@ -399,6 +399,31 @@ def test_joint_rows_with_a_short_last_slice(torch, pkg, H, act, dtype):  # noqa:
             close(got, w, HALF[dtype] * np.abs(w) + (2.0 ** -20 + 10 * 2.0 ** -23 + (n + 3) * ONE) * size + TINY[dtype], "grad")
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_joint_relu_mask_of_special_values(torch, pkg, dtype):  # noqa: F811
+    """Which sums are positive: zeros of both signs, subnormals, neighbours, infinities and NaN."""
+    t = td(torch, dtype)
+    if dtype == "f32":
+        v = torch.tensor([0.0, 1e-45, 1.2e-38, 0.5, 1.0, 1.0000001, 3e38, float("inf"), float("nan")])
+    else:
+        one = 0x3f80 if dtype == "bf16" else 0x3c00
+        inf = 0x7f80 if dtype == "bf16" else 0x7c00
+        v = torch.tensor([0, 1, 2, 0x7f, 0x80, 0x400, one - 1, one, one + 1, inf - 1, inf, inf + 1, 0x7fff],
+                         dtype=torch.int16).view(t)
+    v = torch.cat([v, -v]).to("cuda")
+    n = v.numel()
+    for H in (8, 24, 5):
+        enc, pred = (v.view(1, n, 1).expand(1, n, H).contiguous().requires_grad_(True) for _ in range(2))
+        h = pkg.joint_hidden(enc, pred, ints(torch, [n]), ints(torch, [n - 1]))
+        denc, dpred = torch.autograd.grad(h, (enc, pred), torch.ones_like(h))
+        total = v.float()[:, None] + v.float()[None]
+        want = (total > 0).float().sum(1)  # symmetric, and NaN is not positive
+        assert torch.equal(denc[0].float(), want[:, None].expand(n, H)), dtype
+        assert torch.equal(dpred[0].float(), want[:, None].expand(n, H)), dtype
+        relu = torch.where(total < 0, torch.zeros_like(total), total).to(t)
+        assert torch.equal(torch.nan_to_num(h[0, :, :, 0].float(), 7.0), torch.nan_to_num(relu.float(), 7.0))
+
+
 def test_joint_bad_lengths(torch, pkg):  # noqa: F811
     for H in (24, 5):
         enc = torch.ones((5, 6, H), device="cuda", requires_grad=True)
