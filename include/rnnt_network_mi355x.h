@@ -48,8 +48,8 @@ extern "C" {
  * Every element of dweight (V, D) is written.
  *
  * RNNT_ERR_BAD_SHAPE: B < 1, N < 0, V < 1, D < 1 or start outside [-1, V).
- * RNNT_ERR_UNSUPPORTED: more than 2^31 - 2^16 - 1 rows in the output; in the gradient,
- * 8 rows + V of 2^25 or more per KB of a row.
+ * RNNT_ERR_UNSUPPORTED: more than 2^31 - 2^16 - 1 rows in the output, or D > 2^30; in the
+ * gradient, (rows + 2 V) times the KB of a row, rounded up, of about 2^28 or more.
  */
 typedef struct {
   int32_t B, N, V, D;

@@ -391,7 +391,7 @@ rnnt_status_t check(const int32_t* labels, const rnnt_embedding_shape_t& s, Toke
   if (s.B < 1 || s.N < 0 || s.V < 1 || s.D < 1 || s.start < -1 || s.start >= s.V) return RNNT_ERR_BAD_SHAPE;
   if (!net_dtype_known(s.dtype)) return RNNT_ERR_BAD_DTYPE;
   const int64_t n1 = static_cast<int64_t>(s.N) + (s.start >= 0);
-  if (n1 * s.B > kMaxRows - (1 << 16)) return RNNT_ERR_UNSUPPORTED;
+  if (n1 * s.B > kMaxRows - (1 << 16) || s.D > (1 << 30)) return RNNT_ERR_UNSUPPORTED;
   if (!labels && s.N > 0) return RNNT_ERR_NULL_PTR;
   *src = TokenSource{labels, lens, s.B, s.N, static_cast<int32_t>(n1), s.V, s.start};
   return RNNT_OK;
@@ -479,6 +479,13 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   if (!dweight || (!dout && p.rows > 0)) return RNNT_ERR_NULL_PTR;
   const int64_t e = net_elem_bytes(shape.dtype);
   if (!multiple_of(e, dout) || !multiple_of(e, dweight)) return RNNT_ERR_ALIGNMENT;
+  // every grid of the call before its first launch: a wave to a run or to weight rows, times tiles of 64 groups
+  const int wide = static_cast<int>(16 / e), vec = shape.D >= wide ? wide : 1;
+  p.tiles = (shape.D - 1) / (64 * vec) + 1;
+  p.runs = static_cast<int32_t>((static_cast<int64_t>(p.rows) + kRun - 1) / kRun);
+  const int64_t run_items = static_cast<int64_t>(p.runs) * p.tiles;
+  const int64_t row_waves = (static_cast<int64_t>(shape.V) + kRowsToWave - 1) / kRowsToWave * p.tiles, row_blocks = (row_waves + 3) / 4;
+  if (row_blocks + run_items > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
   const GradLayout L = grad_layout(shape, p.rows);
   NetWorkspace ws;
   st = ws.take(workspace, workspace_bytes, L.total, stream);
@@ -492,7 +499,6 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   p.tokens = reinterpret_cast<int32_t*>(ws.ptr + L.tokens);
   p.first = reinterpret_cast<int32_t*>(ws.ptr + L.first);
   p.sums = reinterpret_cast<float*>(ws.ptr + L.sums);
-  p.runs = static_cast<int32_t>((static_cast<int64_t>(p.rows) + kRun - 1) / kRun);
   const int64_t shares = (static_cast<int64_t>(shape.V) + kSortBlocks - 1) / kSortBlocks;
   p.per_block = static_cast<int32_t>(shares < kSortTokens ? shares : kSortTokens);
   const dim3 sort_grid(static_cast<uint32_t>((static_cast<int64_t>(shape.V) + p.per_block - 1) / p.per_block));
@@ -507,13 +513,8 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   if (launched() != RNNT_OK) return RNNT_ERR_HIP;
   return with_dtype(shape.dtype, [&](auto t) {
     using T = decltype(t);
-    const auto rest = [&](auto vec) {
-      constexpr int VEC = decltype(vec)::value;
-      const int groups = (shape.D + VEC - 1) / VEC;
-      p.tiles = (groups + 63) / 64;
-      const int64_t run_items = static_cast<int64_t>(p.runs) * p.tiles;
-      const int64_t row_waves = (static_cast<int64_t>(shape.V) + kRowsToWave - 1) / kRowsToWave * p.tiles, row_blocks = (row_waves + 3) / 4;
-      if (row_blocks + run_items > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
+    const auto rest = [&](auto v) {
+      constexpr int VEC = decltype(v)::value;
       if (run_items > 0) {
         hipLaunchKernelGGL((net_embedding_runs<T, VEC>), dim3(static_cast<uint32_t>((run_items + 3) / 4)), dim3(256), 0, stream, p);
         if (launched() != RNNT_OK) return RNNT_ERR_HIP;
@@ -522,8 +523,7 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
                          static_cast<int32_t>(row_blocks));
       return launched();
     };
-    constexpr int WIDE = 16 / sizeof(T);
-    return shape.D >= WIDE ? rest(std::integral_constant<int, WIDE>{}) : rest(std::integral_constant<int, 1>{});
+    return vec > 1 ? rest(std::integral_constant<int, 16 / sizeof(T)>{}) : rest(std::integral_constant<int, 1>{});
   });
 }
 

@@ -63,6 +63,19 @@ def test_embedding_refusals(net):
         assert call(lib.rnnt_label_embedding_grad, bwd, over) == want
 
 
+def test_embedding_sizes_past_a_launch(net):
+    """Refused before the call's first launch (9), not by it (8)."""
+    lib, S = net._library(), net.EmbeddingShape
+    fwd = {"labels": FAKE, "lens": FAKE, "shape": S(2, 3, 1, 2 ** 31 - 1, 0, 0), "weight": FAKE, "scale": 1.0, "out": FAKE,
+           "stream": None}
+    assert call(lib.rnnt_label_embedding, fwd, {}) == 9
+    bwd = {"labels": FAKE, "lens": FAKE, "shape": None, "dout": FAKE, "scale": 1.0, "dweight": FAKE, "ws": FAKE,
+           "bytes": 1 << 62, "stream": None}
+    for shape in (S(2, 3, 2 ** 31 - 1, 1, 0, 0), S(2, 3, 1 << 27, 4, -1, 1), S(1 << 14, 1 << 15, 2, 1024, -1, 0),
+                  S(2, 3, 1, 2 ** 31 - 1, 0, 2)):
+        assert call(lib.rnnt_label_embedding_grad, bwd, {"shape": shape}) == 9
+
+
 def test_recurrence_refusals(net):
     lib, S = net._library(), net.RecurrenceShape
     assert lib.rnnt_recurrence_workspace_bytes(S(2, 40, 5, 0, 200, 5, 200, 5)) == 0  # one block to a sequence
