@@ -721,7 +721,7 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
   q.slices = cut.slices;
   q.tile_frames = cut.tile_frames;
   const int64_t x = static_cast<int64_t>(shape.B) * q.t_blocks * q.slices;
-  const int64_t joins = (static_cast<int64_t>(shape.B) * q.U1 * ((shape.H + 3) / 4) + 255) / 256;
+  const int64_t joins = (static_cast<int64_t>(shape.B) * q.U1 * (shape.H < 8 ? shape.H : (shape.H + 3) / 4) + 255) / 256;
   // a block's sums are one buffer of less than 2^31 bytes
   if (x > kMaxRows / 256 || joins > kMaxRows / 256 || static_cast<int64_t>(q.U1) * shape.H >= (int64_t{1} << 29))
     return RNNT_ERR_UNSUPPORTED;

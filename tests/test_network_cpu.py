@@ -136,6 +136,15 @@ def test_joint_refusals(net):
         assert call(lib.rnnt_joint_hidden_grad, bwd, over) == want
 
 
+def test_joint_sizes_past_a_launch(net):
+    """Narrow rows (a thread to a channel) of more threads than a launch holds: refused, with nothing launched."""
+    lib, S = net._library(), net.JointShape
+    bwd = {"enc": FAKE, "pred": FAKE, "shape": None, "tl": FAKE, "ul": FAKE, "act": 0, "p": 0.5, "rng": FAKE, "dh": FAKE,
+           "denc": FAKE, "dpred": FAKE, "ws": FAKE, "bytes": 1 << 62, "stream": None}
+    for shape in (S(15, 1, (1 << 26) - 1, 7, 0), S(15, 1, (1 << 26) - 1, 7, 1), S(1 << 24, 16, 0, 3, 0)):
+        assert call(lib.rnnt_joint_hidden_grad, bwd, {"shape": shape}) == 9
+
+
 def test_binding_refuses_cpu_tensors_and_bad_arguments(net):
     import paper_2303_10384_amd as rnnt
     x, lens = torch.zeros(2, 3, 4), torch.ones(2, dtype=torch.int32)
