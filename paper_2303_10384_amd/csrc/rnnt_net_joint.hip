@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256) void net_joint_grad_narrow(JointGradParams p, 
     const bool keep = !p.drop.threshold ||
                       random16(random_block(rng, static_cast<uint64_t>(n >> 3)), static_cast<int>(n & 7)) >= p.drop.threshold;
     const float w = ACT == RNNT_ACT_RELU ? Activation<ACT>::slope(s) : 0.25f * Activation<ACT>::slope(s);
-    if (keep && w != 0.f) sum += ElemTraits<T>::load1(static_cast<const T*>(p.dh) + n) * w;
+    if (keep && (ACT == RNNT_ACT_TANH || w != 0.f)) sum += ElemTraits<T>::load1(static_cast<const T*>(p.dh) + n) * w;
   }
   ElemTraits<T>::store1(static_cast<T*>(of_enc ? p.denc : p.dpred) + at, sum * p.factor);
 }

@@ -424,6 +424,18 @@ def test_joint_relu_mask_of_special_values(torch, pkg, dtype):  # noqa: F811
         assert torch.equal(torch.nan_to_num(h[0, :, :, 0].float(), 7.0), torch.nan_to_num(relu.float(), 7.0))
 
 
+@pytest.mark.parametrize("H", [5, 8, 20])
+@pytest.mark.parametrize("act", ["relu", "tanh"])
+def test_joint_infinite_upstream_where_the_slope_is_zero(torch, pkg, act, H):  # noqa: F811
+    """relu leaves such an element out (its sum is not positive), tanh multiplies by its 0, whatever the width."""
+    at = -1.0 if act == "relu" else 60.0
+    enc, pred = (torch.full((1, n, H), at, device="cuda", requires_grad=True) for n in (3, 2))
+    h = pkg.joint_hidden(enc, pred, ints(torch, [3]), ints(torch, [1]), act)
+    dh = torch.full_like(h, float("inf"))
+    for g in torch.autograd.grad(h, (enc, pred), dh):
+        assert bool((g == 0).all()) if act == "relu" else bool(g.isnan().all())
+
+
 def test_joint_bad_lengths(torch, pkg):  # noqa: F811
     for H in (24, 5):
         enc = torch.ones((5, 6, H), device="cuda", requires_grad=True)
