@@ -111,6 +111,11 @@ def _check_p(p):
     return p
 
 
+def _dense(*saved):
+    """Saved tensors as the kernels take them: hooks on saved tensors may give any layout back."""
+    return (None if t is None else t.contiguous() for t in saved)
+
+
 def _result(shape, dtype, device, nbytes):
     """A result tensor and the workspace of the call that fills it, or None.
 
@@ -150,7 +155,7 @@ class _LabelEmbedding(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        labels, lens = ctx.saved_tensors
+        labels, lens = _dense(*ctx.saved_tensors)
         (shape, nbytes), dout = ctx.shape, dout.contiguous()
         dw, ws = _result((shape.V, shape.D), dout.dtype, dout.device, nbytes)
         _call(_library().rnnt_label_embedding_grad, dout.device, _ptr(labels), _ptr(lens), shape, _ptr(dout), ctx.scale,
@@ -183,24 +188,32 @@ def label_embedding(labels, weight, lens=None, scale=1.0, start=None):
 
 # ---------------------------------------------------------------- gated recurrence
 
+def _contiguous_channels(t):
+    return t.numel() == 0 or t.shape[2] == 1 or t.stride(2) == 1
+
+
+def _recurrence_shape(x, z):
+    return _shape(RecurrenceShape, "rnnt_recurrence_workspace_bytes", *x.shape, dtype_code(x.dtype), *x.stride()[:2],
+                  *z.stride()[:2])
+
+
 def _recurrence_forward(x, z, h0, lens, with_states):
     B, L, D = x.shape
     dev = x.device
-    shape, nbytes = both = _shape(RecurrenceShape, "rnnt_recurrence_workspace_bytes", B, L, D, dtype_code(x.dtype),
-                                  *x.stride()[:2], *z.stride()[:2])
+    shape, nbytes = _recurrence_shape(x, z)
     h, ws = _result((B, L, D), x.dtype, dev, nbytes)
     last = torch.empty((B, D), dtype=torch.float32, device=dev)
     states = torch.empty((B, -(-L // STATE_STEPS), D), dtype=torch.float32, device=dev) if with_states else None
     _call(_library().rnnt_recurrence, dev, _ptr(x), _ptr(z), shape, _ptr(lens), _ptr(h0), _ptr(h), _ptr(last), _ptr(states),
           *_workspace_args(ws))
-    return h, last, states, both
+    return h, last, states
 
 
 class _GatedRecurrence(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, z, h0, lens):
         ctx.set_materialize_grads(False)
-        h, last, states, ctx.shape = _recurrence_forward(x, z, h0, lens, True)
+        h, last, states = _recurrence_forward(x, z, h0, lens, True)
         ctx.save_for_backward(x, z, lens, states)
         return h, last
 
@@ -208,7 +221,10 @@ class _GatedRecurrence(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dh, dlast):
         x, z, lens, states = ctx.saved_tensors
-        (shape, nbytes), dev = ctx.shape, x.device
+        # hooks on saved tensors may have laid x and z out anew: their strides are taken from what came back
+        x, z = (t if _contiguous_channels(t) else t.contiguous() for t in (x, z))
+        (shape, nbytes), dev = _recurrence_shape(x, z), x.device
+        lens, states = _dense(lens, states)
         dh = None if dh is None else dh.contiguous()
         dlast = None if dlast is None else dlast.contiguous()
         dx, ws = _result(x.shape, x.dtype, dev, nbytes)
@@ -234,7 +250,7 @@ def gated_recurrence(x, z, h0=None, lens=None):
     dtype_code(x.dtype)
     _check("z", z, x.device, x.dtype, x.shape, contiguous=False)
     for name, t in (("x", x), ("z", z)):
-        if t.numel() > 0 and t.shape[2] > 1 and t.stride(2) != 1:
+        if not _contiguous_channels(t):
             raise ValueError("%s must have contiguous channels" % name)
     if h0 is not None:
         _check("h0", h0, x.device, torch.float32, (x.shape[0], x.shape[2]))
@@ -265,7 +281,7 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        return _dropout_call(dy.contiguous(), ctx.p, ctx.saved_tensors[0]), None, None
+        return _dropout_call(dy.contiguous(), ctx.p, *_dense(*ctx.saved_tensors)), None, None
 
 
 def dropout(x, p, rng):
@@ -309,7 +325,7 @@ class _JointHidden(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dh):
-        enc, pred, logit_lens, label_lens, used = ctx.saved_tensors
+        enc, pred, logit_lens, label_lens, used = _dense(*ctx.saved_tensors)
         (shape, nbytes), dh = ctx.shape, dh.contiguous()
         denc, ws = _result(enc.shape, enc.dtype, enc.device, nbytes)
         dpred = torch.empty_like(pred)

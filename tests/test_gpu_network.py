@@ -259,6 +259,25 @@ def test_recurrence_in_pieces(torch, pkg, D):  # noqa: F811
         close(s, want_last, e["last"] + ONE * np.abs(want_last), "last")
 
 
+def test_gradients_with_saved_tensors_on_the_host(torch, pkg):  # noqa: F811
+    """Saved tensors that come back in another layout (views of a projection do) give the same gradients."""
+    g = torch.Generator(device="cuda").manual_seed(17)
+    both = torch.randn((3, 70, 24), device="cuda", generator=g, requires_grad=True)
+    weight = torch.randn((9, 12), device="cuda", generator=g, requires_grad=True)
+    labels = torch.randint(0, 9, (3, 70), device="cuda", generator=g).to(torch.int32)
+    tl, ul = ints(torch, [70, 33, 5]), ints(torch, [69, 2, 40])
+
+    def step():
+        h, last = pkg.gated_recurrence(both[:, :, :12], both[:, :, 12:], None, tl)
+        e = pkg.dropout(pkg.label_embedding(labels, weight, tl), 0.25, rng_of(torch, 1, 2))
+        j = pkg.joint_hidden(h, e, tl, ul, "tanh", 0.5, rng_of(torch, 3, 4))
+        return torch.autograd.grad((j, last), (both, weight), (torch.ones_like(j), torch.ones_like(last)))
+    want = step()
+    with torch.autograd.graph.save_on_cpu():
+        got = step()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("L", [5, 700])
 def test_recurrence_extreme_gates_and_bad_lengths(torch, pkg, L):  # noqa: F811
     inf = float("inf")

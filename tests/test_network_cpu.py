@@ -176,3 +176,32 @@ def test_plain_forms_against_their_float64_results():
             # each element's own rounding, and float32 arithmetic on values of the tensor's size
             assert g.shape == w.shape
             assert bool(((g.double() - w).abs() <= step * w.abs() + 2.0 ** -18 * w.abs().max() + 1e-30).all()), case
+
+
+# ---------------------------------------------------------------- the binding's calls, the library's stubbed
+
+@pytest.fixture
+def calls(net, monkeypatch):
+    """The entry points on CPU tensors: every library call is recorded as (name, arguments) and does nothing."""
+    made = []
+    monkeypatch.setattr(net, "_check", lambda *args, **kw: None)
+    monkeypatch.setattr(net, "_call", lambda fn, device, *args: made.append((fn.__name__, args)))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    return made
+
+
+def test_recurrence_gradient_of_tensors_saved_elsewhere(net, calls):
+    """Hooks on saved tensors give backward copies of x and z laid out anew: the gradient's call names the strides
+    of the copies, whose memory ends long before the strides of the views that the forward pass read would."""
+    import paper_2303_10384_amd as rnnt
+    both = torch.randn(2, 30, 12, requires_grad=True)
+    lens = torch.tensor([30, 7], dtype=torch.int32)
+    for copy in (lambda t: t.clone(memory_format=torch.contiguous_format),
+                 lambda t: t if t.dim() != 3 else t.clone().transpose(1, 2).contiguous().transpose(1, 2)):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, copy):
+            h, _ = rnnt.gated_recurrence(both[:, :, :6], both[:, :, 6:], None, lens)
+            torch.autograd.grad(h, both, torch.ones_like(h))
+        (_, fwd), (name, bwd) = calls[-2:]
+        assert name == "rnnt_recurrence_grad"
+        strides = lambda s: (s.x_stride_b, s.x_stride_t, s.z_stride_b, s.z_stride_t)  # noqa: E731
+        assert strides(fwd[2]) == (360, 12, 360, 12) and strides(bwd[2]) == (180, 6, 180, 6)
