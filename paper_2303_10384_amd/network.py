@@ -22,7 +22,8 @@ import math
 import torch
 from torch.autograd.function import once_differentiable
 
-from .binding import RNNT_OK, RNNTError, _call_workspace, _ptr, _stream_handle, _workspace_args, dtype_code, load_library
+from .binding import (RNNT_ERR_UNSUPPORTED, RNNT_OK, RNNTError, _call_workspace, _ptr, _stream_handle, _workspace_args,
+                      dtype_code, load_library)
 
 ACTIVATIONS = {"relu": 0, "tanh": 1}
 STATE_STEPS = 8  # RNNT_RECURRENCE_STATE_STEPS
@@ -73,6 +74,9 @@ def _library():
 # A call's descriptor and the bytes of its workspace; a program makes the same few again and again.
 @functools.lru_cache(maxsize=1024)
 def _shape(kind, size_of, *fields):
+    # ctypes would keep the low half of a size past 32 bits
+    if any(c_type is _i32 and v > 0x7fffffff for (_, c_type), v in zip(kind._fields_, fields)):
+        raise RNNTError(RNNT_ERR_UNSUPPORTED, kind.__name__)
     shape = kind(*fields)
     return shape, getattr(_library(), size_of)(shape)
 

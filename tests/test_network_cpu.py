@@ -205,3 +205,21 @@ def test_recurrence_gradient_of_tensors_saved_elsewhere(net, calls):
         assert name == "rnnt_recurrence_grad"
         strides = lambda s: (s.x_stride_b, s.x_stride_t, s.z_stride_b, s.z_stride_t)  # noqa: E731
         assert strides(fwd[2]) == (360, 12, 360, 12) and strides(bwd[2]) == (180, 6, 180, 6)
+
+
+def test_sizes_past_32_bits_are_refused(net, calls):
+    """The descriptors hold 32-bit sizes: a larger one is an error, not its low half."""
+    import paper_2303_10384_amd as rnnt
+    wide = (1 << 32) + 8
+    meta = lambda *s, **kw: torch.empty(s, device="meta", **kw)  # noqa: E731
+    i32 = {"dtype": torch.int32}
+    for call in (lambda: rnnt.label_embedding(meta(1, wide, **i32), meta(7, 4)),
+                 lambda: rnnt.label_embedding(meta(1, 3, **i32), meta(wide, 4)),
+                 lambda: rnnt.label_embedding(meta(1, 3, **i32), meta(7, wide, requires_grad=True)),
+                 lambda: rnnt.gated_recurrence(meta(1, wide, 4), meta(1, wide, 4)),
+                 lambda: rnnt.gated_recurrence(meta(wide, 1, 4), meta(wide, 1, 4)),
+                 lambda: rnnt.joint_hidden(meta(1, wide, 4), meta(1, 1, 4), meta(1, **i32), meta(1, **i32)),
+                 lambda: rnnt.joint_hidden(meta(1, 1, 4), meta(1, (1 << 31) + 1, 4), meta(1, **i32), meta(1, **i32))):
+        with pytest.raises(rnnt.RNNTError, match="UNSUPPORTED"):
+            call()
+    assert not calls
