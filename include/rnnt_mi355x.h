@@ -56,7 +56,8 @@ typedef enum {
   RNNT_ERR_BAD_BLANK = 3,    /* blank outside [0, V)                             */
   RNNT_ERR_BAD_DTYPE = 4,    /* unknown dtype, or grad_dtype not dtype / F32     */
   RNNT_ERR_BAD_VARIANT = 5,  /* unknown rnnt_variant_t                           */
-  RNNT_ERR_WORKSPACE = 6,    /* workspace given but smaller than required        */
+  RNNT_ERR_WORKSPACE = 6,    /* workspace given but smaller than required, or none
+                                given on a stream under capture                   */
   RNNT_ERR_ALIGNMENT = 7,    /* logits or grad not 16-byte aligned               */
   RNNT_ERR_HIP = 8,          /* a HIP runtime call failed (launch, allocation)   */
   RNNT_ERR_UNSUPPORTED = 9,  /* shape outside what the library handles (U_max+1 > 2048,
@@ -119,7 +120,10 @@ size_t rnnt_loss_workspace_bytes(rnnt_shape_t shape);
  *               posteriors; wild-card arcs carry no parameter.
  *   workspace   device buffer of at least rnnt_loss_workspace_bytes(shape)
  *               bytes, 256-byte aligned, or NULL: the library then takes and
- *               releases one with hipMallocAsync / hipFreeAsync on `stream`.
+ *               releases one with hipMallocAsync / hipFreeAsync on `stream`,
+ *               or returns RNNT_ERR_WORKSPACE where `stream` is being captured
+ *               (a captured call brings a workspace that lives as long as the
+ *               graph; the same holds for every call here that takes one).
  *               Its contents need no initialisation and are not preserved.
  *   stream      HIP stream the work is ordered on.
  * Calls that overlap in time must not share a workspace.  Shapes with

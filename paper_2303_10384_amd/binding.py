@@ -6,6 +6,7 @@ missing or the tensors are not on a GPU, the calls raise.
 """
 import ctypes
 import functools
+import math
 import os
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -169,10 +170,12 @@ def _stream_handle(device):
 # the current stream, like the call's kernels, and costs a lookup; the library's own
 # hipMallocAsync went back to the driver after every synchronisation (B=16 T=400 U=300 V=32,
 # the first pass on new inputs: 824 us so, 338 us now).  None, for the library to take its own, where
-# it refuses the shape anyway, before it allocates anything; where torch has no memory left, so that the
-# call's arguments are still checked first and its errors stay RNNTError; and under a stream capture: a
-# capture that torch did not begin would hand a block of torch's pool, free again after this call, to every
-# replay, where hipMallocAsync is captured with the kernels.
+# it refuses the shape anyway, before it allocates anything, and where torch has no memory left, so that the
+# call's arguments are still checked first and its errors stay RNNTError.
+# Under a stream capture the library takes none (RNNT_ERR_WORKSPACE), and a block that is free again after the call
+# would be handed to others while a capture that torch did not begin still writes it at every replay.  There it lives
+# as long as a result of the call does: behind the result in one block of memory where the call makes that (_result),
+# else held by the caller's result tensor.
 @functools.lru_cache(maxsize=256)
 def _workspace_size(kind, B, T_max, U_max, V):
     if U_max + 1 > 2048 or T_max * (U_max + 1) >= 1 << 27:
@@ -180,16 +183,42 @@ def _workspace_size(kind, B, T_max, U_max, V):
     return getattr(load_library(), kind)(Shape(B, T_max, U_max, V, DTYPE_F32, DTYPE_F32))
 
 
-def _call_workspace(nbytes, device):
+def _capturing(device):
+    torch = _torch()
+    if device.index == torch._C._cuda_getDevice():
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.device(device):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _workspace_block(nbytes, device):
     if not 0 < nbytes < 1 << 42:
         return None
     torch = _torch()
-    if torch.cuda.is_current_stream_capturing():
-        return None
     try:
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
     except torch.OutOfMemoryError:
         return None
+
+
+def _call_workspace(nbytes, device, result):
+    """A workspace, or None, for a call that writes `result`, a tensor that the caller keeps."""
+    workspace = _workspace_block(nbytes, device)
+    if workspace is not None and _capturing(device):
+        result._captured_workspaces = getattr(result, "_captured_workspaces", ()) + (workspace,)
+    return workspace
+
+
+def _result(shape, dtype, device, nbytes):
+    """A result tensor and the workspace of the call that fills it, or None."""
+    torch = _torch()
+    if nbytes and _capturing(device):
+        size = -(-math.prod(shape) * dtype.itemsize // 256) * 256
+        both = _workspace_block(size + nbytes, device)
+        if both is not None:
+            return torch.empty(0, dtype=dtype, device=device).set_(both.untyped_storage(), 0, shape), both[size:]
+        nbytes = 0
+    return torch.empty(shape, dtype=dtype, device=device), _workspace_block(nbytes, device)
 
 
 def shape_of(logits, grad_dtype=None):
@@ -233,10 +262,8 @@ def step_forward(logits, labels, logit_lens, label_lens, blank, variant):
     shape = _check_loss_inputs(logits, labels, logit_lens, label_lens, variant)
     dev = logits.device
     loss = torch.empty(shape.B, dtype=torch.float32, device=dev)
-    rows = torch.empty((shape.B * shape.T_max * (shape.U_max + 1), 4), dtype=torch.int32, device=dev)
-    # from torch's allocator, ordered on the current stream like the kernels that use it
-    workspace = _call_workspace(_workspace_size("rnnt_step_workspace_bytes", shape.B, shape.T_max, shape.U_max,
-                                                shape.V), dev)
+    rows, workspace = _result((shape.B * shape.T_max * (shape.U_max + 1), 4), torch.int32, dev,
+                              _workspace_size("rnnt_step_workspace_bytes", shape.B, shape.T_max, shape.U_max, shape.V))
     ws_ptr, ws_bytes = _workspace_args(workspace)
     st = lib.rnnt_step_forward(_ptr(logits), shape, _ptr(labels), _ptr(logit_lens), _ptr(label_lens), int(blank),
                                VARIANTS[variant], _ptr(loss), _ptr(rows), ws_ptr, ws_bytes, _stream_handle(dev))
@@ -265,6 +292,17 @@ def step_gradient(logits, rows, blank, scale=None, divisor=1.0):
     return grad
 
 
+def _loss_and_workspace(loss_out, B, device, workspace, nbytes):
+    """The losses' tensor, the caller's or a new one, and the call's workspace, the caller's or one of nbytes."""
+    torch = _torch()
+    if loss_out is None:
+        loss, own = _result((B,), torch.float32, device, nbytes)
+    else:
+        _check_gpu("loss_out", loss_out, torch.float32)
+        loss, own = loss_out, None if workspace is not None else _call_workspace(nbytes, device, loss_out)
+    return loss, own if workspace is None else workspace
+
+
 def rnnt_loss(logits, labels, logit_lens, label_lens, blank=0, variant="rnnt", need_grad=True,
               workspace=None, grad_out=None, loss_out=None, events=None, grad_dtype=None):
     """Per-utterance loss (float32, shape (B,)) and gradient (logits' shape and dtype, or None).
@@ -281,8 +319,12 @@ def rnnt_loss(logits, labels, logit_lens, label_lens, blank=0, variant="rnnt", n
         grad_dtype = grad_out.dtype
     shape = _check_loss_inputs(logits, labels, logit_lens, label_lens, variant, grad_dtype)
     dev = logits.device
-    loss = loss_out if loss_out is not None else torch.empty(shape.B, dtype=torch.float32, device=dev)
-    _check_gpu("loss_out", loss, torch.float32)
+    if workspace is not None:
+        _check_gpu("workspace", workspace)
+        nbytes = 0
+    else:
+        nbytes = _workspace_size("rnnt_loss_workspace_bytes", shape.B, shape.T_max, shape.U_max, shape.V)
+    loss, workspace = _loss_and_workspace(loss_out, shape.B, dev, workspace, nbytes)
     grad = None
     if need_grad:
         gdt = logits.dtype if grad_dtype is None else grad_dtype
@@ -290,11 +332,6 @@ def rnnt_loss(logits, labels, logit_lens, label_lens, blank=0, variant="rnnt", n
         _check_gpu("grad_out", grad, gdt)
         if grad.shape != logits.shape:
             raise ValueError("grad_out must have the logits' shape")
-    if workspace is not None:
-        _check_gpu("workspace", workspace)
-    else:
-        workspace = _call_workspace(_workspace_size("rnnt_loss_workspace_bytes", shape.B, shape.T_max, shape.U_max,
-                                                    shape.V), dev)
     ws_ptr, ws_bytes = _workspace_args(workspace)
     if events is None:
         st = lib.rnnt_loss(_ptr(logits), shape, _ptr(labels), _ptr(logit_lens), _ptr(label_lens), int(blank),
@@ -374,10 +411,12 @@ def lattice_scores(lp_blank, lp_label, logit_lens, label_lens, variant="rnnt"):
            for k in ("alpha", "beta", "occ_blank", "occ_label")}
     out["loss"] = torch.full((B,), nan, dtype=torch.float64, device=dev)
     out["loss_bwd"] = torch.full((B,), nan, dtype=torch.float64, device=dev)
+    workspace = _call_workspace(lib.rnnt_lattice_workspace_bytes(shape), dev, out["loss"]) if _capturing(dev) else None
+    ws_ptr, ws_bytes = _workspace_args(workspace)
     st = lib.rnnt_lattice_scores(_ptr(lp_blank), _ptr(lp_label), shape, _ptr(logit_lens), _ptr(label_lens),
                                  VARIANTS[variant], _ptr(out["alpha"]), _ptr(out["beta"]), _ptr(out["loss"]),
                                  _ptr(out["loss_bwd"]), _ptr(out["occ_blank"]), _ptr(out["occ_label"]),
-                                 None, 0, _stream_handle(dev))
+                                 ws_ptr, ws_bytes, _stream_handle(dev))
     if st != RNNT_OK:
         raise RNNTError(st, "rnnt_lattice_scores")
     return out
@@ -416,7 +455,7 @@ def viterbi_align(logits, labels, logit_lens, label_lens, blank=0, variant="rnnt
         _check_gpu("workspace", workspace)
     else:
         workspace = _call_workspace(_workspace_size("rnnt_viterbi_workspace_bytes", shape.B, shape.T_max, shape.U_max,
-                                                    shape.V), dev)
+                                                    shape.V), dev, score)
     ws_ptr, ws_bytes = _workspace_args(workspace)
     args = (_ptr(logits), shape, _ptr(labels), _ptr(logit_lens), _ptr(label_lens), int(blank), VARIANTS[variant],
             _ptr(score), _ptr(frames), _ptr(span), ws_ptr, ws_bytes, _stream_handle(dev))
@@ -503,8 +542,12 @@ def arc_loss(logits, logit_lens, label_lens, plan, need_grad=True, workspace=Non
     if logit_lens.shape != (shape.B,) or label_lens.shape != (shape.B,):
         raise ValueError("the length vectors must be (B,)")
     dev = logits.device
-    loss = loss_out if loss_out is not None else torch.empty(shape.B, dtype=torch.float32, device=dev)
-    _check_gpu("loss_out", loss, torch.float32)
+    nbytes = 0
+    if workspace is not None:
+        _check_gpu("workspace", workspace)
+    elif (plan.desc.B, plan.desc.T_max, plan.desc.U_max, plan.desc.V) == (shape.B, shape.T_max, shape.U_max, shape.V):
+        nbytes = arc_loss_workspace_bytes(plan)
+    loss, workspace = _loss_and_workspace(loss_out, shape.B, dev, workspace, nbytes)
     grad = None
     if need_grad:
         gdt = logits.dtype if grad_dtype is None else grad_dtype
@@ -512,10 +555,6 @@ def arc_loss(logits, logit_lens, label_lens, plan, need_grad=True, workspace=Non
         _check_gpu("grad_out", grad, gdt)
         if grad.shape != logits.shape:
             raise ValueError("grad_out must have the logits' shape")
-    if workspace is not None:
-        _check_gpu("workspace", workspace)
-    elif (plan.desc.B, plan.desc.T_max, plan.desc.U_max, plan.desc.V) == (shape.B, shape.T_max, shape.U_max, shape.V):
-        workspace = _call_workspace(arc_loss_workspace_bytes(plan), dev)
     ws_ptr, ws_bytes = _workspace_args(workspace)
     args = (_ptr(logits), shape, _ptr(logit_lens), _ptr(label_lens), ctypes.byref(plan.desc), _ptr(plan.image),
             _ptr(loss), _ptr(grad), ws_ptr, ws_bytes, _stream_handle(dev))

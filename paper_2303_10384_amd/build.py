@@ -23,7 +23,8 @@ SOURCES = ["csrc/rnnt_api.hip", "csrc/rnnt_launch_k1_lattice.hip", "csrc/rnnt_la
            "csrc/rnnt_net_joint.hip"]
 HEADERS = ["csrc/rnnt_device.h", "csrc/rnnt_k1_populate.h", "csrc/rnnt_k2_lattice.h", "csrc/rnnt_k2_linear.h", "csrc/rnnt_k2_viterbi.h",
            "csrc/rnnt_k3_grad.h", "csrc/rnnt_arc_layout.h", "csrc/rnnt_arc_kernels.h", "csrc/rnnt_launch.h", "csrc/rnnt_step.h",
-           "csrc/rnnt_launch_k1.h", "csrc/rnnt_launch_k2.h", "csrc/rnnt_net.h"]
+           "csrc/rnnt_launch_k1.h", "csrc/rnnt_launch_k2.h", "csrc/rnnt_net.h",
+           "csrc/rnnt_workspace.h"]
 
 
 def hipcc():

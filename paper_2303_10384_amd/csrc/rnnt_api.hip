@@ -10,6 +10,7 @@
 #include "rnnt_mi355x.h"
 #include "rnnt_launch.h"
 #include "rnnt_step.h"
+#include "rnnt_workspace.h"
 
 // Workspace of rnnt_loss_noalloc: one copy on every GPU the library runs on.  In
 // host code this name is only a stand-in for the array; its device address is
@@ -115,28 +116,6 @@ bool keep_logits(const rnnt_shape_t& s, bool need_grad) {
 }
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
-
-// Stream-ordered workspace when the caller passes none.
-struct OwnedWorkspace {
-  void* ptr = nullptr;
-  hipStream_t stream = nullptr;
-  ~OwnedWorkspace() {
-    if (ptr) (void)hipFreeAsync(ptr, stream);
-  }
-};
-
-rnnt_status_t take_workspace(void* workspace, size_t workspace_bytes, size_t need, hipStream_t stream,
-                             OwnedWorkspace& owned, char** ws) {
-  if (workspace && workspace_bytes < need) return RNNT_ERR_WORKSPACE;
-  if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return RNNT_ERR_ALIGNMENT;
-  *ws = static_cast<char*>(workspace);
-  if (!*ws) {
-    if (hipMallocAsync(&owned.ptr, need, stream) != hipSuccess) return RNNT_ERR_HIP;
-    owned.stream = stream;
-    *ws = static_cast<char*>(owned.ptr);
-  }
-  return RNNT_OK;
-}
 
 // ---- arc-list lattices -------------------------------------------------------
 
@@ -401,10 +380,10 @@ rnnt_status_t rnnt_loss_timed(const void* logits, rnnt_shape_t shape, const int3
                                      grad_out);
   if (st != RNNT_OK) return st;
   const Layout L = make_layout(shape, true);
-  OwnedWorkspace owned;
-  char* ws = nullptr;
-  st = take_workspace(workspace, workspace_bytes, L.total, stream, owned, &ws);
+  Workspace space;
+  st = space.take(workspace, workspace_bytes, L.total, stream);
   if (st != RNNT_OK) return st;
+  char* const ws = space.ptr;
 
   const bool need_grad = grad_out != nullptr;
   RowInfo* rows = need_grad ? reinterpret_cast<RowInfo*>(ws + L.rowinfo) : nullptr;
@@ -447,10 +426,10 @@ rnnt_status_t rnnt_step_forward(const void* logits, rnnt_shape_t shape, const in
   if (!rows_out) return RNNT_ERR_NULL_PTR;
   if (!aligned16(rows_out)) return RNNT_ERR_ALIGNMENT;
   const Layout L = make_layout(shape, true);
-  OwnedWorkspace owned;
-  char* ws = nullptr;
-  const rnnt_status_t st_ws = take_workspace(workspace, workspace_bytes, L.total - L.lp2, stream, owned, &ws);
+  Workspace space;
+  const rnnt_status_t st_ws = space.take(workspace, workspace_bytes, L.total - L.lp2, stream);
   if (st_ws != RNNT_OK) return st_ws;
+  char* const ws = space.ptr;
   // the row records live in rows_out: the workspace is the layout from lp2 on
   return run_rows(logits, shape, labels, logit_lens, label_lens, blank, variant, loss_out, ws - L.lp2, L,
                   static_cast<RowInfo*>(rows_out), keep_logits(shape, true), stream, nullptr);
@@ -515,10 +494,10 @@ rnnt_status_t rnnt_viterbi_timed(const void* logits, rnnt_shape_t shape, const i
   if (!aligned16(logits)) return RNNT_ERR_ALIGNMENT;
   if (!sweep_fits(shape)) return RNNT_ERR_UNSUPPORTED;
   const ViterbiLayout L = make_viterbi_layout(shape);
-  OwnedWorkspace owned;
-  char* ws = nullptr;
-  st = take_workspace(workspace, workspace_bytes, L.total, stream, owned, &ws);
+  Workspace space;
+  st = space.take(workspace, workspace_bytes, L.total, stream);
   if (st != RNNT_OK) return st;
+  char* const ws = space.ptr;
   auto mark = [&](int i) { return events ? hipEventRecord(events[i], stream) : hipSuccess; };
   if (mark(0) != hipSuccess) return RNNT_ERR_HIP;
 
@@ -580,10 +559,10 @@ rnnt_status_t rnnt_arc_loss_timed(const void* logits, rnnt_shape_t shape, const 
   if (!aligned16(logits) || (grad_out && !aligned16(grad_out)) || !aligned16(plan_image))
     return RNNT_ERR_ALIGNMENT;
   const ArcLayout L = make_arc_layout(*plan);
-  OwnedWorkspace owned;
-  char* ws = nullptr;
-  st = take_workspace(workspace, workspace_bytes, L.total, stream, owned, &ws);
+  Workspace space;
+  st = space.take(workspace, workspace_bytes, L.total, stream);
   if (st != RNNT_OK) return st;
+  char* const ws = space.ptr;
   const char* img = static_cast<const char*>(plan_image);
   auto arr = [&](int i) { return img + plan->off[i]; };
 
@@ -750,10 +729,10 @@ rnnt_status_t rnnt_lattice_scores(const double* lp_blank, const double* lp_label
   if (!variant_known(variant)) return RNNT_ERR_BAD_VARIANT;
   if (!scores_fit(s)) return RNNT_ERR_UNSUPPORTED;
   const Layout L = make_layout(s, false);
-  OwnedWorkspace owned;
-  char* ws = nullptr;
-  st = take_workspace(workspace, workspace_bytes, L.total, stream, owned, &ws);
+  Workspace space;
+  st = space.take(workspace, workspace_bytes, L.total, stream);
   if (st != RNNT_OK) return st;
+  char* const ws = space.ptr;
 
   LatticeParams p2{};
   p2.B = s.B;

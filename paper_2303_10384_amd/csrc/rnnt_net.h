@@ -9,6 +9,7 @@
 
 #include "rnnt_device.h"
 #include "rnnt_network_mi355x.h"
+#include "rnnt_workspace.h"
 
 namespace rnnt {
 
@@ -358,32 +359,6 @@ inline bool drop_params(double p, const int64_t* rng, DropParams* out) {
   out->rng = rng;
   return true;
 }
-
-// The caller's workspace, or one taken for the call, stream-ordered.  None is taken for a stream
-// under capture: a graph of several calls, each with an allocation and a free of its own, has
-// faulted when it was replayed, so a captured call brings its workspace.
-struct NetWorkspace {
-  char* ptr = nullptr;
-  void* owned = nullptr;
-  hipStream_t stream = nullptr;
-  ~NetWorkspace() {
-    if (owned) (void)hipFreeAsync(owned, stream);
-  }
-  rnnt_status_t take(void* given, size_t given_bytes, size_t need, hipStream_t s) {
-    if (given && given_bytes < need) return RNNT_ERR_WORKSPACE;
-    if (given && !multiple_of(256, given)) return RNNT_ERR_ALIGNMENT;
-    ptr = static_cast<char*>(given);
-    if (!ptr && need > 0) {
-      hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-      if (hipStreamIsCapturing(s, &capture) != hipSuccess) return RNNT_ERR_HIP;
-      if (capture != hipStreamCaptureStatusNone) return RNNT_ERR_WORKSPACE;
-      if (hipMallocAsync(&owned, need, s) != hipSuccess) return RNNT_ERR_HIP;
-      stream = s;
-      ptr = static_cast<char*>(owned);
-    }
-    return RNNT_OK;
-  }
-};
 
 inline rnnt_status_t launched() { return hipGetLastError() == hipSuccess ? RNNT_OK : RNNT_ERR_HIP; }
 

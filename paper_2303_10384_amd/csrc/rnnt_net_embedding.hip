@@ -487,7 +487,7 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   const int64_t row_waves = (static_cast<int64_t>(shape.V) + kRowsToWave - 1) / kRowsToWave * p.tiles, row_blocks = (row_waves + 3) / 4;
   if (row_blocks + run_items > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
   const GradLayout L = grad_layout(shape, p.rows);
-  NetWorkspace ws;
+  Workspace ws;
   st = ws.take(workspace, workspace_bytes, L.total, stream);
   if (st != RNNT_OK) return st;
   p.dout = dout;

@@ -699,7 +699,7 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
   if (!multiple_of(e, enc) || !multiple_of(e, pred) || !multiple_of(e, dh) || !multiple_of(e, denc) ||
       !multiple_of(e, dpred) || !multiple_of(8, rng))
     return RNNT_ERR_ALIGNMENT;
-  NetWorkspace ws;
+  Workspace ws;
   st = ws.take(workspace, workspace_bytes, rnnt_joint_hidden_grad_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
   q.enc = enc;

@@ -574,7 +574,7 @@ rnnt_status_t rnnt_recurrence(const void* x, const void* z, rnnt_recurrence_shap
   if (!multiple_of(e, x) || !multiple_of(e, z) || !multiple_of(e, h_out) || !multiple_of(4, h0) ||
       !multiple_of(4, last_out) || !multiple_of(16, states_out))
     return RNNT_ERR_ALIGNMENT;
-  NetWorkspace ws;
+  Workspace ws;
   st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
   RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);
@@ -612,7 +612,7 @@ rnnt_status_t rnnt_recurrence_grad(const void* x, const void* z, rnnt_recurrence
   if (!multiple_of(e, x) || !multiple_of(e, z) || !multiple_of(e, dh) || !multiple_of(e, dx) || !multiple_of(e, dz) ||
       !multiple_of(4, dlast) || !multiple_of(4, dh0) || !multiple_of(16, states))
     return RNNT_ERR_ALIGNMENT;
-  NetWorkspace ws;
+  Workspace ws;
   st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
   RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);

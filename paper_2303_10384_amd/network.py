@@ -13,17 +13,16 @@ with h0 the state before, enc (B, 1, H) against pred (B, 1, H).
 Every tensor of a call is on one GPU, which need not be the current one; work is queued on
 that GPU's current stream.  A gradient of a gradient is not offered.  Calls may be captured
 into a graph, backward passes too (as with any operation, while no eager graph of the same
-leaves is alive); a captured loss call brings its workspace.
+leaves is alive).
 """
 import ctypes
 import functools
-import math
 
 import torch
 from torch.autograd.function import once_differentiable
 
-from .binding import (RNNT_ERR_UNSUPPORTED, RNNT_OK, RNNTError, _call_workspace, _ptr, _stream_handle, _workspace_args,
-                      dtype_code, load_library)
+from .binding import (RNNT_ERR_UNSUPPORTED, RNNT_OK, RNNTError, _ptr, _result, _stream_handle, _workspace_args, dtype_code,
+                      load_library)
 
 ACTIVATIONS = {"relu": 0, "tanh": 1}
 STATE_STEPS = 8  # RNNT_RECURRENCE_STATE_STEPS
@@ -118,22 +117,6 @@ def _check_p(p):
 def _dense(*saved):
     """Saved tensors as the kernels take them: hooks on saved tensors may give any layout back."""
     return (None if t is None else t.contiguous() for t in saved)
-
-
-def _result(shape, dtype, device, nbytes):
-    """A result tensor and the workspace of the call that fills it, or None.
-
-    Under a stream capture the workspace is the rest of the result's memory, so that it belongs
-    to the graph for as long as the program holds what the graph computes, whoever began the
-    capture; else it is a block of torch's allocator, free again behind the call's kernels (None
-    where torch has no memory left: the library then takes its own)."""
-    if not nbytes:
-        return torch.empty(shape, dtype=dtype, device=device), None
-    if not torch.cuda.is_current_stream_capturing():
-        return torch.empty(shape, dtype=dtype, device=device), _call_workspace(nbytes, device)
-    size = -(-math.prod(shape) * dtype.itemsize // 256) * 256
-    both = torch.empty(size + nbytes, dtype=torch.uint8, device=device)
-    return torch.empty(0, dtype=dtype, device=device).set_(both.untyped_storage(), 0, shape), both[size:]
 
 
 # ---------------------------------------------------------------- label embedding

@@ -115,3 +115,61 @@ def test_no_memory_left_in_torch(torch, pkg, monkeypatch):  # noqa: F811
     assert np.array_equal(xr.grad.cpu().numpy(), grad_ref.cpu().numpy())
     with pytest.raises(pkg.RNNTError, match="blank"):
         pkg.rnnt_loss(lg, labels, tl, ul, blank=99, grad_out=grad, loss_out=loss)
+
+
+def test_captured_call_without_a_workspace_is_refused(torch, pkg):  # noqa: F811
+    """The C calls: none is allocated inside a capture, which goes on; eager calls take their own."""
+    from paper_2303_10384_amd import binding
+    lg, labels, tl, ul = inputs(torch)
+    loss_ref, grad_ref = pkg.rnnt_loss(lg, labels, tl, ul)
+    lib, shape = binding.load_library(), binding.shape_of(lg)
+    loss, grad = torch.zeros_like(loss_ref), torch.zeros_like(lg)
+    ptr = lambda t: t.data_ptr()  # noqa: E731
+
+    def call():
+        return lib.rnnt_loss(ptr(lg), shape, ptr(labels), ptr(tl), ptr(ul), 0, 0, ptr(loss), ptr(grad), None, 0,
+                             torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        status = call()
+        loss.fill_(3.0)
+    assert status == 6
+    g.replay()
+    torch.cuda.synchronize()
+    assert bool((loss == 3).all()) and bool((grad == 0).all())
+    assert call() == 0
+    torch.cuda.synchronize()
+    assert torch.equal(loss, loss_ref) and torch.equal(grad, grad_ref)
+
+
+def test_captured_autograd_loss(torch, pkg):  # noqa: F811
+    """Loss and gradient through autograd in a graph, with memory of torch's alone; the upstream gradient and the
+    logits change between the replays."""
+    lg, labels, tl, ul = inputs(torch)
+    up = torch.ones(6, device="cuda")
+    lg.requires_grad_(True)
+
+    def step():
+        loss = pkg.rnnt_loss_autograd(lg, labels, tl, ul, reduction="none")
+        return loss.detach(), torch.autograd.grad(loss, lg, up)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for i in range(4):
+        up.fill_(1.0 + i)
+        with torch.no_grad():
+            lg.mul_(1.125)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

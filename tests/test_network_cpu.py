@@ -223,3 +223,47 @@ def test_sizes_past_32_bits_are_refused(net, calls):
         with pytest.raises(rnnt.RNNTError, match="UNSUPPORTED"):
             call()
     assert not calls
+
+
+def test_captured_losses_bring_their_workspace(net, monkeypatch):
+    """Under a capture every loss call names a workspace (the library would have to refuse it without), which lives
+    as long as a result does: behind the rows that backward needs, behind the losses, or with the caller's tensor."""
+    import paper_2303_10384_amd as rnnt
+    from paper_2303_10384_amd import binding
+    real, made = binding.load_library(), []
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith("_bytes") or name == "rnnt_status_string":
+                return getattr(real, name)
+            return lambda *args: made.append((name, args)) or 0
+
+    monkeypatch.setattr(binding, "_lib", Library())
+    monkeypatch.setattr(binding, "_check_gpu", lambda *args: None)
+    monkeypatch.setattr(binding, "_stream_handle", lambda device: 0)
+    monkeypatch.setattr(binding, "_capturing", lambda device: True)
+    logits = torch.randn(2, 5, 4, 6, requires_grad=True)
+    labels, tl, ul = torch.ones(2, 3, dtype=torch.int32), torch.full((2,), 5, dtype=torch.int32), torch.full((2,), 3, dtype=torch.int32)
+
+    def inside(ptr, size, t):
+        at = t.untyped_storage().data_ptr()
+        return size > 0 and ptr % 256 == at % 256 and at + t.numel() * t.element_size() <= ptr and \
+            ptr + size <= at + t.untyped_storage().nbytes()
+    loss = rnnt.rnnt_loss_autograd(logits, labels, tl, ul)
+    torch.autograd.grad(loss, logits, retain_graph=True)
+    (name, fwd), (_, bwd) = made
+    assert name == "rnnt_step_forward"
+    rows = loss.grad_fn.saved_tensors[1]
+    assert fwd[8] == bwd[3] == rows.data_ptr() and inside(fwd[9], fwd[10], rows)
+    x = logits.detach()
+    loss, _ = rnnt.rnnt_loss(x, labels, tl, ul)
+    assert inside(made[-1][1][9], made[-1][1][10], loss)
+    mine = torch.empty(2)
+    rnnt.rnnt_loss(x, labels, tl, ul, loss_out=mine, grad_out=torch.empty_like(x))
+    rnnt.rnnt_loss(x, labels, tl, ul, loss_out=mine, need_grad=False)
+    assert [made[i][1][9] for i in (-2, -1)] == [w.data_ptr() for w in mine._captured_workspaces]
+    score, _, _ = rnnt.viterbi_align(x, labels, tl, ul)
+    assert made[-1][1][10] == score._captured_workspaces[0].data_ptr()
+    given = torch.empty(1 << 20, dtype=torch.uint8)
+    rnnt.rnnt_loss(x, labels, tl, ul, workspace=given)
+    assert made[-1][1][9] == given.data_ptr()
