@@ -11,14 +11,15 @@ A streaming decoder takes the same calls one step at a time: labels (B, 1), x an
 with h0 the state before, enc (B, 1, H) against pred (B, 1, H).
 
 Every tensor of a call is on one GPU, which need not be the current one; work is queued on
-that GPU's current stream.  A gradient of a gradient is not offered.  Calls may be captured
-into a graph, backward passes too (as with any operation, while no eager graph of the same
-leaves is alive).
+that GPU's current stream.  A gradient of a gradient and forward mode are not offered.  Calls
+may be captured into a graph, backward passes too (as with any operation, while no eager graph
+of the same leaves is alive).
 """
 import ctypes
 import functools
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from .binding import (RNNT_ERR_UNSUPPORTED, RNNT_OK, RNNTError, _ptr, _result, _stream_handle, _workspace_args, dtype_code,
@@ -114,6 +115,14 @@ def _check_p(p):
     return p
 
 
+def _recorded(*tensors):
+    """Whether a call goes through autograd: for a gradient, and wherever a tensor could carry a tangent, which
+    autograd refuses (the operators have no forward mode)."""
+    if forward_ad._current_level >= 0:
+        return True
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 def _dense(*saved):
     """Saved tensors as the kernels take them: hooks on saved tensors may give any layout back."""
     return (None if t is None else t.contiguous() for t in saved)
@@ -168,7 +177,7 @@ def label_embedding(labels, weight, lens=None, scale=1.0, start=None):
     if start is not None and not 0 <= start < weight.shape[0]:
         raise ValueError("start must be None or a row of weight, got %r" % (start,))
     args = (labels, weight, lens, float(scale), -1 if start is None else int(start))
-    if weight.requires_grad and torch.is_grad_enabled():
+    if _recorded(weight):
         return _LabelEmbedding.apply(*args)
     return _embedding_forward(*args)[0]
 
@@ -243,7 +252,7 @@ def gated_recurrence(x, z, h0=None, lens=None):
         _check("h0", h0, x.device, torch.float32, (x.shape[0], x.shape[2]))
     if lens is not None:
         _check("lens", lens, x.device, torch.int32, x.shape[:1])
-    if torch.is_grad_enabled() and (x.requires_grad or z.requires_grad or (h0 is not None and h0.requires_grad)):
+    if _recorded(x, z, h0):
         return _GatedRecurrence.apply(x, z, h0, lens)
     return _recurrence_forward(x, z, h0, lens, False)[:2]
 
@@ -283,7 +292,7 @@ def dropout(x, p, rng):
     dtype_code(x.dtype)
     p = _check_p(p)
     _check("rng", rng, x.device, torch.int64, (2,))
-    if x.requires_grad and torch.is_grad_enabled():
+    if _recorded(x):
         return _Dropout.apply(x, p, rng)
     return _dropout_call(x, p, rng)
 
@@ -346,6 +355,6 @@ def joint_hidden(enc, pred, logit_lens, label_lens, activation="relu", p=0.0, rn
     if rng is not None:
         _check("rng", rng, enc.device, torch.int64, (2,))
     args = (enc, pred, logit_lens, label_lens, ACTIVATIONS[activation], p, rng)
-    if torch.is_grad_enabled() and (enc.requires_grad or pred.requires_grad):
+    if _recorded(enc, pred):
         return _JointHidden.apply(*args)
     return _joint_forward(*args)[0]

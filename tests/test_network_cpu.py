@@ -267,3 +267,25 @@ def test_captured_losses_bring_their_workspace(net, monkeypatch):
     given = torch.empty(1 << 20, dtype=torch.uint8)
     rnnt.rnnt_loss(x, labels, tl, ul, workspace=given)
     assert made[-1][1][9] == given.data_ptr()
+
+
+def test_forward_mode_is_refused(net, calls):
+    """A tensor that carries a tangent is an error, with and without requires_grad, not a result without one."""
+    import torch.autograd.forward_ad as fw
+    import paper_2303_10384_amd as rnnt
+    x, w = torch.randn(2, 3, 4), torch.randn(5, 4)
+    labels, lens, rng = torch.zeros(2, 3, dtype=torch.int32), torch.ones(2, dtype=torch.int32), torch.tensor([1, 2])
+    h0 = torch.randn(2, 4)
+    with fw.dual_level():
+        dual = lambda t, grad: fw.make_dual(t.clone().requires_grad_(grad), torch.ones_like(t))  # noqa: E731
+        for grad in (False, True):
+            for call in (lambda: rnnt.label_embedding(labels, dual(w, grad)), lambda: rnnt.gated_recurrence(dual(x, grad), x),
+                         lambda: rnnt.gated_recurrence(x, dual(x, grad)), lambda: rnnt.gated_recurrence(x, x, dual(h0, grad)),
+                         lambda: rnnt.dropout(dual(x, grad), 0.5, rng), lambda: rnnt.joint_hidden(dual(x, grad), x, lens, lens),
+                         lambda: rnnt.joint_hidden(x, dual(x, grad), lens, lens)):
+                with pytest.raises(NotImplementedError):
+                    call()
+                with pytest.raises(NotImplementedError), torch.no_grad():
+                    call()
+        n = len(calls)
+        assert not rnnt.dropout(x, 0.5, rng).requires_grad and len(calls) == n + 1  # no tangent: as ever
