@@ -9,15 +9,14 @@ namespace rnnt {
 namespace {
 
 // A block of W waves takes a tile of channels of one sequence and goes over its steps W * kSteps at a time, kSteps of
-// them to a wave: a wave scans its steps from a zero state and multiplies their gates up, the waves' (product, state) pairs
-// meet in LDS, and every wave adds the state that arrives at its first step, h_j = S_j + P_j h_in.  x and z are
-// read once, the next tile's while this one is computed.
+// them to a wave: a wave scans its steps from a zero state and multiplies their gates up, the waves' pairs (product P
+// of the gates, state S) meet in LDS, every wave finds the state P h + S that arrives at its first step, and takes its
+// steps again from there.  x and z are read once, the next tile's while this one is computed.
 // Where sequences and channel tiles are too few to fill the chip, the steps are cut into segments: a first kernel
 // finds each segment's pair, the second one begins each block at the state that the pairs before it give.
-// Bound by the bytes of x, z and h, twice x and z in segments (L=60013 D=640 bf16, one sequence: 27 us at 5.6 TB/s for
-// the pairs, 41 us at 5.7 TB/s for the states).  One pass in which a block waits for the blocks before it would read
-// them once; not built: 469 tiles of that sequence, about a hundred of them on the chip at a time, would each look back
-// over those through the memory-side cache, an estimated 6 to 12 us a tile, which is what the second read costs.
+// Bound by the bytes of x, z and h, twice x and z in segments, and for 16 bits as much by the instructions of gates and
+// runs (L=60013 D=640 bf16, one sequence: 30 us at 5.2 TB/s for the pairs, 46 us at 5.0 TB/s for the states).  One pass in which a block waits for the blocks before it would read
+// them once; not built.
 constexpr int kSteps = RNNT_RECURRENCE_STATE_STEPS;
 constexpr int kWaves = 16;                     // of a block where sequences are few: as many as it can have
 constexpr int kTileSteps = kSteps * kWaves;    // segments are multiples of it
@@ -38,6 +37,63 @@ struct RecurrenceParams {
   float2* pairs;  // (B, segments, D) of the segments
   int32_t B, L, D, n_states, tiles, segments, seg_steps;
 };
+
+// ---- a step, and steps joined ---------------------------------------------------
+// Whatever a state is added up from, a rounding has the size of a h or of (1 - a) x: what a shut gate lets through
+// keeps its digits however large the state that it drops, and what an open one holds does not drift, however long.
+
+// A step on its own, from the nearer of h and x a small part of the way to the other: h + g (x - h) where the gate is
+// open, x + a (h - x) where it is shut (x = h stays).  By the definition where the difference is no finite float.
+__device__ __forceinline__ float advance(float a, float g, float x, float h) {
+  const float d = x - h;
+  if (__builtin_isfinite(d)) return a < g ? __builtin_fmaf(-a, d, x) : __builtin_fmaf(g, d, h);
+  return __builtin_fmaf(a, h, g * x);
+}
+
+constexpr float kLeast = 0x1p-126f;  // a product of gates that is below the floats does not make NaN of an infinity
+
+// A run of steps, h -> P h + S.  Up to 2 kSteps of them go by the definition, h = fma(a, h, g x), whose rounded a costs
+// 2^-24 a step.  Between runs that would grow with the gates' memory, as 2^-24 / (1 - a) (z = 10 over 60000 steps: 5e-4),
+// so Q = 1 - P is added up on its own.
+struct Run {
+  float P = 1.f, Q = 0.f, S = 0.f;
+
+  // one step more; returns g x
+  __device__ __forceinline__ float step(float a, float g, float x, bool on) {
+    const float in = g * x, q = __builtin_fmaf(g, P, Q), p = a * P, s = __builtin_fmaf(a, S, in);
+    Q = on ? q : Q;
+    P = on ? p : P;
+    S = on ? s : S;
+    return in;
+  }
+  // The run joined to the state h as h + (S - Q h) where Q is below 1/2, as P h + S elsewhere.
+  __device__ __forceinline__ float join(float h) const {
+    if (Q < 0.5f && __builtin_isfinite(h)) return __builtin_fmaf(-Q, h, S) + h;
+    return __builtin_fmaf(fmaxf(P, kLeast), h, S);
+  }
+  // `next` behind this one
+  __device__ __forceinline__ void append(const Run& next) {
+    S = next.join(S);
+    Q = __builtin_fmaf(next.P, Q, next.Q);
+    P = next.Q < 0.5f ? __builtin_fmaf(-next.Q, P, P) : next.P * P;
+  }
+  // In memory (m, S): m is P, or -Q where Q is below 1/2 (and below 0 also where Q = 0), from which the other is known
+  // to its last digit.
+  __device__ __forceinline__ float2 pack() const { return make_float2(Q < 0.5f ? fminf(-Q, -kLeast) : P, S); }
+  __device__ __forceinline__ static Run unpack(float2 k) {
+    Run r;
+    r.P = k.x < 0.f ? 1.f + k.x : k.x;
+    r.Q = k.x < 0.f ? -k.x : 1.f - k.x;
+    r.S = k.y;
+    return r;
+  }
+};
+
+// Run::unpack(k).join(h) for a finite h, in three operations; not finite for one that is not, nor is any behind it.
+__device__ __forceinline__ float join_finite(float2 k, float h) {
+  const float keep = __builtin_amdgcn_fmed3f(k.x * -0x1p127f, 0.f, 1.f);  // 1 where m is -Q
+  return __builtin_fmaf(keep, h, __builtin_fmaf(k.x, h, k.y));
+}
 
 // The part of the work that a block has, and its sequence's length.
 struct Place {
@@ -90,13 +146,15 @@ struct RowStore {
   }
 };
 
-// The (product, state) pairs of a block's waves, two sets of them in turn.
+// The pairs of a block's waves, two sets of them in turn: forward Run::pack()'s, backward the product of the gates and
+// the sum, whose terms have weights of at most 1.
 template <int VEC, int W>
 struct PairBoard {
   struct __attribute__((aligned(8 * VEC))) Pairs {
     float2 of[VEC];
   };
   Pairs at[2][W][64];
+  float state[2][64][VEC];  // forward: at the tile's first step
 
   __device__ __forceinline__ void put(int set, int wave, int lane, const float* A, const float* S) {
     Pairs k;
@@ -104,12 +162,40 @@ struct PairBoard {
     for (int v = 0; v < VEC; ++v) k.of[v] = make_float2(A[v], S[v]);
     at[set][wave][lane] = k;
   }
-  // carry through all waves' pairs, in order or backwards; `mine` is what arrives at `wave`
-  template <bool BACK>
+  __device__ __forceinline__ void put(int set, int wave, int lane, const Run* run) {
+    Pairs k;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) k.of[v] = run[v].pack();
+    at[set][wave][lane] = k;
+  }
+  // forward: the state that arrives at `wave`'s run, from the tile's through the runs before
+  __device__ __forceinline__ void arrive(int set, int wave, int lane, float* h) const {
+    float first[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) h[v] = first[v] = state[set][lane][v];
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {
+      if (i >= wave) break;
+      const Pairs k = at[set][i][lane];
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) h[v] = join_finite(k.of[v], h[v]);
+    }
+    bool finite = true;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) finite = finite && __builtin_isfinite(h[v]);
+    if (finite) return;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) h[v] = first[v];
+#pragma unroll 1
+    for (int i = 0; i < wave; ++i) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) h[v] = Run::unpack(at[set][i][lane].of[v]).join(h[v]);
+    }
+  }
+  // backward: carry through all waves' pairs from the last on; `mine` is what arrives at `wave`
   __device__ __forceinline__ void compose(int set, int wave, int lane, float* carry, float* mine) const {
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const int w = BACK ? W - 1 - i : i;
+    for (int w = W - 1; w >= 0; --w) {
       const Pairs k = at[set][w][lane];
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
@@ -128,30 +214,46 @@ __device__ __forceinline__ void carry_in(const RecurrenceParams& p, const Place&
   if (n == 0) return;
   const int share = (n + W - 1) / W, from = min(wave * share, n), to = min(from + share, n);
   const float2* pairs = p.pairs + (static_cast<int64_t>(at.b) * p.segments + (BACK ? at.segment + 1 : 0)) * p.D + c;
-  float A[VEC], S[VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-    A[v] = 1.f;
-    S[v] = 0.f;
-  }
-#pragma unroll 4
-  for (int i = from; i < to; ++i) {
-    const int seg = BACK ? to - 1 - (i - from) : i;
+  if constexpr (BACK) {
+    float A[VEC], S[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      const float2 k = pairs[static_cast<int64_t>(seg) * p.D + v];
-      S[v] = __builtin_fmaf(k.x, S[v], k.y);
-      A[v] *= k.x;
+      A[v] = 1.f;
+      S[v] = 0.f;
+    }
+#pragma unroll 4
+    for (int i = to - 1; i >= from; --i) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float2 k = pairs[static_cast<int64_t>(i) * p.D + v];
+        S[v] = __builtin_fmaf(k.x, S[v], k.y);
+        A[v] *= k.x;
+      }
+    }
+    board.put(1, wave, lane, A, S);
+    __syncthreads();
+    float none[VEC];
+    board.compose(1, wave, lane, carry, none);
+  } else {
+    Run run[VEC];
+#pragma unroll 4
+    for (int i = from; i < to; ++i) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) run[v].append(Run::unpack(pairs[static_cast<int64_t>(i) * p.D + v]));
+    }
+    board.put(1, wave, lane, run);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const auto one = board.at[1][i][lane];
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) carry[v] = Run::unpack(one.of[v]).join(carry[v]);
     }
   }
-  board.put(1, wave, lane, A, S);
-  __syncthreads();
-  float none[VEC];
-  board.template compose<BACK>(1, wave, lane, carry, none);
 }
 
 template <typename T, int VEC, int W>
-__global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
+__global__ __launch_bounds__(64 * W, 4) void net_recurrence(RecurrenceParams p) {
   constexpr int TILE = W * kSteps;
   __shared__ PairBoard<VEC, W> board;
   const Place at(p);
@@ -173,12 +275,8 @@ __global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
     zs.load(z, p.z_st, t0 + wave * kSteps, at.len, c);
     for (int set = 0; t0 < min(at.end, at.len); t0 += TILE, set ^= 1) {
       const int t = t0 + wave * kSteps, live = at.len - t;
-      float S[kSteps][VEC], P[kSteps][VEC], s[VEC], q[VEC];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        s[v] = 0.f;
-        q[v] = 1.f;
-      }
+      float a[kSteps][VEC], in[kSteps][VEC];  // in: (1 - a) x
+      Run run[VEC];
       // the next tile's rows, on their way while this one is computed
       const Rows<T, VEC> xn = xs, zn = zs;
       if (t0 + TILE < min(at.end, at.len)) {
@@ -195,25 +293,30 @@ __global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
           zn.r[j].get(zf);
 #pragma unroll
           for (int v = 0; v < VEC; ++v) {
-            float a, g;
-            gate<T>(zf[v], a, g);
-            const float next = __builtin_fmaf(g, xf[v] - s[v], s[v]);
-            s[v] = all || j < live ? next : s[v];
-            q[v] = all || j < live ? a * q[v] : q[v];
-            S[j][v] = s[v];
-            P[j][v] = q[v];
+            float g;
+            gate_above_zero<T>(zf[v], a[j][v], g);
+            in[j][v] = run[v].step(a[j][v], g, xf[v], all || j < live);
           }
+          if (j == kSteps / 2 - 1) __builtin_amdgcn_sched_barrier(0);  // all gates begun at once would not fit the registers
         }
       };
       if (whole) scan(std::true_type{});
       else scan(std::false_type{});
-      board.put(set, wave, lane, q, s);
+      board.put(set, wave, lane, run);
+      if (wave == W - 1) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) board.state[set][lane][v] = carry[v];
+      }
       __syncthreads();  // one to a tile: the other set is written before the next
-      float in[VEC];
-      board.template compose<false>(set, wave, lane, carry, in);
+      float first[VEC];
+      board.arrive(set, wave, lane, first);
+      if (wave == W - 1) {  // to the next tile
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) carry[v] = run[v].join(first[v]);
+      }
       if (p.states && t < at.end) {
         Pack<float, VEC> k;
-        k.set(in);
+        k.set(first);
         k.store(p.states + (static_cast<int64_t>(at.b) * p.n_states + t / kSteps) * p.D + c);
       }
       const RowStore<T, VEC, W> out(h, row0 + t0, at.end - t0, p.D, c);
@@ -221,7 +324,10 @@ __global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
       for (int j = 0; j < kSteps; ++j) {
         float f[VEC];
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) f[v] = whole || j < live ? __builtin_fmaf(P[j][v], in[v], S[j][v]) : 0.f;
+        for (int v = 0; v < VEC; ++v) {
+          first[v] = __builtin_fmaf(a[j][v], first[v], in[j][v]);
+          f[v] = whole || j < live ? first[v] : 0.f;
+        }
         out.put(wave * kSteps + j, f);
       }
     }
@@ -234,7 +340,7 @@ __global__ __launch_bounds__(64 * W) void net_recurrence(RecurrenceParams p) {
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) out.put(wave * kSteps + j, f);
   }
-  if (at.segment == p.segments - 1 && wave == 0) {
+  if (at.segment == p.segments - 1 && wave == W - 1) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) p.last[bc + v] = carry[v];
   }
@@ -275,8 +381,8 @@ __global__ __launch_bounds__(64) void net_recurrence_short(RecurrenceParams p) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         float a, g;
-        gate<T>(zf[v], a, g);
-        f[v] = s[v] = __builtin_fmaf(g, xf[v] - s[v], s[v]);
+        gate_above_zero<T>(zf[v], a, g);
+        f[v] = s[v] = advance(a, g, xf[v], s[v]);
       }
     }
     k.set(f);
@@ -299,6 +405,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
   const int stop = min(at.end, at.len);
   const int from = min(at.begin + wave * share, stop), to = min(from + share, stop);
   float A[VEC], S[VEC];
+  Run all[VEC], run[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
     A[v] = 1.f;
@@ -325,45 +432,83 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
         if (with_x) xs.load(x, x_st, step_of(i + 1), to, c);
         zs.load(z, p.z_st, step_of(i + 1), to, c);
       }
+      if constexpr (BACK) {
 #pragma unroll
-      for (int k = 0; k < kSteps; ++k) {
-        const int j = BACK ? kSteps - 1 - k : k;
-        float xf[VEC], zf[VEC];
-        xn.r[j].get(xf);
-        zn.r[j].get(zf);
+        for (int j = kSteps - 1; j >= 0; --j) {
+          float xf[VEC], zf[VEC];
+          xn.r[j].get(xf);
+          zn.r[j].get(zf);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          float a, g;
-          gate<T>(zf[v], a, g);
-          const float next = BACK ? a * (S[v] + xf[v]) : __builtin_fmaf(g, xf[v] - S[v], S[v]);
-          S[v] = j < live ? next : S[v];
-          A[v] = j < live ? a * A[v] : A[v];
+          for (int v = 0; v < VEC; ++v) {
+            float a, g;
+            gate<T>(zf[v], a, g);
+            const float next = a * (S[v] + xf[v]);
+            S[v] = j < live ? next : S[v];
+            A[v] = j < live ? a * A[v] : A[v];
+          }
+        }
+      } else {
+        const auto scan = [&](auto whole) {
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j) {
+            float xf[VEC], zf[VEC];
+            xn.r[j].get(xf);
+            zn.r[j].get(zf);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+              float a, g;
+              gate_above_zero<T>(zf[v], a, g);
+              run[v].step(a, g, xf[v], whole || j < live);
+            }
+          }
+        };
+        if (live >= kSteps) scan(std::true_type{});
+        else scan(std::false_type{});
+        if ((i & 1) || i + 1 == batches) {  // two batches to a run
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) {
+            all[v].append(run[v]);
+            run[v] = Run{};
+          }
         }
       }
+    }
+  }
+  if constexpr (!BACK) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float2 k = all[v].pack();
+      A[v] = k.x;
+      S[v] = k.y;
     }
   }
   board.put(0, wave, lane, A, S);
   __syncthreads();
   if (wave != 0) return;
-  // the waves' pairs into one: the state from zero, and the product
+  // the waves' pairs into one
   float2* out = p.pairs + (static_cast<int64_t>(at.b) * p.segments + at.segment) * p.D + c;
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
-    float prod = 1.f, sum = 0.f;
+    float sum = 0.f, product = 1.f;
+    Run run;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
       const float2 k = board.at[0][BACK ? kWaves - 1 - i : i][lane].of[v];
-      sum = __builtin_fmaf(k.x, sum, k.y);
-      prod *= k.x;
+      if constexpr (BACK) {
+        sum = __builtin_fmaf(k.x, sum, k.y);
+        product *= k.x;
+      } else {
+        run.append(Run::unpack(k));
+      }
     }
-    out[v] = make_float2(prod, sum);
+    out[v] = BACK ? make_float2(product, sum) : run.pack();
   }
 }
 
 // The gradient goes the other way: s_t = dh_t + a_{t+1} s_{t+1}, tile by tile from the end, its carry d = a s.  The
 // states that dz needs are formed again from the one stored before the wave's first step.
 template <typename T, int VEC, int W>
-__global__ __launch_bounds__(64 * W) void net_recurrence_grad(RecurrenceParams p) {
+__global__ __launch_bounds__(64 * W, 4) void net_recurrence_grad(RecurrenceParams p) {
   constexpr int TILE = W * kSteps;
   __shared__ PairBoard<VEC, W> board;
   const Place at(p);
@@ -423,10 +568,12 @@ __global__ __launch_bounds__(64 * W) void net_recurrence_grad(RecurrenceParams p
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
           gate<T>(zf[v], a[j][v], g[j][v]);
-          const float off = xf[v] - s[v];
-          w[j][v] = -off * (a[j][v] * g[j][v]);
-          s[v] = __builtin_fmaf(g[j][v], off, s[v]);
+          const float in = g[j][v] * xf[v];
+          // (h - x) a g, the difference of the products: that of h and x may be past the floats
+          w[j][v] = __builtin_fmaf(a[j][v] * g[j][v], s[v], -(a[j][v] * in));
+          s[v] = __builtin_fmaf(a[j][v], s[v], in);
         }
+        if (j == kSteps / 2 - 1) __builtin_amdgcn_sched_barrier(0);  // as in net_recurrence
       }
       Rows<T, VEC> d = ds;
       if (i > 0) load(i - 1);
@@ -449,7 +596,7 @@ __global__ __launch_bounds__(64 * W) void net_recurrence_grad(RecurrenceParams p
       board.put(set, wave, lane, A, S);
       __syncthreads();  // one to a tile: the other set is written before the next
       float in[VEC];
-      board.template compose<true>(set, wave, lane, carry, in);
+      board.compose(set, wave, lane, carry, in);
       const RowStore<T, VEC, W> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
 #pragma unroll
       for (int j = kSteps - 1; j >= 0; --j) {

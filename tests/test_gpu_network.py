@@ -259,6 +259,127 @@ def test_recurrence_in_pieces(torch, pkg, D):  # noqa: F811
         close(s, want_last, e["last"] + ONE * np.abs(want_last), "last")
 
 
+def decayed_bounds(x, z, h0, dh=None, dlast=None):
+    """Error bounds of h and dz that forget what the recurrence forgets, in units of what each step adds up.
+
+    M_t = a_t M_{t-1} + (1 - a_t) |x_t|, M_{-1} = |h0|.  A step's difference, product and sum are rounded at the size of
+    a |h| or (1 - a) |x| (2^-24 each) and its gate is off by GATE of itself, so it adds at most 2 GATE M_t; a run of
+    steps joined to the state before it adds a few roundings more (product, complement, sum: each off by GATE + 2^-24
+    of itself a step).  4 GATE M_t covers both: e_t = a_t e_{t-1} + 4 GATE M_t.  dz_t = s (h_{t-1} - x) a (1 - a): the
+    error of s as in recurrence_bounds, against M_{t-1} + |x|."""
+    B, L, D = x.shape
+    e = {k: np.zeros(x.shape) for k in ("h", "dz")}
+    for b in range(B):
+        a, g = R._sigmoid(z[b]), R._sigmoid(-z[b])
+        m, err = np.abs(h0[b]).astype(np.float64), np.zeros(D)
+        before = []
+        for t in range(L):
+            before.append((m, err))
+            m = a[t] * m + g[t] * np.abs(x[b, t])
+            err = a[t] * err + 4.0 * GATE * m
+            e["h"][b, t] = err
+        if dh is None:
+            continue
+        s, r = np.abs(dlast[b]), np.zeros(D)
+        for t in range(L - 1, -1, -1):
+            s = s + np.abs(dh[b, t])
+            r = r + s
+            size = before[t][0] + np.abs(x[b, t])
+            e["dz"][b, t] = a[t] * g[t] * (size * (4.0 * GATE * r + 8.0 * GATE * s) + s * before[t][1])
+            s, r = a[t] * s, a[t] * r
+    return e
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,D", [(2, 1, 40), (3, 8, 9), (3, 70, 66), (2, 300, 24), (1, 2500, 33), (500, 90, 40)])
+def test_recurrence_after_a_reset(torch, pkg, B, L, D, dtype):  # noqa: F811
+    """States and inputs of many sizes, gates from wide open to shut: what a shut gate lets in keeps its digits."""
+    rng = np.random.Generator(np.random.PCG64(40 + L))
+    sizes = 10.0 ** rng.uniform(-4, 4, size=(B, L, D)) * rng.choice([-1.0, 1.0], size=(B, L, D))
+    sizes[:, ::5] *= np.where(rng.random((B, (L + 4) // 5, D)) < 0.3, 5.0, 1.0)
+    x, xd = rounded(torch, sizes, dtype)
+    z, zd = rounded(torch, rng.standard_normal((B, L, D)) * 14.0, dtype)
+    h0 = (10.0 ** rng.uniform(-4, 8, size=(B, D)) * rng.choice([-1.0, 1.0], size=(B, D))).astype(np.float32)
+    dh, dhd = rounded(torch, rng.standard_normal((B, L, D)), dtype)
+    dlast, dlastd = rounded(torch, rng.standard_normal((B, D)), "f32")
+    h0t = torch.from_numpy(h0).to("cuda")
+    x.requires_grad_(True)
+    z.requires_grad_(True)
+    h, last = pkg.gated_recurrence(x, z, h0t)
+    dx, dz = torch.autograd.grad((h, last), (x, z), (dh, dlast))
+    few = slice(0, 6)  # oracle's share
+    xd, zd, h0, dhd, dlastd = (v[few] for v in (xd, zd, h0, dhd, dlastd))
+    want, want_last = R.gated_recurrence(xd, zd, h0)
+    e = decayed_bounds(xd, zd, h0, dhd, dlastd)
+    half, tiny = HALF[dtype], TINY[dtype] + 2.0 ** -90
+    over = np.abs(want) * (1 + half) >= float(torch.finfo(td(torch, dtype)).max)  # f16: past the largest value
+    got = h[few].detach().double().cpu().numpy()
+    assert np.array_equal(np.isinf(got), over)
+    close(torch.from_numpy(np.where(over, 0.0, got)), np.where(over, 0.0, want),
+          np.where(over, 0.0, e["h"] + half * np.abs(want)) + tiny, "h")
+    close(last[few], want_last, e["h"][:, -1] + ONE * np.abs(want_last) + tiny, "last")
+    wdx, wdz, _ = R.gated_recurrence_grad(xd, zd, dhd, dlastd, h0)
+    size = recurrence_bounds(xd, zd, h0, None, dhd, dlastd)["dx"]
+    close(dx[few], wdx, size + half * np.abs(wdx) + tiny, "dx")
+    fits = np.abs(wdz) < 0.99 * float(torch.finfo(td(torch, dtype)).max)
+    close(torch.where(torch.from_numpy(fits).cuda(), dz[few], torch.zeros_like(dz[few])), np.where(fits, wdz, 0.0),
+          np.where(fits, e["dz"] + half * np.abs(wdz), 0.0) + tiny, "dz")
+
+
+@pytest.mark.parametrize("B,L", [(2, 5), (2, 60), (3, 700), (1, 3000), (600, 60)])
+def test_recurrence_near_the_ends_of_float32(torch, pkg, B, L):  # noqa: F811
+    """Differences past the largest float, infinite inputs and states, NaN."""
+    rng = np.random.Generator(np.random.PCG64(50 + L))
+    inf = np.inf
+    D = 70
+    x = np.where(rng.random((B, L, D)) < 0.5, 3.0e38, -3.0e38) * rng.uniform(0.5, 1.0, size=(B, L, D))
+    z = rng.standard_normal((B, L, D)) * 3.0
+    h0 = np.where(rng.random((B, D)) < 0.5, 3.0e38, -3.0e38)
+    x[:, :, 8:] = rng.standard_normal((B, L, D - 8))
+    at = lambda k: min(k, L - 1)  # noqa: E731
+    x[:, at(3), 10] = inf
+    x[:, at(3), 11], x[:, at(40), 11] = inf, -inf
+    x[:, at(2), 12] = np.nan
+    x[:, at(650), 13] = -inf
+    h0[:, 8:] = rng.standard_normal((B, D - 8))
+    h0[:, 14], h0[:, 15], h0[:, 16] = inf, -inf, np.nan
+    z[:, :, 15] = -12.0
+    z[:, :, 17], h0[:, 17] = 12.0, inf
+    z[:, :, 18] = -100.0  # sigmoid is below the floats
+    h0[:, 18] = inf
+    (x, xd), (z, zd), (h0t, h0) = (rounded(torch, v, "f32") for v in (x, z, h0))
+    x.requires_grad_(True)
+    z.requires_grad_(True)
+    h, last = pkg.gated_recurrence(x, z, h0t)
+    dx, dz = torch.autograd.grad(h, (x, z), torch.full_like(h, 0.01))
+    few = slice(0, 4)
+    with np.errstate(all="ignore"):
+        want, want_last = R.gated_recurrence(xd[few], zd[few], h0[few])
+        wdx, wdz, _ = R.gated_recurrence_grad(xd[few], zd[few], np.full(want.shape, 0.01), None, h0[few])
+        e = decayed_bounds(xd[few], zd[few], h0[few], np.full(want.shape, 0.01), np.zeros(want_last.shape))
+    for name, got, w, tol in (("h", h, want, e["h"]), ("last", last, want_last, e["h"][:, -1])):
+        g = got[few].detach().double().cpu().numpy()
+        for kind in (np.isnan, np.isposinf, np.isneginf):
+            assert np.array_equal(kind(g), kind(w)), (name, kind.__name__, np.argwhere(kind(g) != kind(w))[:5])
+        ok = np.isfinite(w)
+        assert np.all(np.abs(g[ok] - w[ok]) <= tol[ok] + ONE * np.abs(w[ok]) + 2.0 ** -90), name
+    g, ok = dz[few].double().cpu().numpy(), np.isfinite(wdz)
+    assert np.array_equal(np.isfinite(g), ok)
+    assert np.all(np.abs(g[ok] - wdz[ok]) <= e["dz"][ok] + ONE * np.abs(wdz[ok]) + 2.0 ** -90)
+
+
+@pytest.mark.parametrize("B,L", [(1, 60000), (700, 2000)])
+def test_recurrence_holds_its_value(torch, pkg, B, L):  # noqa: F811
+    """x = h0 = 1 stays at 1 however long the gates remember.  A run of eight steps goes towards S / (1 - P), which is 1
+    up to eight roundings of S and of 1 - P (2^-24 each) and the gates' errors in common: within 2^-20 of 1."""
+    x = torch.ones((B, L, 64), device="cuda")
+    z = torch.tensor([10.0, 16.0, 3.0, 0.5, 0.0, -3.0, 7.0, 20.0], device="cuda").repeat(8).expand(B, L, 64)
+    h, last = pkg.gated_recurrence(x, z, torch.ones((B, 64), device="cuda"))
+    assert float((h - 1.0).abs().max()) <= 2.0 ** -20 and float((last - 1.0).abs().max()) <= 2.0 ** -20
+    step, s = pkg.gated_recurrence(x[:, :8], z[:, :8], torch.ones((B, 64), device="cuda"))
+    assert bool((step == 1).all()) and bool((s == 1).all())
+
+
 def test_gradients_with_saved_tensors_on_the_host(torch, pkg):  # noqa: F811
     """Saved tensors that come back in another layout (views of a projection do) give the same gradients."""
     g = torch.Generator(device="cuda").manual_seed(17)
