@@ -27,15 +27,24 @@ struct Workspace {
     ptr = static_cast<char*>(given);
     if (ptr || need == 0) return RNNT_OK;
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(stream, &capture) != hipSuccess) return RNNT_ERR_HIP;
+    if (hipStreamIsCapturing(stream, &capture) != hipSuccess) return failed();
     if (capture != hipStreamCaptureStatusNone) return RNNT_ERR_WORKSPACE;
-    if (hipMallocAsync(&owned_, need, stream) != hipSuccess) return RNNT_ERR_HIP;
+    if (hipMallocAsync(&owned_, need, stream) != hipSuccess) {
+      owned_ = nullptr;
+      return failed();
+    }
     stream_ = stream;
     ptr = static_cast<char*>(owned_);
     return RNNT_OK;
   }
 
  private:
+  // the error is this call's status: it is not left for the check behind the next launch to find
+  static rnnt_status_t failed() {
+    (void)hipGetLastError();
+    return RNNT_ERR_HIP;
+  }
+
   void* owned_ = nullptr;
   hipStream_t stream_ = nullptr;
 };

@@ -173,3 +173,18 @@ def test_captured_autograd_loss(torch, pkg):  # noqa: F811
         want = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_refused_allocation_is_not_the_next_calls_error(torch, pkg):  # noqa: F811
+    """A workspace of 8.8 TB, which the runtime refuses, is this call's status 8; the next call is not told of it."""
+    net = pkg.network
+    lib = net._library()
+    x = torch.ones(1 << 12, dtype=torch.bfloat16, device="cuda")
+    lens = torch.ones(16, dtype=torch.int32, device="cuda")
+    huge = net.JointShape(16, 8191, (1 << 18) - 1, 1024, 1)
+    assert lib.rnnt_joint_hidden_grad_workspace_bytes(huge) > 1 << 42
+    p, q, stream = x.data_ptr(), lens.data_ptr(), torch.cuda.current_stream().cuda_stream
+    torch.cuda.synchronize()
+    assert lib.rnnt_joint_hidden_grad(p, p, huge, q, q, 0, 0.0, None, p, p, p, None, 0, stream) == 8
+    y = pkg.dropout(x, 0.0, torch.zeros(2, dtype=torch.int64, device="cuda"))
+    assert torch.equal(x, y)
