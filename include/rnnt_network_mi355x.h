@@ -49,7 +49,8 @@ extern "C" {
  *
  * RNNT_ERR_BAD_SHAPE: B < 1, N < 0, V < 1, D < 1 or start outside [-1, V).
  * RNNT_ERR_UNSUPPORTED: more than 2^31 - 2^16 - 1 rows in the output, or D > 2^30; in the
- * gradient, (rows + 2 V) times the KB of a row, rounded up, of about 2^28 or more.
+ * gradient, (rows + 2 V) times the KB of a row, rounded up, of about 2^28 or more.  The
+ * workspace's size is 0 for a shape that the gradient refuses.
  */
 typedef struct {
   int32_t B, N, V, D;
@@ -143,10 +144,14 @@ rnnt_status_t rnnt_dropout(const void* x, int64_t n, rnnt_dtype_t dtype, double 
  * in a fixed order.
  *
  * logit_lens outside [0, T_max] or label_lens outside [0, U_max] is a bad length.
- * RNNT_ERR_BAD_SHAPE: B < 1, T_max < 1, U_max < 0, H < 1 (or 2^31 or more rows of
- * an utterance).  RNNT_ERR_BAD_VARIANT: unknown activation, p outside [0, 1).
- * RNNT_ERR_UNSUPPORTED: B * T_max or B * (U_max+1) of about 2^23 or more, or 2^29 or
- * more elements of an utterance's pred.
+ * RNNT_ERR_BAD_SHAPE: B < 1, T_max < 1, U_max < 0, H outside [1, 2^20], 2^31 or more
+ * rows (t, u) of an utterance, or more than 2^40 rows.  RNNT_ERR_BAD_VARIANT: unknown
+ * activation, p outside [0, 1).
+ * RNNT_ERR_UNSUPPORTED, forward: B * T_max or B * (U_max+1) of 2^31 or more,
+ * B * ceil(T_max / 4) of 2^23 or more, or an utterance's pred of about 2^30 elements or
+ * more.  Gradient: B * ceil(T_max / 16) (8 in float32) times ceil(H / 120) of 2^23 or
+ * more, B * (U_max+1) * H of about 2^33 or more (2^31, H < 8), or an utterance's pred of
+ * 2^29 elements or more; its workspace's size is 0 for such a shape.
  */
 typedef enum { RNNT_ACT_RELU = 0, RNNT_ACT_TANH = 1 } rnnt_activation_t;
 

@@ -403,6 +403,23 @@ int lanes_for(int groups) {
   return n;
 }
 
+// The gradient's grids: a wave to a run or to weight rows, times tiles of 64 groups of channels.
+struct GradGrid {
+  int vec, tiles;
+  int64_t runs, run_items, row_blocks;
+
+  explicit GradGrid(const rnnt_embedding_shape_t& s, int64_t rows) {
+    const int wide = static_cast<int>(16 / net_elem_bytes(s.dtype));
+    vec = s.D >= wide ? wide : 1;
+    tiles = (s.D - 1) / (64 * vec) + 1;
+    runs = (rows + kRun - 1) / kRun;
+    run_items = runs * tiles;
+    const int64_t row_waves = (static_cast<int64_t>(s.V) + kRowsToWave - 1) / kRowsToWave * tiles;
+    row_blocks = (row_waves + 3) / 4;
+  }
+  bool fits() const { return row_blocks + run_items <= kMaxRows / 256; }
+};
+
 // Workspace of the gradient, 256-byte aligned pieces.
 struct GradLayout {
   size_t keys, sorted, tokens, first, sums, total;
@@ -466,7 +483,8 @@ size_t rnnt_label_embedding_grad_workspace_bytes(rnnt_embedding_shape_t shape) {
   TokenSource src;
   int32_t any;
   if (check(&any, shape, &src, nullptr) != RNNT_OK) return 0;
-  return grad_layout(shape, static_cast<int64_t>(src.n1) * shape.B).total;
+  const int64_t rows = static_cast<int64_t>(src.n1) * shape.B;
+  return GradGrid(shape, rows).fits() ? grad_layout(shape, rows).total : 0;
 }
 
 rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* lens, rnnt_embedding_shape_t shape,
@@ -479,13 +497,11 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
   if (!dweight || (!dout && p.rows > 0)) return RNNT_ERR_NULL_PTR;
   const int64_t e = net_elem_bytes(shape.dtype);
   if (!multiple_of(e, dout) || !multiple_of(e, dweight)) return RNNT_ERR_ALIGNMENT;
-  // every grid of the call before its first launch: a wave to a run or to weight rows, times tiles of 64 groups
-  const int wide = static_cast<int>(16 / e), vec = shape.D >= wide ? wide : 1;
-  p.tiles = (shape.D - 1) / (64 * vec) + 1;
-  p.runs = static_cast<int32_t>((static_cast<int64_t>(p.rows) + kRun - 1) / kRun);
-  const int64_t run_items = static_cast<int64_t>(p.runs) * p.tiles;
-  const int64_t row_waves = (static_cast<int64_t>(shape.V) + kRowsToWave - 1) / kRowsToWave * p.tiles, row_blocks = (row_waves + 3) / 4;
-  if (row_blocks + run_items > kMaxRows / 256) return RNNT_ERR_UNSUPPORTED;
+  const GradGrid cut(shape, p.rows);
+  if (!cut.fits()) return RNNT_ERR_UNSUPPORTED;
+  p.tiles = cut.tiles;
+  p.runs = static_cast<int32_t>(cut.runs);
+  const int64_t run_items = cut.run_items, row_blocks = cut.row_blocks;
   const GradLayout L = grad_layout(shape, p.rows);
   Workspace ws;
   st = ws.take(workspace, workspace_bytes, L.total, stream);
@@ -523,7 +539,7 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
                          static_cast<int32_t>(row_blocks));
       return launched();
     };
-    return vec > 1 ? rest(std::integral_constant<int, 16 / sizeof(T)>{}) : rest(std::integral_constant<int, 1>{});
+    return cut.vec > 1 ? rest(std::integral_constant<int, 16 / sizeof(T)>{}) : rest(std::integral_constant<int, 1>{});
   });
 }
 

@@ -595,7 +595,17 @@ struct GradShape {
   }
 };
 
+// The gradient's grids and its buffers of sums (a block's is one of less than 2^31 bytes), whatever p is.
+bool grad_fits(const rnnt_joint_shape_t& s) {
+  const GradShape cut(s, true);
+  const int64_t U1 = static_cast<int64_t>(s.U_max) + 1;
+  const int64_t x = static_cast<int64_t>(s.B) * cut.t_blocks * cut.slices;
+  const int64_t joins = (s.B * U1 * (s.H < 8 ? s.H : (s.H + 3) / 4) + 255) / 256;
+  return x <= kMaxRows / 256 && joins <= kMaxRows / 256 && U1 * s.H < (int64_t{1} << 29);
+}
+
 size_t grad_bytes(const rnnt_joint_shape_t& s) {
+  if (!grad_fits(s)) return 0;
   const GradShape cut(s, true);  // the same whatever p is
   return net_align256(static_cast<size_t>(s.B) * cut.t_blocks * (static_cast<size_t>(s.U_max) + 1) * s.H * sizeof(float));
 }
@@ -699,8 +709,9 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
   if (!multiple_of(e, enc) || !multiple_of(e, pred) || !multiple_of(e, dh) || !multiple_of(e, denc) ||
       !multiple_of(e, dpred) || !multiple_of(8, rng))
     return RNNT_ERR_ALIGNMENT;
+  if (!grad_fits(shape)) return RNNT_ERR_UNSUPPORTED;
   Workspace ws;
-  st = ws.take(workspace, workspace_bytes, rnnt_joint_hidden_grad_workspace_bytes(shape), stream);
+  st = ws.take(workspace, workspace_bytes, grad_bytes(shape), stream);
   if (st != RNNT_OK) return st;
   q.enc = enc;
   q.pred = pred;
@@ -721,10 +732,7 @@ rnnt_status_t rnnt_joint_hidden_grad(const void* enc, const void* pred, rnnt_joi
   q.slices = cut.slices;
   q.tile_frames = cut.tile_frames;
   const int64_t x = static_cast<int64_t>(shape.B) * q.t_blocks * q.slices;
-  const int64_t joins = (static_cast<int64_t>(shape.B) * q.U1 * (shape.H < 8 ? shape.H : (shape.H + 3) / 4) + 255) / 256;
-  // a block's sums are one buffer of less than 2^31 bytes
-  if (x > kMaxRows / 256 || joins > kMaxRows / 256 || static_cast<int64_t>(q.U1) * shape.H >= (int64_t{1} << 29))
-    return RNNT_ERR_UNSUPPORTED;
+  const int64_t joins = (static_cast<int64_t>(shape.B) * q.U1 * ((shape.H + 3) / 4) + 255) / 256;
   return with_dtype(shape.dtype, [&](auto t) {
     using T = decltype(t);
     if (shape.H < 8) {

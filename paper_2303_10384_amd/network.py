@@ -128,12 +128,22 @@ def _dense(*saved):
     return (None if t is None else t.contiguous() for t in saved)
 
 
+def _check_gradient(shape_and_bytes, *sizes):
+    """A step whose gradient would be refused, for which its workspace's size is 0, is refused before it starts (an
+    empty tensor is left to the forward call's own error)."""
+    shape, nbytes = shape_and_bytes
+    if not nbytes and 0 not in sizes:
+        raise RNNTError(RNNT_ERR_UNSUPPORTED, "gradient of %s" % type(shape).__name__)
+
+
 # ---------------------------------------------------------------- label embedding
 
-def _embedding_forward(labels, weight, lens, scale, start):
+def _embedding_forward(labels, weight, lens, scale, start, for_gradient=False):
     B, N = labels.shape
     V, D = weight.shape
     shape = _shape(EmbeddingShape, "rnnt_label_embedding_grad_workspace_bytes", B, N, V, D, start, dtype_code(weight.dtype))
+    if for_gradient:
+        _check_gradient(shape, B, V, D)
     out = torch.empty((B, N + (start >= 0), D), dtype=weight.dtype, device=weight.device)
     _call(_library().rnnt_label_embedding, weight.device, _ptr(labels), _ptr(lens), shape[0], _ptr(weight), scale,
           _ptr(out))
@@ -143,7 +153,7 @@ def _embedding_forward(labels, weight, lens, scale, start):
 class _LabelEmbedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, labels, weight, lens, scale, start):
-        out, ctx.shape = _embedding_forward(labels, weight, lens, scale, start)
+        out, ctx.shape = _embedding_forward(labels, weight, lens, scale, start, ctx.needs_input_grad[1])
         ctx.scale = scale
         ctx.save_for_backward(labels, lens)
         return out
@@ -299,10 +309,12 @@ def dropout(x, p, rng):
 
 # ---------------------------------------------------------------- the joint's hidden layer
 
-def _joint_forward(enc, pred, logit_lens, label_lens, act, p, rng, rng_out=None):
+def _joint_forward(enc, pred, logit_lens, label_lens, act, p, rng, rng_out=None, for_gradient=False):
     B, T, H = enc.shape
     U1 = pred.shape[1]
     shape = _shape(JointShape, "rnnt_joint_hidden_grad_workspace_bytes", B, T, U1 - 1, H, dtype_code(enc.dtype))
+    if for_gradient:
+        _check_gradient(shape, B, T, U1, H)
     h = torch.empty((B, T, U1, H), dtype=enc.dtype, device=enc.device)
     _call(_library().rnnt_joint_hidden, enc.device, _ptr(enc), _ptr(pred), shape[0], _ptr(logit_lens), _ptr(label_lens),
           act, p, _ptr(rng), _ptr(rng_out), _ptr(h))
@@ -314,7 +326,8 @@ class _JointHidden(torch.autograd.Function):
     def forward(ctx, enc, pred, logit_lens, label_lens, act, p, rng):
         ctx.act, ctx.p = act, p
         used = None if rng is None else torch.empty_like(rng)
-        h, ctx.shape = _joint_forward(enc, pred, logit_lens, label_lens, act, p, rng, used)
+        h, ctx.shape = _joint_forward(enc, pred, logit_lens, label_lens, act, p, rng, used,
+                                      any(ctx.needs_input_grad[:2]))
         ctx.save_for_backward(enc, pred, logit_lens, label_lens, used)
         return h
 
