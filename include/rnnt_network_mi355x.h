@@ -8,8 +8,9 @@
  * Conventions are those of rnnt_mi355x.h: device pointers unless a comment says
  * otherwise, work queued on `stream`, no synchronisation, no state kept between
  * calls, host-visible errors return a status and launch nothing.  In addition
- *   - tensors need the alignment of their elements only; rows and pointers that
- *     are multiples of 16 bytes take wider loads and stores.
+ *   - tensors need the alignment of their elements only; accesses are as wide at
+ *     any address, and fastest where rows and pointers are multiples of 16 bytes.
+ *   - outputs share no memory with inputs or with one another, unless a call says so.
  *   - lengths are (B) int32; rows behind a length are never used (they may hold
  *     anything, NaN included) and are exactly 0 in every output.  A length
  *     outside its range, seen on the device, gives NaN in that utterance's
@@ -92,7 +93,8 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
  * Only long sequences that are few need a workspace (0 bytes: none).
  *
  * RNNT_ERR_BAD_SHAPE: B < 1, L < 0, D < 1, or a stride below 0.
- * RNNT_ERR_UNSUPPORTED: L > 2^30, D > 2^21, or B * ceil(D / 64) of 2^21 or more.
+ * RNNT_ERR_UNSUPPORTED: L > 2^30, D > 2^21, or B * ceil(D / 64) of 2^21 or more; h0 and
+ * last_out, or dlast and dh0, that share memory (a streaming caller keeps two states in turn).
  */
 #define RNNT_RECURRENCE_STATE_STEPS 8
 

@@ -631,6 +631,14 @@ rnnt_status_t check(const rnnt_recurrence_shape_t& s) {
   return RNNT_OK;
 }
 
+// Whether two (B, D) float32 states share memory: blocks write the one while others, of later segments or of the next
+// channels (which begin early in a row that is no multiple of a block's), still read the other.
+bool overlap(const float* a, const float* b, const rnnt_recurrence_shape_t& s) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a), bt = reinterpret_cast<uintptr_t>(b);
+  const uintptr_t bytes = static_cast<uintptr_t>(s.B) * s.D * sizeof(float);
+  return a && b && (at < bt ? bt - at : at - bt) < bytes;
+}
+
 int state_count(int L) { return static_cast<int>((static_cast<int64_t>(L) + kSteps - 1) / kSteps); }
 
 // Blocks to a sequence: one, or as many segments of at least two tiles as give the chip a block to a CU.
@@ -724,6 +732,7 @@ rnnt_status_t rnnt_recurrence(const void* x, const void* z, rnnt_recurrence_shap
   Workspace ws;
   st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
+  if (overlap(h0, last_out, shape)) return RNNT_ERR_UNSUPPORTED;
   RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);
   p.h0 = h0;
   p.h = h_out;
@@ -762,6 +771,7 @@ rnnt_status_t rnnt_recurrence_grad(const void* x, const void* z, rnnt_recurrence
   Workspace ws;
   st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
+  if (overlap(dlast, dh0, shape)) return RNNT_ERR_UNSUPPORTED;
   RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);
   p.states = const_cast<float*>(static_cast<const float*>(states));
   p.dh = dh;

@@ -316,3 +316,13 @@ def test_gradients_past_a_launch_are_refused_before_the_forward_call(net, calls)
     bwd = {"enc": FAKE, "pred": FAKE, "shape": net.JointShape(1024, 16384, 0, 16384, 1), "tl": FAKE, "ul": FAKE, "act": 0,
            "p": 0.5, "rng": FAKE, "dh": FAKE, "denc": FAKE, "dpred": FAKE, "ws": None, "bytes": 0, "stream": None}
     assert call(lib.rnnt_joint_hidden_grad, bwd, {}) == 9  # and no workspace is taken for it
+
+
+def test_recurrence_states_in_place_are_refused(net):
+    """Blocks that write the state would meet blocks that still read it."""
+    lib = net._library()
+    shape = net.RecurrenceShape(2, 8, 129, 1, 1032, 129, 1032, 129)  # needs no workspace
+    size = 2 * 129 * 4
+    for off in (0, 4, -4, size - 4, 4 - size):
+        assert lib.rnnt_recurrence(FAKE, FAKE, shape, FAKE, FAKE, FAKE, FAKE + off, None, None, 0, None) == 9
+        assert lib.rnnt_recurrence_grad(FAKE, FAKE, shape, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE + off, None, 0, None) == 9
