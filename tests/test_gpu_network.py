@@ -139,6 +139,30 @@ def test_embedding_gradient_of_many_rows(torch, pkg):  # noqa: F811
     assert torch.equal(dw.double().cpu(), want)
 
 
+@pytest.mark.parametrize("dtype,D,N", [("bf16", 257, 4100), ("f16", 33, 32000), ("f32", 130, 4100), ("bf16", 5, 210000)])
+def test_embedding_stored_past_the_caches(torch, pkg, dtype, D, N):  # noqa: F811
+    """Results of 128 MB and more, with rows that are no multiple of 16 bytes and a weight off 16 bytes: every row has
+    the bits of its weights times the scale, rounded once."""
+    g = torch.Generator(device="cuda").manual_seed(D)
+    B, V = 64, 50
+    base = torch.randn(V * D + 1, device="cuda", generator=g).to(td(torch, dtype))
+    weight = base[1:].view(V, D)
+    labels = torch.randint(0, V, (B, N), device="cuda", generator=g).to(torch.int32)
+    lens = torch.randint(0, N + 1, (B,), device="cuda", generator=g).to(torch.int32)
+    labels[3, 0], lens[3], lens[5] = V, N, -1  # a bad label and a bad length
+    out = pkg.label_embedding(labels, weight, lens, scale=1.75)
+    assert out.numel() * out.element_size() >= 1 << 27
+    rows = (weight.float() * 1.75).to(weight.dtype)
+    for b in range(B):
+        n = int(lens[b])
+        if b == 5:
+            assert bool(out[b].isnan().all())
+            continue
+        first = 1 if b == 3 else 0
+        assert torch.equal(out[b, first:n], rows[labels[b, first:n].long()]) and bool((out[b, n:] == 0).all())
+    assert bool(out[3, 0].isnan().all())
+
+
 # ---------------------------------------------------------------- gated recurrence
 
 RECURRENCE = [  # B, L, D, lengths, h0, layout
@@ -640,6 +664,50 @@ def test_recurrence_of_many_sequences(torch, pkg):  # noqa: F811
                 want = a.double().cpu().numpy()
                 # two orders of one sum
                 close(b[0], want, 2 * e[name] + 2 * HALF[dtype if name != "last" else "f32"] * np.abs(want) + 2.0 ** -120, name)
+
+
+@pytest.mark.parametrize("act", ["relu", "tanh"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("p", [0.0, 0.3])
+@pytest.mark.parametrize("B,T,U,H", [(2050, 3, 1, 7), (2050, 3, 1, 24), (1030, 6, 2, 9), (1030, 6, 2, 24), (520, 13, 0, 33),
+                                     (1024, 5, 0, 4001), (1, 2, 1, 15001)])
+def test_joint_of_blocks_of_frames(torch, pkg, B, T, U, H, p, dtype, act):  # noqa: F811
+    """Launches of enough blocks take four frames to a block, the last one fewer; the last two cases' rows do not fit
+    LDS.  Against float64 on the GPU, with the mask of dropout (its numbers are checked elsewhere, and here again for
+    some utterances)."""
+    g = torch.Generator(device="cuda").manual_seed(B + H)
+    t = td(torch, dtype)
+    enc, pred = (torch.randn((B, n, H), device="cuda", generator=g).to(t) for n in (T, U + 1))
+    dh = torch.randn((B, T, U + 1, H), device="cuda", generator=g).to(t)
+    tl = torch.randint(0, T + 1, (B,), device="cuda", generator=g).to(torch.int32)
+    ul = torch.randint(0, U + 1, (B,), device="cuda", generator=g).to(torch.int32)
+    tl[0], ul[0] = T, U
+    valid = ((torch.arange(T, device="cuda")[None, :, None] < tl[:, None, None])
+             & (torch.arange(U + 1, device="cuda")[None, None] <= ul[:, None, None]))[..., None]
+    dh = torch.where(valid, dh, torch.full_like(dh, float("nan")))
+    enc.requires_grad_(True)
+    pred.requires_grad_(True)
+    h = pkg.joint_hidden(enc, pred, tl, ul, act, p, rng_of(torch, 11, 12) if p else None)
+    denc, dpred = torch.autograd.grad(h, (enc, pred), dh)
+    keep = pkg.dropout(torch.ones(h.shape, device="cuda"), p, rng_of(torch, 11, 12)) if p else torch.ones((), device="cuda")
+    if p:
+        for b in (0, B - 1):
+            n = T * (U + 1) * H
+            assert np.array_equal((keep[b] != 0).cpu().numpy().reshape(-1)[:999], R.keep_mask((n,), p, 11, 12, b * n)[:999])
+    scale = torch.where(keep != 0, 65536.0 / (65536 - R.threshold(p)), 0.0).double()
+    s = enc.detach().double()[:, :, None] + pred.detach().double()[:, None]
+    value, slope = (s.tanh(), 1.0 / s.cosh() ** 2) if act == "tanh" else (s.clamp(min=0.0), (s > 0).double())
+    zero = torch.zeros((), dtype=torch.float64, device="cuda")
+    want = torch.where(valid, value * scale, zero)
+    half, tiny = HALF[dtype], TINY[dtype]
+    # as in test_joint
+    assert bool(((h.double() - want).abs() <= (half + 2.0 ** -20 + 2 * ONE) * want.abs() + tiny).all())
+    assert bool((h.detach()[(~valid).expand(h.shape)] == 0).all())
+    w = torch.where(valid, slope * scale * torch.nan_to_num(dh.double()), zero)
+    for got, dim, n in ((denc, 2, U + 1), (dpred, 1, T)):
+        want, size = w.sum(dim), w.abs().sum(dim)
+        tol = half * want.abs() + (2.0 ** -20 + 10 * 2.0 ** -23 + (n + 3) * ONE) * size + tiny
+        assert bool(((got.double() - want).abs() <= tol).all()), dim
 
 
 def test_joint_past_32_bits(torch, pkg):  # noqa: F811
