@@ -228,25 +228,38 @@ struct Activation;
 
 template <>
 struct Activation<RNNT_ACT_RELU> {
+  template <typename T>
   __device__ static __forceinline__ float value(float s) { return s < 0.f ? 0.f : s; }  // NaN stays
   __device__ static __forceinline__ float slope(float s) { return s > 0.f ? 1.f : 0.f; }
 };
 
-// tanh s = 1 - 2 / (1 + e^2s), which ends at -1 and 1 whatever overflows; below 0.3, where the
-// difference loses digits, the odd series through s^9 (the next term is 5e-8 of the value there).  Its slope
-// is 4u / (1 + u)^2 with u = e^-2|s|.  The rounding of the exponent, 2|s| 2^-24 of the exponential, needs no
-// correction: where it grows, little of the value is left to it, and in the slope it is what the rounding of s
-// itself costs.
+// tanh s = 1 - 2 / (1 + e^2s), which ends at -1 and 1 whatever overflows; near 0, where the difference loses
+// digits, an odd polynomial.  For float32 of |s|, as at negative s the quotient would be near 1 and its rounding
+// twice the value's, and from 0.6 on; the polynomial goes through s^11 (least relative error, 3e-9, fitted by
+// reweighted least squares).  For a result of 16 bits (h is rounded to 2^-12 or 2^-9) of s itself, and from 0.3 on,
+// through s^9: off by up to 8e-7, 271 -> 253 us for B=32 T=250 U=80 H=640 bf16 with dropout.  The slope is 4u / (1 + u)^2
+// with u = e^-2|s|.  The rounding of the exponent, 2|s| 2^-24 of the exponential, needs no correction: where it
+// grows, little of the value is left to it, and in the slope it is what the rounding of s itself costs.
 template <>
 struct Activation<RNNT_ACT_TANH> {
   __device__ static __forceinline__ float u_of(float s) { return fast_exp2(__builtin_fabsf(s) * (-2.f * kLog2eF)); }
+  template <typename T>
   __device__ static __forceinline__ float value(float s) {
-    const float q = s * s;
-    const float big = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * (2.f * kLog2eF))), 1.f);
-    float p = __builtin_fmaf(q, 62.f / 2835.f, -17.f / 315.f);
-    p = __builtin_fmaf(q, p, 2.f / 15.f);
-    p = __builtin_fmaf(q, p, -1.f / 3.f);
-    return __builtin_fabsf(s) < 0.3f ? __builtin_fmaf(q * p, s, s) : big;
+    constexpr bool F32 = sizeof(T) == 4;
+    const float q = s * s, y = F32 ? __builtin_fabsf(s) : s;
+    const float big = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(y * (2.f * kLog2eF))), 1.f);
+    float p;
+    if constexpr (F32) {
+      p = __builtin_fmaf(q, -5.895158276e-3f, 2.079597116e-2f);
+      p = __builtin_fmaf(q, p, -5.378383026e-2f);
+      p = __builtin_fmaf(q, p, 1.333192438e-1f);
+      p = __builtin_fmaf(q, p, -3.333329856e-1f);
+    } else {
+      p = __builtin_fmaf(q, 62.f / 2835.f, -17.f / 315.f);
+      p = __builtin_fmaf(q, p, 2.f / 15.f);
+      p = __builtin_fmaf(q, p, -1.f / 3.f);
+    }
+    return __builtin_fabsf(s) < (F32 ? 0.6f : 0.3f) ? __builtin_fmaf(q * p, s, s) : F32 ? __builtin_copysignf(big, s) : big;
   }
   __device__ static __forceinline__ float slope(float s) {
     const float u = u_of(s), r = __builtin_amdgcn_rcpf(1.f + u);

@@ -73,7 +73,7 @@ template <typename T, int ACT>
 __device__ __forceinline__ void joint_group(const float* e, const float* q, float scale, Pack<T, 8>& out) {
   float f[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = Activation<ACT>::value(e[i] + q[i]) * scale;
+  for (int i = 0; i < 8; ++i) f[i] = Activation<ACT>::template value<T>(e[i] + q[i]) * scale;
   out.set(f);
 }
 
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void net_joint_odd(JointParams p) {
           if (j + q >= 0 && j + q < total) {
             float v = valid < 0 ? __builtin_nanf("") : 0.f;
             if (j + q < valid && !(dropped >> q & 1u))
-              v = Activation<ACT>::value(ElemTraits<T>::load1(enc + cj) + ElemTraits<T>::load1(pred + j + q)) * p.drop.scale;
+              v = Activation<ACT>::template value<T>(ElemTraits<T>::load1(enc + cj) + ElemTraits<T>::load1(pred + j + q)) * p.drop.scale;
             ElemTraits<T>::store1(h + j + q, v);
           }
           if (++cj == p.H) cj = 0;

@@ -600,6 +600,24 @@ def test_joint_infinite_upstream_where_the_slope_is_zero(torch, pkg, act, H):  #
         assert bool((g == 0).all()) if act == "relu" else bool(g.isnan().all())
 
 
+def test_joint_tanh_keeps_float32s_digits(torch, pkg):  # noqa: F811
+    """tanh of float32 over its range.  Past 0.6 the value is 1 - 2r, r = 1 / (1 + E), E = e^2s: E is off by 2^-23 (the
+    exponential) and 2s 2^-24 (its argument), the sum by 2^-24 and r by 2^-23, so the value by
+    2r (E/(1+E) (2 + 2s) + 3) 2^-24 + 2^-25, which is largest at 0.6: 2.9e-7 of the value there.  Below, the
+    polynomial's 3e-9, and one rounding of its correction and of the result each: 2^-23."""
+    H = 1 << 14
+    s = torch.linspace(-9.0, 9.0, 64 * H, device="cuda").view(1, 64, H)
+    s[0, :8] = torch.linspace(-0.7, 0.7, 8 * H, device="cuda").view(8, H)
+    h = pkg.joint_hidden(s, torch.zeros((1, 1, H), device="cuda"), ints(torch, [64]), ints(torch, [0]), "tanh")
+    v = s[0].double().cpu().numpy()
+    want, got = np.tanh(v), h[0, :, 0].double().cpu().numpy()
+    y = np.abs(v)
+    E = np.exp(2 * y)
+    past = 2 / (1 + E) * (E / (1 + E) * (2 + 2 * y) + 3) * ONE + ONE
+    tol = np.where(y < 0.6, 2.0 ** -23 * np.abs(want) + 2.0 ** -126, past)
+    assert np.all(np.abs(got - want) <= tol), float(np.max(np.abs(got - want) / tol))
+
+
 def test_joint_bad_lengths(torch, pkg):  # noqa: F811
     for H in (24, 5):
         enc = torch.ones((5, 6, H), device="cuda", requires_grad=True)
