@@ -641,19 +641,25 @@ bool overlap(const float* a, const float* b, const rnnt_recurrence_shape_t& s) {
 
 int state_count(int L) { return static_cast<int>((static_cast<int64_t>(L) + kSteps - 1) / kSteps); }
 
-// Blocks to a sequence: one, or as many segments of at least two tiles as give the chip a block to a CU.
-// Segments read x and z twice (5/3 of the bytes forward, 7/5 backward), which pays up to half a chip of blocks: D=640
-// bf16 L=2000, forward and backward, one block and segments: 20 sequences (100 blocks) 63 + 82 us and 57 + 70,
-// 25 (125) 63 + 92 and 61 + 82, 32 (160) 63 + 102 and 104 + 133 (53 + 96 in one block with the pairs read 16 bytes at
-// a time, which the other figures came before).
-void segments_of(const rnnt_recurrence_shape_t& s, RecurrenceParams* p) {
+// Blocks to a sequence: one, or as many segments of at least two tiles as give the chip a block to a CU.  Segments read
+// x and z twice (backward: z and dh) and are two launches, so they pay where a sequence is long and blocks are few.
+// D=640 bf16, us in one block and in segments (pairs and states or gradients):
+//                        768 steps          896                1280               2000
+//   forward   5 blocks   23, 23             26, 28             36, 23
+//            80          25, 26             29, 31             39, 38             59, 51
+//           100, 125                        29, 37 (125)       40, 47 (125)       60, 62 (100)  61, 66 (125)
+//   backward  5          28, 19             33, 25             45, 19
+//            80          32, 26             36, 31             50, 40             79, 55
+//           125          34, 35             38, 42             55, 52             93, 82
+// At 160 blocks they lose both ways (2000 steps: 66, 113 and 99, 134).
+void segments_of(const rnnt_recurrence_shape_t& s, bool back, RecurrenceParams* p) {
   const int vec = s.dtype == RNNT_DTYPE_F32 || s.D < 2 ? 1 : 2;
   p->tiles = (s.D + 64 * vec - 1) / (64 * vec);
   const int64_t blocks = static_cast<int64_t>(s.B) * p->tiles, steps = (static_cast<int64_t>(s.L) + kTileSteps - 1) / kTileSteps;
   p->segments = 1;
   p->seg_steps = s.L;
-  if (blocks <= 128 && steps >= 4) {
-    int64_t want = 256 / blocks;
+  int64_t want = 256 / blocks;
+  if (want >= 3 ? steps >= (back ? 6 : 8) : back && want == 2 && steps >= 9) {
     if (want > steps / 2) want = steps / 2;
     const int64_t per = (steps + want - 1) / want;
     p->segments = static_cast<int32_t>((steps + per - 1) / per);
@@ -661,9 +667,9 @@ void segments_of(const rnnt_recurrence_shape_t& s, RecurrenceParams* p) {
   }
 }
 
-size_t pair_bytes(const rnnt_recurrence_shape_t& s) {
+size_t pair_bytes(const rnnt_recurrence_shape_t& s, bool back) {
   RecurrenceParams p{};
-  segments_of(s, &p);
+  segments_of(s, back, &p);
   return p.segments > 1 ? net_align256(static_cast<size_t>(s.B) * p.segments * s.D * sizeof(float2)) : 0;
 }
 
@@ -687,7 +693,8 @@ rnnt_status_t with_vector(const rnnt_recurrence_shape_t& s, F&& f) {
   });
 }
 
-RecurrenceParams params_of(const void* x, const void* z, const rnnt_recurrence_shape_t& s, const int32_t* lens, char* ws) {
+RecurrenceParams params_of(const void* x, const void* z, const rnnt_recurrence_shape_t& s, const int32_t* lens, bool back,
+                           char* ws) {
   RecurrenceParams p{};
   p.x = x;
   p.z = z;
@@ -701,7 +708,7 @@ RecurrenceParams params_of(const void* x, const void* z, const rnnt_recurrence_s
   p.D = s.D;
   p.n_states = state_count(s.L);
   p.pairs = reinterpret_cast<float2*>(ws);
-  segments_of(s, &p);
+  segments_of(s, back, &p);
   return p;
 }
 
@@ -717,7 +724,11 @@ size_t rnnt_recurrence_states_bytes(rnnt_recurrence_shape_t shape) {
   return static_cast<size_t>(shape.B) * state_count(shape.L) * shape.D * sizeof(float);
 }
 
-size_t rnnt_recurrence_workspace_bytes(rnnt_recurrence_shape_t shape) { return check(shape) == RNNT_OK ? pair_bytes(shape) : 0; }
+size_t rnnt_recurrence_workspace_bytes(rnnt_recurrence_shape_t shape) {
+  if (check(shape) != RNNT_OK) return 0;
+  const size_t forward = pair_bytes(shape, false), back = pair_bytes(shape, true);
+  return forward > back ? forward : back;
+}
 
 rnnt_status_t rnnt_recurrence(const void* x, const void* z, rnnt_recurrence_shape_t shape, const int32_t* lens,
                               const float* h0, void* h_out, float* last_out, void* states_out, void* workspace,
@@ -730,10 +741,10 @@ rnnt_status_t rnnt_recurrence(const void* x, const void* z, rnnt_recurrence_shap
       !multiple_of(4, last_out) || !multiple_of(16, states_out))
     return RNNT_ERR_ALIGNMENT;
   Workspace ws;
-  st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
+  st = ws.take(workspace, workspace_bytes, pair_bytes(shape, false), stream);
   if (st != RNNT_OK) return st;
   if (overlap(h0, last_out, shape)) return RNNT_ERR_UNSUPPORTED;
-  RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);
+  RecurrenceParams p = params_of(x, z, shape, lens, false, ws.ptr);
   p.h0 = h0;
   p.h = h_out;
   p.last = last_out;
@@ -769,10 +780,10 @@ rnnt_status_t rnnt_recurrence_grad(const void* x, const void* z, rnnt_recurrence
       !multiple_of(4, dlast) || !multiple_of(4, dh0) || !multiple_of(16, states))
     return RNNT_ERR_ALIGNMENT;
   Workspace ws;
-  st = ws.take(workspace, workspace_bytes, rnnt_recurrence_workspace_bytes(shape), stream);
+  st = ws.take(workspace, workspace_bytes, pair_bytes(shape, true), stream);
   if (st != RNNT_OK) return st;
   if (overlap(dlast, dh0, shape)) return RNNT_ERR_UNSUPPORTED;
-  RecurrenceParams p = params_of(x, z, shape, lens, ws.ptr);
+  RecurrenceParams p = params_of(x, z, shape, lens, true, ws.ptr);
   p.states = const_cast<float*>(static_cast<const float*>(states));
   p.dh = dh;
   p.dlast = dlast;

@@ -392,6 +392,30 @@ def test_recurrence_near_the_ends_of_float32(torch, pkg, B, L):  # noqa: F811
     assert np.all(np.abs(g[ok] - wdz[ok]) <= e["dz"][ok] + ONE * np.abs(wdz[ok]) + 2.0 ** -90)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L,D", [(100, 1153, 33), (128, 1200, 9), (85, 1025, 64), (60, 900, 64), (86, 1500, 40), (129, 1200, 9)])
+def test_recurrence_where_segments_begin(torch, pkg, B, L, D, dtype):  # noqa: F811
+    """Numbers of blocks and steps at which forward, backward or both are cut into segments; some sequences against
+    the reference."""
+    few = [0, 1, B - 1]
+    rng, x, z, xd, zd, h0, _ = recurrence_case(torch, B, L, D, None, True, "dense", dtype, 60)
+    lens = rng.integers(0, L + 1, size=B)
+    lens[0], lens[1], lens[B - 1] = L, L - 130, 129
+    x.requires_grad_(True)
+    z.requires_grad_(True)
+    h0t = torch.from_numpy(h0).to("cuda").requires_grad_(True)
+    h, last = pkg.gated_recurrence(x, z, h0t, ints(torch, lens))
+    dh, dhd = rounded(torch, rng.standard_normal((B, L, D)), dtype)
+    dlast, dlastd = rounded(torch, rng.standard_normal((B, D)), "f32")
+    got = (h, last) + torch.autograd.grad((h, last), (x, z, h0t), (dh, dlast))
+    xd, zd, h0, lens, dhd, dlastd = (v[few] for v in (xd, zd, h0, lens, dhd, dlastd))
+    wants = R.gated_recurrence(xd, zd, h0, lens) + R.gated_recurrence_grad(xd, zd, dhd, dlastd, h0, lens)
+    e = recurrence_bounds(xd, zd, h0, lens, dhd, dlastd)
+    for name, g, want in zip(("h", "last", "dx", "dz", "dh0"), got, wants):
+        t = "f32" if name in ("last", "dh0") else dtype
+        close(g[few], want, e[name] + HALF[t] * np.abs(want) + TINY[t], name)
+
+
 @pytest.mark.parametrize("B,L", [(1, 60000), (700, 2000)])
 def test_recurrence_holds_its_value(torch, pkg, B, L):  # noqa: F811
     """x = h0 = 1 stays at 1 however long the gates remember.  A run of eight steps goes towards S / (1 - P), which is 1
