@@ -75,8 +75,9 @@ rnnt_status_t rnnt_label_embedding_grad(const int32_t* labels, const int32_t* le
  * (h0 NULL).  h_out (B, L, D), last_out (B, D) float32: the state after the last
  * valid step (h0 where lens[b] = 0).  One step of a streaming decoder is L = 1.
  * Roundings have the size of a h and of (1 - a) x, so what a shut gate lets in keeps
- * its digits whatever the state that it drops.  An infinite x or state stays infinite
- * (in the forward pass a gate below 2^-126, 0 included, counts as 2^-126).
+ * its digits whatever the state that it drops.  An infinite x or state makes the states
+ * behind it infinite, or NaN where it meets the other infinity or a gate that is 0 in
+ * float32 (|z| of 88 and more).
  *
  * x and z may be views with contiguous channels: *_stride_b and *_stride_t are
  * in elements (halves of one projection, for instance); outputs are dense.

@@ -184,9 +184,9 @@ __device__ __forceinline__ void store_pair(Pack<T, 8> k, T* p) {
 
 // e^-y for y >= 0 within 2 ulp: the product with log2 e in two parts, so that a large y does
 // not cost its digits (|y| log2 e rounded alone would be off by up to 5e-6 of the result at
-// y = 80).  A y past `limit`, infinity included, gives e^-limit; NaN stays.
-__device__ __forceinline__ float exp_neg(float y, float limit) {
-  y = y > limit ? limit : y;
+// y = 80).  A y past 104, infinity included, gives 0; NaN stays.
+__device__ __forceinline__ float exp_neg(float y) {
+  y = y > 104.f ? 104.f : y;
   const float t = -y * kLog2eF;
   const float lo = __builtin_fmaf(-y, kLog2eF, -t) - y * 1.925963033500e-8f;  // log2 e - float(log2 e)
   const float r = fast_exp2(t);
@@ -199,27 +199,13 @@ __device__ __forceinline__ float exp_neg(float y, float limit) {
 template <typename T>
 __device__ __forceinline__ void gate(float z, float& a, float& g) {
   if constexpr (sizeof(T) == 4) {
-    const float e = exp_neg(__builtin_fabsf(z), 104.f), small = e * __builtin_amdgcn_rcpf(1.f + e), big = 1.f - small;
+    const float e = exp_neg(__builtin_fabsf(z)), small = e * __builtin_amdgcn_rcpf(1.f + e), big = 1.f - small;
     a = z < 0.f ? small : big;
     g = z < 0.f ? big : small;
   } else {
     const float e = fast_exp2(z * -kLog2eF);
     a = __builtin_amdgcn_rcpf(1.f + e);
     g = z < 0.f ? 1.f - a : e * a;
-  }
-}
-
-// The same with neither below 2^-126, the least normal float, so that none makes NaN of an infinity.
-template <typename T>
-__device__ __forceinline__ void gate_above_zero(float z, float& a, float& g) {
-  if constexpr (sizeof(T) == 4) {
-    const float e = exp_neg(__builtin_fabsf(z), 126.f * kLn2F), small = e * __builtin_amdgcn_rcpf(1.f + e), big = 1.f - small;
-    a = z < 0.f ? small : big;
-    g = z < 0.f ? big : small;
-  } else {
-    const float e = fast_exp2(__builtin_elementwise_minimum(__builtin_elementwise_maximum(z * -kLog2eF, -126.f), 126.f));  // NaN stays
-    a = __builtin_amdgcn_rcpf(1.f + e);
-    g = e * a;
   }
 }
 

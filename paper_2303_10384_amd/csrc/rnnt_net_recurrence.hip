@@ -50,7 +50,7 @@ __device__ __forceinline__ float advance(float a, float g, float x, float h) {
   return __builtin_fmaf(a, h, g * x);
 }
 
-constexpr float kLeast = 0x1p-126f;  // a product of gates that is below the floats does not make NaN of an infinity
+constexpr float kLeast = 0x1p-126f;  // the least normal float
 
 // A run of steps, h -> P h + S.  Up to 2 kSteps of them go by the definition, h = fma(a, h, g x), whose rounded a costs
 // 2^-24 a step.  Between runs that would grow with the gates' memory, as 2^-24 / (1 - a) (z = 10 over 60000 steps: 5e-4),
@@ -66,10 +66,11 @@ struct Run {
     S = on ? s : S;
     return in;
   }
-  // The run joined to the state h as h + (S - Q h) where Q is below 1/2, as P h + S elsewhere.
+  // The run joined to the state h as h + (S - Q h) where Q is below 1/2, as P h + S elsewhere.  A product of gates that is
+  // below the floats does not make NaN of an infinite state.
   __device__ __forceinline__ float join(float h) const {
-    if (Q < 0.5f && __builtin_isfinite(h)) return __builtin_fmaf(-Q, h, S) + h;
-    return __builtin_fmaf(fmaxf(P, kLeast), h, S);
+    const float next = Q < 0.5f ? __builtin_fmaf(-Q, h, S) + h : __builtin_fmaf(P, h, S);
+    return __builtin_isfinite(h) ? next : __builtin_fmaf(fmaxf(P, kLeast), h, S);
   }
   // `next` behind this one
   __device__ __forceinline__ void append(const Run& next) {
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(64 * W, 4) void net_recurrence(RecurrenceParams p) 
 #pragma unroll
           for (int v = 0; v < VEC; ++v) {
             float g;
-            gate_above_zero<T>(zf[v], a[j][v], g);
+            gate<T>(zf[v], a[j][v], g);
             in[j][v] = run[v].step(a[j][v], g, xf[v], all || j < live);
           }
           if (j == kSteps / 2 - 1) __builtin_amdgcn_sched_barrier(0);  // all gates begun at once would not fit the registers
@@ -381,7 +382,7 @@ __global__ __launch_bounds__(64) void net_recurrence_short(RecurrenceParams p) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         float a, g;
-        gate_above_zero<T>(zf[v], a, g);
+        gate<T>(zf[v], a, g);
         f[v] = s[v] = advance(a, g, xf[v], s[v]);
       }
     }
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
               float a, g;
-              gate_above_zero<T>(zf[v], a, g);
+              gate<T>(zf[v], a, g);
               run[v].step(a, g, xf[v], whole || j < live);
             }
           }

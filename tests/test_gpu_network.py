@@ -289,7 +289,8 @@ def decayed_bounds(x, z, h0, dh=None, dlast=None):
     M_t = a_t M_{t-1} + (1 - a_t) |x_t|, M_{-1} = |h0|.  A step's difference, product and sum are rounded at the size of
     a |h| or (1 - a) |x| (2^-24 each) and its gate is off by GATE of itself, so it adds at most 2 GATE M_t; a run of
     steps joined to the state before it adds a few roundings more (product, complement, sum: each off by GATE + 2^-24
-    of itself a step).  4 GATE M_t covers both: e_t = a_t e_{t-1} + 4 GATE M_t.  dz_t = s (h_{t-1} - x) a (1 - a): the
+    of itself a step).  4 GATE M_t covers both: e_t = a_t e_{t-1} + 4 GATE M_t.  A gate below the normal floats is 0,
+    off by less than 2^-126 (nothing where it is 0 indeed), times its operand.  dz_t = s (h_{t-1} - x) a (1 - a): the
     error of s as in recurrence_bounds, against M_{t-1} + |x|."""
     B, L, D = x.shape
     e = {k: np.zeros(x.shape) for k in ("h", "dz")}
@@ -299,8 +300,10 @@ def decayed_bounds(x, z, h0, dh=None, dlast=None):
         before = []
         for t in range(L):
             before.append((m, err))
+            lost = sum(np.where((gate > 0) & (gate < 2.0 ** -126), 2.0 ** -126, 0.0) * v for gate, v in
+                       ((a[t], np.abs(m)), (g[t], np.abs(x[b, t]))))
             m = a[t] * m + g[t] * np.abs(x[b, t])
-            err = a[t] * err + 4.0 * GATE * m
+            err = a[t] * err + 4.0 * GATE * m + lost
             e["h"][b, t] = err
         if dh is None:
             continue
@@ -309,7 +312,9 @@ def decayed_bounds(x, z, h0, dh=None, dlast=None):
             s = s + np.abs(dh[b, t])
             r = r + s
             size = before[t][0] + np.abs(x[b, t])
-            e["dz"][b, t] = a[t] * g[t] * (size * (4.0 * GATE * r + 8.0 * GATE * s) + s * before[t][1])
+            slope = a[t] * g[t]
+            lost = np.where((slope > 0) & (slope < 2.0 ** -125), 2.0 ** -125, 0.0) * size * s
+            e["dz"][b, t] = slope * (size * (4.0 * GATE * r + 8.0 * GATE * s) + s * before[t][1]) + lost
             s, r = a[t] * s, a[t] * r
     return e
 
@@ -369,8 +374,12 @@ def test_recurrence_near_the_ends_of_float32(torch, pkg, B, L):  # noqa: F811
     h0[:, 14], h0[:, 15], h0[:, 16] = inf, -inf, np.nan
     z[:, :, 15] = -12.0
     z[:, :, 17], h0[:, 17] = 12.0, inf
-    z[:, :, 18] = -100.0  # sigmoid is below the floats
+    z[:, :, 18] = -80.0
     h0[:, 18] = inf
+    z[:, :, 19], h0[:, 19] = -100.0, 3.0e38  # sigmoid is below the normal floats
+    z[:, :, 20], h0[:, 20] = -inf, -3.0e38
+    z[:, ::2, 21], x[:, :, 21] = -inf, 1e-30 * np.sign(x[:, :, 21])
+    h0[:, 21] = 3.0e38
     (x, xd), (z, zd), (h0t, h0) = (rounded(torch, v, "f32") for v in (x, z, h0))
     x.requires_grad_(True)
     z.requires_grad_(True)
