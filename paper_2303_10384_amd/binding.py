@@ -138,10 +138,10 @@ def _dtype_codes():
     return {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
 
-def dtype_code(dtype):
+def dtype_code(dtype, name="logits"):
     code = _dtype_codes().get(dtype)
     if code is None:
-        raise TypeError("logits must be float32, bfloat16 or float16, got %s" % dtype)
+        raise TypeError("%s must be float32, bfloat16 or float16, got %s" % (name, dtype))
     return code
 
 

@@ -183,7 +183,7 @@ def label_embedding(labels, weight, lens=None, scale=1.0, start=None):
         raise ValueError("labels must be (B, N) and weight (V, D)")
     if lens is not None:
         _check("lens", lens, weight.device, torch.int32, labels.shape[:1])
-    dtype_code(weight.dtype)
+    dtype_code(weight.dtype, "weight")
     if start is not None and not 0 <= start < weight.shape[0]:
         raise ValueError("start must be None or a row of weight, got %r" % (start,))
     args = (labels, weight, lens, float(scale), -1 if start is None else int(start))
@@ -253,7 +253,7 @@ def gated_recurrence(x, z, h0=None, lens=None):
     _check("x", x, contiguous=False)
     if x.dim() != 3:
         raise ValueError("x must be (B, L, D)")
-    dtype_code(x.dtype)
+    dtype_code(x.dtype, "x")
     _check("z", z, x.device, x.dtype, x.shape, contiguous=False)
     for name, t in (("x", x), ("z", z)):
         if not _contiguous_channels(t):
@@ -299,7 +299,7 @@ def dropout(x, p, rng):
     stored: the backward pass counts the same numbers again.
     """
     _check("x", x)
-    dtype_code(x.dtype)
+    dtype_code(x.dtype, "x")
     p = _check_p(p)
     _check("rng", rng, x.device, torch.int64, (2,))
     if _recorded(x):
@@ -354,7 +354,7 @@ def joint_hidden(enc, pred, logit_lens, label_lens, activation="relu", p=0.0, rn
     _check("enc", enc)
     if enc.dim() != 3:
         raise ValueError("enc must be (B, T, H)")
-    dtype_code(enc.dtype)
+    dtype_code(enc.dtype, "enc")
     _check("pred", pred, enc.device, enc.dtype)
     if pred.dim() != 3 or pred.shape[0] != enc.shape[0] or pred.shape[2] != enc.shape[2]:
         raise ValueError("pred must be (B, U+1, H) with enc's B and H")

@@ -326,3 +326,14 @@ def test_recurrence_states_in_place_are_refused(net):
     for off in (0, 4, -4, size - 4, 4 - size):
         assert lib.rnnt_recurrence(FAKE, FAKE, shape, FAKE, FAKE, FAKE, FAKE + off, None, None, 0, None) == 9
         assert lib.rnnt_recurrence_grad(FAKE, FAKE, shape, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE + off, None, 0, None) == 9
+
+
+def test_an_unknown_type_is_named(net, calls):
+    import paper_2303_10384_amd as rnnt
+    x, lens = torch.zeros(2, 3, 4, dtype=torch.float64), torch.ones(2, dtype=torch.int32)
+    for name, call_it in (("weight", lambda: rnnt.label_embedding(torch.zeros(2, 3, dtype=torch.int32), x[0])),
+                          ("x", lambda: rnnt.gated_recurrence(x, x)),
+                          ("x", lambda: rnnt.dropout(x, 0.5, torch.zeros(2, dtype=torch.int64))),
+                          ("enc", lambda: rnnt.joint_hidden(x, x, lens, lens))):
+        with pytest.raises(TypeError, match="^%s must be float32, bfloat16 or float16, got torch.float64" % name):
+            call_it()
