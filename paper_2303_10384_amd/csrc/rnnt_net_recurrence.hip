@@ -52,20 +52,21 @@ __device__ __forceinline__ float advance(float a, float g, float x, float h) {
 
 constexpr float kLeast = 0x1p-126f;  // the least normal float
 
-// A run of steps, h -> P h + S.  Up to 2 kSteps of them go by the definition, h = fma(a, h, g x), whose rounded a costs
-// 2^-24 a step.  Between runs that would grow with the gates' memory, as 2^-24 / (1 - a) (z = 10 over 60000 steps: 5e-4),
-// so Q = 1 - P is added up on its own.
+// A run of steps, h -> P h + S: of states forward, of the gradient's sums backward.  Up to 2 kSteps of them go by the
+// definition, h = fma(a, h, g x), whose rounded a costs 2^-24 a step.  Between runs that would grow with the gates'
+// memory, as 2^-24 / (1 - a) (z = 10 over 60000 steps: 5e-4), so Q = 1 - P is added up on its own.
 struct Run {
   float P = 1.f, Q = 0.f, S = 0.f;
 
-  // one step more; returns g x
-  __device__ __forceinline__ float step(float a, float g, float x, bool on) {
-    const float in = g * x, q = __builtin_fmaf(g, P, Q), p = a * P, s = __builtin_fmaf(a, S, in);
+  // one step more, to the sum `next`
+  __device__ __forceinline__ void step(float a, float g, float next, bool on) {
+    const float q = __builtin_fmaf(g, P, Q), p = a * P;
     Q = on ? q : Q;
     P = on ? p : P;
-    S = on ? s : S;
-    return in;
+    S = on ? next : S;
   }
+  __device__ __forceinline__ void forward(float a, float in, float g, bool on) { step(a, g, __builtin_fmaf(a, S, in), on); }
+  __device__ __forceinline__ void back(float a, float d, float g, bool on) { step(a, g, a * (S + d), on); }
   // The run joined to the state h as h + (S - Q h) where Q is below 1/2, as P h + S elsewhere.  A product of gates that is
   // below the floats does not make NaN of an infinite state.
   __device__ __forceinline__ float join(float h) const {
@@ -147,37 +148,32 @@ struct RowStore {
   }
 };
 
-// The pairs of a block's waves, two sets of them in turn: forward Run::pack()'s, backward the product of the gates and
-// the sum, whose terms have weights of at most 1.
+// The runs of a block's waves in Run::pack()'s form, two sets of them in turn.  BACK: the last wave's comes first.
 template <int VEC, int W>
 struct PairBoard {
   struct __attribute__((aligned(8 * VEC))) Pairs {
     float2 of[VEC];
   };
   Pairs at[2][W][64];
-  float state[2][64][VEC];  // forward: at the tile's first step
+  float state[2][64][VEC];  // that arrives at the tile
 
-  __device__ __forceinline__ void put(int set, int wave, int lane, const float* A, const float* S) {
-    Pairs k;
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) k.of[v] = make_float2(A[v], S[v]);
-    at[set][wave][lane] = k;
-  }
   __device__ __forceinline__ void put(int set, int wave, int lane, const Run* run) {
     Pairs k;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) k.of[v] = run[v].pack();
     at[set][wave][lane] = k;
   }
-  // forward: the state that arrives at `wave`'s run, from the tile's through the runs before
+  // the state that arrives at `wave`'s run, from the tile's through the runs before
+  template <bool BACK>
   __device__ __forceinline__ void arrive(int set, int wave, int lane, float* h) const {
+    const int n = BACK ? W - 1 - wave : wave;
     float first[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) h[v] = first[v] = state[set][lane][v];
 #pragma unroll
     for (int i = 0; i < W - 1; ++i) {
-      if (i >= wave) break;
-      const Pairs k = at[set][i][lane];
+      if (i >= n) break;
+      const Pairs k = at[set][BACK ? W - 1 - i : i][lane];
 #pragma unroll
       for (int v = 0; v < VEC; ++v) h[v] = join_finite(k.of[v], h[v]);
     }
@@ -188,21 +184,9 @@ struct PairBoard {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) h[v] = first[v];
 #pragma unroll 1
-    for (int i = 0; i < wave; ++i) {
+    for (int i = 0; i < n; ++i) {
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) h[v] = Run::unpack(at[set][i][lane].of[v]).join(h[v]);
-    }
-  }
-  // backward: carry through all waves' pairs from the last on; `mine` is what arrives at `wave`
-  __device__ __forceinline__ void compose(int set, int wave, int lane, float* carry, float* mine) const {
-#pragma unroll
-    for (int w = W - 1; w >= 0; --w) {
-      const Pairs k = at[set][w][lane];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        if (w == wave) mine[v] = carry[v];
-        carry[v] = __builtin_fmaf(k.of[v].x, carry[v], k.of[v].y);
-      }
+      for (int v = 0; v < VEC; ++v) h[v] = Run::unpack(at[set][BACK ? W - 1 - i : i][lane].of[v]).join(h[v]);
     }
   }
 };
@@ -215,41 +199,20 @@ __device__ __forceinline__ void carry_in(const RecurrenceParams& p, const Place&
   if (n == 0) return;
   const int share = (n + W - 1) / W, from = min(wave * share, n), to = min(from + share, n);
   const float2* pairs = p.pairs + (static_cast<int64_t>(at.b) * p.segments + (BACK ? at.segment + 1 : 0)) * p.D + c;
-  if constexpr (BACK) {
-    float A[VEC], S[VEC];
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      A[v] = 1.f;
-      S[v] = 0.f;
-    }
+  Run run[VEC];
 #pragma unroll 4
-    for (int i = to - 1; i >= from; --i) {
+  for (int i = from; i < to; ++i) {
+    const int64_t seg = BACK ? to - 1 - (i - from) : i;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const float2 k = pairs[static_cast<int64_t>(i) * p.D + v];
-        S[v] = __builtin_fmaf(k.x, S[v], k.y);
-        A[v] *= k.x;
-      }
-    }
-    board.put(1, wave, lane, A, S);
-    __syncthreads();
-    float none[VEC];
-    board.compose(1, wave, lane, carry, none);
-  } else {
-    Run run[VEC];
-#pragma unroll 4
-    for (int i = from; i < to; ++i) {
+    for (int v = 0; v < VEC; ++v) run[v].append(Run::unpack(pairs[seg * p.D + v]));
+  }
+  board.put(1, wave, lane, run);
+  __syncthreads();
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) run[v].append(Run::unpack(pairs[static_cast<int64_t>(i) * p.D + v]));
-    }
-    board.put(1, wave, lane, run);
-    __syncthreads();
+  for (int i = 0; i < W; ++i) {
+    const auto one = board.at[1][BACK ? W - 1 - i : i][lane];
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const auto one = board.at[1][i][lane];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) carry[v] = Run::unpack(one.of[v]).join(carry[v]);
-    }
+    for (int v = 0; v < VEC; ++v) carry[v] = Run::unpack(one.of[v]).join(carry[v]);
   }
 }
 
@@ -296,7 +259,8 @@ __global__ __launch_bounds__(64 * W, 4) void net_recurrence(RecurrenceParams p) 
           for (int v = 0; v < VEC; ++v) {
             float g;
             gate<T>(zf[v], a[j][v], g);
-            in[j][v] = run[v].step(a[j][v], g, xf[v], all || j < live);
+            in[j][v] = g * xf[v];
+            run[v].forward(a[j][v], in[j][v], g, all || j < live);
           }
           if (j == kSteps / 2 - 1) __builtin_amdgcn_sched_barrier(0);  // all gates begun at once would not fit the registers
         }
@@ -310,7 +274,7 @@ __global__ __launch_bounds__(64 * W, 4) void net_recurrence(RecurrenceParams p) 
       }
       __syncthreads();  // one to a tile: the other set is written before the next
       float first[VEC];
-      board.arrive(set, wave, lane, first);
+      board.template arrive<false>(set, wave, lane, first);
       if (wave == W - 1) {  // to the next tile
 #pragma unroll
         for (int v = 0; v < VEC; ++v) carry[v] = run[v].join(first[v]);
@@ -405,13 +369,7 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
   const int share = (p.seg_steps / kSteps + kWaves - 1) / kWaves * kSteps;
   const int stop = min(at.end, at.len);
   const int from = min(at.begin + wave * share, stop), to = min(from + share, stop);
-  float A[VEC], S[VEC];
   Run all[VEC], run[VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-    A[v] = 1.f;
-    S[v] = 0.f;
-  }
   const int batches = max(0, (to - from + kSteps - 1) / kSteps);
   if (batches > 0) {
     const T* z = static_cast<const T*>(p.z) + at.b * p.z_sb;
@@ -433,9 +391,10 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
         if (with_x) xs.load(x, x_st, step_of(i + 1), to, c);
         zs.load(z, p.z_st, step_of(i + 1), to, c);
       }
-      if constexpr (BACK) {
+      const auto scan = [&](auto whole) {
 #pragma unroll
-        for (int j = kSteps - 1; j >= 0; --j) {
+        for (int k = 0; k < kSteps; ++k) {
+          const int j = BACK ? kSteps - 1 - k : k;
           float xf[VEC], zf[VEC];
           xn.r[j].get(xf);
           zn.r[j].get(zf);
@@ -443,66 +402,33 @@ __global__ __launch_bounds__(64 * kWaves) void net_recurrence_pairs(RecurrencePa
           for (int v = 0; v < VEC; ++v) {
             float a, g;
             gate<T>(zf[v], a, g);
-            const float next = a * (S[v] + xf[v]);
-            S[v] = j < live ? next : S[v];
-            A[v] = j < live ? a * A[v] : A[v];
+            if constexpr (BACK) run[v].back(a, xf[v], g, whole || j < live);
+            else run[v].forward(a, g * xf[v], g, whole || j < live);
           }
         }
-      } else {
-        const auto scan = [&](auto whole) {
+      };
+      if (live >= kSteps) scan(std::true_type{});
+      else scan(std::false_type{});
+      if ((i & 1) || i + 1 == batches) {  // two batches to a run
 #pragma unroll
-          for (int j = 0; j < kSteps; ++j) {
-            float xf[VEC], zf[VEC];
-            xn.r[j].get(xf);
-            zn.r[j].get(zf);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-              float a, g;
-              gate<T>(zf[v], a, g);
-              run[v].step(a, g, xf[v], whole || j < live);
-            }
-          }
-        };
-        if (live >= kSteps) scan(std::true_type{});
-        else scan(std::false_type{});
-        if ((i & 1) || i + 1 == batches) {  // two batches to a run
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            all[v].append(run[v]);
-            run[v] = Run{};
-          }
+        for (int v = 0; v < VEC; ++v) {
+          all[v].append(run[v]);
+          run[v] = Run{};
         }
       }
     }
   }
-  if constexpr (!BACK) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const float2 k = all[v].pack();
-      A[v] = k.x;
-      S[v] = k.y;
-    }
-  }
-  board.put(0, wave, lane, A, S);
+  board.put(0, wave, lane, all);
   __syncthreads();
   if (wave != 0) return;
   // the waves' pairs into one
   float2* out = p.pairs + (static_cast<int64_t>(at.b) * p.segments + at.segment) * p.D + c;
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
-    float sum = 0.f, product = 1.f;
-    Run run;
+    Run one;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      const float2 k = board.at[0][BACK ? kWaves - 1 - i : i][lane].of[v];
-      if constexpr (BACK) {
-        sum = __builtin_fmaf(k.x, sum, k.y);
-        product *= k.x;
-      } else {
-        run.append(Run::unpack(k));
-      }
-    }
-    out[v] = BACK ? make_float2(product, sum) : run.pack();
+    for (int i = 0; i < kWaves; ++i) one.append(Run::unpack(board.at[0][BACK ? kWaves - 1 - i : i][lane].of[v]));
+    out[v] = one.pack();
   }
 }
 
@@ -559,7 +485,7 @@ __global__ __launch_bounds__(64 * W, 4) void net_recurrence_grad(RecurrenceParam
     for (int i = live_tiles - 1, set = 0; i >= 0; --i, set ^= 1) {
       const int t0 = at.begin + i * TILE, live = at.len - t0 - wave * kSteps;
       const bool whole = live >= kSteps;
-      float a[kSteps][VEC], g[kSteps][VEC], w[kSteps][VEC], s[VEC], A[VEC], S[VEC];
+      float a[kSteps][VEC], g[kSteps][VEC], w[kSteps][VEC], s[VEC];
       st.get(s);
 #pragma unroll
       for (int j = 0; j < kSteps; ++j) {
@@ -578,26 +504,26 @@ __global__ __launch_bounds__(64 * W, 4) void net_recurrence_grad(RecurrenceParam
       }
       Rows<T, VEC> d = ds;
       if (i > 0) load(i - 1);
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        A[v] = 1.f;
-        S[v] = 0.f;
-      }
+      Run run[VEC];
 #pragma unroll
       for (int j = kSteps - 1; j >= 0; --j) {
         float df[VEC];
         d.r[j].get(df);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const float next = a[j][v] * (S[v] + df[v]);
-          S[v] = whole || j < live ? next : S[v];
-          A[v] = whole || j < live ? a[j][v] * A[v] : A[v];
-        }
+        for (int v = 0; v < VEC; ++v) run[v].back(a[j][v], df[v], g[j][v], whole || j < live);
       }
-      board.put(set, wave, lane, A, S);
+      board.put(set, wave, lane, run);
+      if (wave == 0) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) board.state[set][lane][v] = carry[v];
+      }
       __syncthreads();  // one to a tile: the other set is written before the next
       float in[VEC];
-      board.compose(set, wave, lane, carry, in);
+      board.template arrive<true>(set, wave, lane, in);
+      if (wave == 0) {  // to the tile before
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) carry[v] = run[v].join(in[v]);
+      }
       const RowStore<T, VEC, W> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
 #pragma unroll
       for (int j = kSteps - 1; j >= 0; --j) {

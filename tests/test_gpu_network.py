@@ -437,6 +437,28 @@ def test_recurrence_holds_its_value(torch, pkg, B, L):  # noqa: F811
     assert bool((step == 1).all()) and bool((s == 1).all())
 
 
+@pytest.mark.parametrize("B,L", [(1, 60000), (700, 2000)])
+def test_recurrence_gradient_of_long_memories(torch, pkg, B, L):  # noqa: F811
+    """An upstream gradient of 1 at every state: s_t = (1 - a^n) / (1 - a) with n = L - t, so dx_t = 1 - a^n and dh0 =
+    a (1 - a^L) / (1 - a).  A run of eight steps is off by eight roundings of its gates and sums (2^-21 and less), and
+    sums of runs, joined by 1 - P, by no more; the gate's own 2^-21 is in both.  2^-19 of the value covers them."""
+    x = torch.zeros((B, L, 64), device="cuda", requires_grad=True)
+    h0 = torch.zeros((B, 64), device="cuda", requires_grad=True)
+    z0 = np.array([10.0, 13.0, 3.0, 0.5, 0.0, -3.0, 7.0, 11.0])
+    z = torch.tensor(z0, device="cuda", dtype=torch.float32).repeat(8).expand(B, L, 64)
+    h, _ = pkg.gated_recurrence(x, z, h0)
+    dx, dh0 = torch.autograd.grad(h, (x, h0), torch.ones_like(h))
+    g = R._sigmoid(-z0)
+    n = np.arange(L, 0, -1)[:, None]
+    some = np.r_[0:40, L // 2:L // 2 + 300, L - 200:L]
+    want = -np.expm1(n[some] * np.log1p(-g))
+    for b in (0, B - 1):
+        got = dx[b, :, :8].double().cpu().numpy()[some]
+        assert np.all(np.abs(got - want) <= 2.0 ** -19 * want)
+        total = (1 - g) * -np.expm1(L * np.log1p(-g)) / g
+        assert np.all(np.abs(dh0[b, :8].double().cpu().numpy() - total) <= 2.0 ** -19 * total)
+
+
 def test_gradients_with_saved_tensors_on_the_host(torch, pkg):  # noqa: F811
     """Saved tensors that come back in another layout (views of a projection do) give the same gradients."""
     g = torch.Generator(device="cuda").manual_seed(17)
