@@ -212,12 +212,14 @@ def _call_workspace(nbytes, device, result):
 def _result(shape, dtype, device, nbytes):
     """A result tensor and the workspace of the call that fills it, or None."""
     torch = _torch()
-    if nbytes and _capturing(device):
+    if not nbytes:
+        return torch.empty(shape, dtype=dtype, device=device), None
+    if _capturing(device):
         size = -(-math.prod(shape) * dtype.itemsize // 256) * 256
         both = _workspace_block(size + nbytes, device)
         if both is not None:
             return torch.empty(0, dtype=dtype, device=device).set_(both.untyped_storage(), 0, shape), both[size:]
-        nbytes = 0
+        return torch.empty(shape, dtype=dtype, device=device), None
     return torch.empty(shape, dtype=dtype, device=device), _workspace_block(nbytes, device)
 
 

@@ -120,7 +120,11 @@ def _recorded(*tensors):
     autograd refuses (the operators have no forward mode)."""
     if forward_ad._current_level >= 0:
         return True
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _dense(*saved):
@@ -195,7 +199,7 @@ def label_embedding(labels, weight, lens=None, scale=1.0, start=None):
 # ---------------------------------------------------------------- gated recurrence
 
 def _contiguous_channels(t):
-    return t.numel() == 0 or t.shape[2] == 1 or t.stride(2) == 1
+    return t.stride(2) == 1 or t.shape[2] == 1 or t.numel() == 0
 
 
 def _recurrence_shape(x, z):
