@@ -43,8 +43,8 @@ extern "C" {
  * labels[b, i], valid for i < lens[b].  lens NULL: every row is valid.
  * A valid label outside [0, V) gives a row of NaN and no gradient.
  *
- * The gradient sums the rows of every token in the order of their positions
- * (b, i), so equal inputs give equal bits:
+ * The gradient sums the rows of every token in one order, so equal inputs give equal
+ * bits (by position (b, i) in stretches of up to 32 rows, then the stretches' sums):
  *   dweight[v, :] = scale * sum over valid (b, i) with token(b, i) = v of dout[b, i, :].
  * Every element of dweight (V, D) is written.
  *

@@ -15,8 +15,9 @@ namespace {
 // Where sequences and channel tiles are too few to fill the chip, the steps are cut into segments: a first kernel
 // finds each segment's pair, the second one begins each block at the state that the pairs before it give.
 // Bound by the bytes of x, z and h, twice x and z in segments, and for 16 bits as much by the instructions of gates and
-// runs (L=60013 D=640 bf16, one sequence: 30 us at 5.2 TB/s for the pairs, 46 us at 5.0 TB/s for the states).  One pass in which a block waits for the blocks before it would read
-// them once; not built.
+// runs (L=60013 D=640 bf16, one sequence: 31 us at 5.0 TB/s for the pairs, 45 us at 5.1 TB/s for the states, whose
+// vector instructions fill about three quarters of the time).  One pass in which a block waits for the blocks before
+// it would read x and z once; not built.
 constexpr int kSteps = RNNT_RECURRENCE_STATE_STEPS;
 constexpr int kWaves = 16;                     // of a block where sequences are few: as many as it can have
 constexpr int kTileSteps = kSteps * kWaves;    // segments are multiples of it
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(64 * W, 4) void net_recurrence(RecurrenceParams p) 
 }
 
 // At most kSteps steps (one, for a streaming decoder): a thread to VEC channels, step by step, nothing to exchange.
-// 16 sequences of 640 float32 channels: one step 2.0 us and eight 3.3, where the tiles of sixteen waves take 5.9.
+// 16 sequences of 640 float32 channels: one step 2.7 us and eight 4.0, where the tiles of four waves take 3.8 and 3.9.
 template <typename T, int VEC>
 __global__ __launch_bounds__(64) void net_recurrence_short(RecurrenceParams p) {
   const int b = static_cast<int>(blockIdx.x) / p.tiles, tile = static_cast<int>(blockIdx.x) % p.tiles;
@@ -601,8 +602,8 @@ size_t pair_bytes(const rnnt_recurrence_shape_t& s, bool back) {
 }
 
 // Waves of a block: sixteen while channel tiles are few, then four or one, no more than the steps have use for
-// (forward, sixteen waves and these: B=8 L=20 D=640 bf16 6.9 and 5.2 us, B=64 L=81 D=1024 bf16 14.5 and 9.8,
-// B=600 L=60 D=512 bf16 59 and 24, B=256 L=81 D=1024 f32 78 and 41, 6.3 TB/s).
+// (forward, sixteen waves and these: B=8 L=20 D=640 bf16 7.1 and 4.2 us, B=64 L=81 D=1024 bf16 14.8 and 11.3,
+// B=600 L=60 D=512 bf16 53 and 24, B=256 L=81 D=1024 f32 72 and 42, 6.2 TB/s).
 template <typename F>
 rnnt_status_t with_waves(const RecurrenceParams& p, F&& f) {
   const int64_t blocks = static_cast<int64_t>(p.B) * p.tiles * p.segments;
