@@ -188,3 +188,37 @@ def test_a_refused_allocation_is_not_the_next_calls_error(torch, pkg):  # noqa: 
     assert lib.rnnt_joint_hidden_grad(p, p, huge, q, q, 0, 0.0, None, p, p, p, None, 0, stream) == 8
     y = pkg.dropout(x, 0.0, torch.zeros(2, dtype=torch.int64, device="cuda"))
     assert torch.equal(x, y)
+
+
+def test_every_call_captured_without_a_workspace(torch, pkg):  # noqa: F811
+    """Alignment, lattice scores, the loss over arc lists and the loss, with results of their own, in one graph: each
+    call's workspace lives with a result of it."""
+    lg, labels, tl, ul = inputs(torch)
+    lab, t, u = (a.cpu().numpy() for a in (labels, tl, ul))
+    lattices = [pkg.topologies.grid_lattice(int(t[b]), int(u[b]), lab[b, :u[b]], variant="rnnt") for b in range(6)]
+    plan = pkg.arc_plan(lattices, 20, 9, 48, blank=0, device="cuda")
+    _, lp_blank, lp_label = pkg.log_softmax_gather(lg, labels, tl, ul)
+
+    def call():
+        scores = pkg.lattice_scores(lp_blank, lp_label, tl, ul)
+        return (pkg.rnnt_loss(lg, labels, tl, ul) + pkg.viterbi_align(lg, labels, tl, ul) + pkg.arc_loss(lg, tl, ul, plan)
+                + pkg.rnnt_loss(lg, labels, tl, ul, variant="wrnnt", need_grad=False)[:1]
+                + tuple(scores[k] for k in sorted(scores)))
+
+    want = [x.clone() for x in call()]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = call()
+    for _ in range(3):
+        for x in out:
+            x.fill_(-7)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(torch.nan_to_num(a.double(), 3e300), torch.nan_to_num(b.double(), 3e300))
+        again = call()  # eager work between the replays
+        torch.cuda.synchronize()
+        assert all(torch.equal(torch.nan_to_num(a.double(), 3e300), torch.nan_to_num(b.double(), 3e300))
+                   for a, b in zip(again, want))
