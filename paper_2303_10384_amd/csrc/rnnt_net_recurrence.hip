@@ -526,21 +526,25 @@ __global__ __launch_bounds__(64 * W, 4) void net_recurrence_grad(RecurrenceParam
         for (int v = 0; v < VEC; ++v) carry[v] = run[v].join(in[v]);
       }
       const RowStore<T, VEC, W> ox(dx, row0 + t0, at.end - t0, p.D, c), oz(dz, row0 + t0, at.end - t0, p.D, c);
+      const auto gradients = [&](auto all) {
 #pragma unroll
-      for (int j = kSteps - 1; j >= 0; --j) {
-        float df[VEC], fx[VEC], fz[VEC];
-        d.r[j].get(df);
+        for (int j = kSteps - 1; j >= 0; --j) {
+          float df[VEC], fx[VEC], fz[VEC];
+          d.r[j].get(df);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const bool on = whole || j < live;
-          const float total = in[v] + df[v];
-          fx[v] = on ? g[j][v] * total : 0.f;
-          fz[v] = on ? w[j][v] * total : 0.f;
-          in[v] = on ? a[j][v] * total : in[v];
+          for (int v = 0; v < VEC; ++v) {
+            const bool on = all || j < live;
+            const float total = in[v] + df[v];
+            fx[v] = on ? g[j][v] * total : 0.f;
+            fz[v] = on ? w[j][v] * total : 0.f;
+            in[v] = on ? a[j][v] * total : in[v];
+          }
+          ox.put(wave * kSteps + j, fx);
+          oz.put(wave * kSteps + j, fz);
         }
-        ox.put(wave * kSteps + j, fx);
-        oz.put(wave * kSteps + j, fz);
-      }
+      };
+      if (whole) gradients(std::true_type{});
+      else gradients(std::false_type{});
     }
   }
   if (p.dh0 && at.segment == 0 && wave == 0) {
