@@ -1,0 +1,535 @@
+// Attention of a chunk of new tokens over a paged cache (contract in include/rnnt_encoder_mi355x.h).
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "rnnt_enc.h"
+#include "rnnt_pages.h"
+
+namespace rnnt {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+struct AttentionParams {
+  const void *q, *k, *v;
+  void *k_cache, *v_cache, *out;
+  const int32_t *lens, *cached, *pages;
+  float* part;  // of the splits: sums over values, then {maximum, sum of weights}
+  int64_t q_stride_b, q_stride_t, q_stride_h, k_stride_b, k_stride_t, k_stride_h, v_stride_b, v_stride_t, v_stride_h;
+  int32_t B, L, Hq, Hkv, G, D, shift, table, num_pages, causal, left, tiles, splits;
+  float scale;  // times log2 e
+};
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr int kRowTile = 16;  // rows (tokens times the heads that share keys) to a block
+constexpr int kKeys = 32;     // keys to a wave's step
+constexpr int kWaves = 4;
+
+// ---- an utterance and its tile of rows ------------------------------------------
+// Row r of an utterance's head of keys is token r / G and query head h G + r % G.
+struct Tile {
+  int b, h, tile, split;
+  int n, cached, end;    // new tokens, cached ones, all
+  int state;             // 1 there are valid rows, 0 none, -1 bad lengths
+  PageTable table;
+
+  __device__ __forceinline__ Tile(const AttentionParams& p, int64_t unit, int split_) : split(split_) {
+    tile = static_cast<int>(unit % p.tiles);
+    const int bh = static_cast<int>(unit / p.tiles);
+    b = bh / p.Hkv;
+    h = bh - b * p.Hkv;
+    n = p.lens ? p.lens[b] : p.L;
+    cached = p.cached[b];
+    table = PageTable{p.pages + static_cast<int64_t>(b) * p.table, p.table, p.num_pages, p.shift};
+    const bool fits = lengths_fit(n, p.L, cached, static_cast<int64_t>(p.table) << p.shift);
+    end = cached + n;
+    state = !fits ? -1 : static_cast<int64_t>(tile) * kRowTile < static_cast<int64_t>(n) * p.G;
+  }
+  __device__ __forceinline__ int token(const AttentionParams& p, int row) const {
+    return (tile * kRowTile + row) / p.G;
+  }
+};
+
+// The row of a key: of the cache, or (the top bit) the chunk's own token.
+constexpr uint32_t kNewRow = 0x80000000u, kBadRow = 0xffffffffu;
+__device__ __forceinline__ uint32_t row_of(const AttentionParams& p, const Tile& t, int pos) {
+  const int id = t.table.page_of(pos);
+  if (id < 0) return kBadRow;
+  return pos >= t.cached ? kNewRow | static_cast<uint32_t>(pos - t.cached) : cache_row(id, p.Hkv, t.h, pos, p.shift);
+}
+
+template <typename T>
+__device__ __forceinline__ const T* row_pointer(const T* cache, const T* fresh, int64_t stride_t, uint32_t row, int D) {
+  if (row == kBadRow) return fresh;  // a valid address; its key is NaN wherever it is seen
+  return row & kNewRow ? fresh + static_cast<int64_t>(row & ~kNewRow) * stride_t : cache + static_cast<int64_t>(row) * D;
+}
+
+// ---- eight elements in a matrix instruction's order ------------------------------
+// A 16 x 16 product over 32: lane l holds row (or column) l % 16 and elements 8 (l / 16) .. + 7.  Float32
+// takes eight instructions over 4, which add up the same 32 in another order.
+template <typename T>
+struct Eight {
+  u32x4 w[sizeof(T) / 2];
+
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (auto& x : w) x = u32x4{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<u32x4*>(p)[i] = w[i];
+  }
+  __device__ __forceinline__ void set(const float* f) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i / 4][i % 4] = __float_as_uint(f[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[0][i] = Pack<T, 2>::pack2(f[2 * i], f[2 * i + 1]);
+    }
+  }
+  // an infinity or NaN among them
+  __device__ __forceinline__ bool odd() const {
+    constexpr uint32_t kExp = sizeof(T) == 4 ? 0x7f800000u : __is_same(T, bf16_t) ? 0x7f80u : 0x7c00u;
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        any |= (w[i][j] & kExp) == kExp;
+        if constexpr (sizeof(T) == 2) any |= (w[i][j] & (kExp << 16)) == (kExp << 16);
+      }
+    return any;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ f32x4 mma(const Eight<T>& a, const Eight<T>& b, f32x4 c) {
+  if constexpr (__is_same(T, bf16_t)) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.w[0]), __builtin_bit_cast(bf16x8, b.w[0]), c, 0, 0, 0);
+  } else if constexpr (__is_same(T, f16_t)) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.w[0]), __builtin_bit_cast(f16x8, b.w[0]), c, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w[i / 4][i % 4]), __uint_as_float(b.w[i / 4][i % 4]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// ---- values through LDS ------------------------------------------------------------
+// Rows of values lie in LDS as they do in memory, each 32 bytes (16 in float32) longer, so that the four rows that a
+// group of lanes reads at once, and the groups' rows, meet different banks.
+template <typename T, int DT>
+struct Values {
+  static constexpr int kStride = DT * 32 + (sizeof(T) == 4 ? 4 : 16);  // elements
+  static constexpr int kElems = kKeys * kStride;
+
+  // values of channel 16 c + lane % 16 and the eight keys of the lane's group g: 4 g + j and 16 + 4 g + j
+  __device__ __forceinline__ static Eight<T> column(const T* lds, int c, int lane) {
+    Eight<T> e;
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        e.w[j / 4][j % 4] = *reinterpret_cast<const uint32_t*>(lds + (16 * (j / 4) + 4 * g + j % 4) * kStride + 16 * c + i);
+    } else {
+      // sixteen lanes read four rows of sixteen channels, and each gets the four of its own channel
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const T* at = lds + (16 * half + 4 * g + (i >> 2)) * kStride + 16 * c + 4 * (i & 3);
+        const i16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at);
+        const auto two = __builtin_bit_cast(uint2, t);
+        e.w[0][2 * half] = two.x;
+        e.w[0][2 * half + 1] = two.y;
+      }
+    }
+    return e;
+  }
+};
+
+__device__ __forceinline__ float across_groups_max(float x) {
+  x = __builtin_fmaxf(x, __shfl_xor(x, 16));
+  return __builtin_fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float across_groups_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// ---- the chunk's own keys and values, into the cache ---------------------------------
+// The tokens whose first row lies in the tile, by the tile's first split.  Nothing in this launch reads them there.
+template <typename T>
+__device__ __forceinline__ void write_cache(const AttentionParams& p, const Tile& t, int rows) {
+  const int first = (t.tile * rows + p.G - 1) / p.G, last = min(((t.tile + 1) * rows + p.G - 1) / p.G, t.n);
+  const int pieces = p.D / 8, total = (last - first) * pieces;
+  for (int i = static_cast<int>(threadIdx.x); i < total; i += static_cast<int>(blockDim.x)) {
+    const int token = first + i / pieces, c = 8 * (i % pieces), pos = t.cached + token;
+    const int id = t.table.page_of(pos);
+    if (id < 0) continue;
+    const int64_t to = static_cast<int64_t>(cache_row(id, p.Hkv, t.h, pos, p.shift)) * p.D + c;
+    Eight<T> e;
+    e.load(static_cast<const T*>(p.k) + t.b * p.k_stride_b + token * p.k_stride_t + t.h * p.k_stride_h + c);
+    e.store(static_cast<T*>(p.k_cache) + to);
+    e.load(static_cast<const T*>(p.v) + t.b * p.v_stride_b + token * p.v_stride_t + t.h * p.v_stride_h + c);
+    e.store(static_cast<T*>(p.v_cache) + to);
+  }
+}
+
+// ---- attention ------------------------------------------------------------------------
+// A block of four waves takes sixteen rows and, of their keys, every wave every fourth step of 32.  Scores are formed
+// transposed, keys by rows, so that a lane holds one row's scores and the weights are already where the product with
+// the values takes them: group g's eight keys are 4 g + j and 16 + 4 g + j in both.  The waves' maxima, sums and
+// products meet in LDS, or, where a sequence is split among blocks, in memory.
+template <typename T, int DT>
+__global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) {
+  using V = Values<T, DT>;
+  constexpr int kPieces = 4 * DT, kLoads = kKeys * kPieces / 64;  // 16-byte pieces of a row (float32: pairs of them)
+  constexpr int kValueBytes = kWaves * V::kElems * static_cast<int>(sizeof(T));
+  constexpr int kJoinBytes = kWaves * 32 * DT * 17 * 4;
+  __shared__ __attribute__((aligned(16))) char lds[kValueBytes > kJoinBytes ? kValueBytes : kJoinBytes];
+  __shared__ float stat[2][kWaves][16];
+  const int lane = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6;
+  const int g = lane >> 4, col = lane & 15;
+  const Tile t(p, blockIdx.x / p.splits, static_cast<int>(blockIdx.x % p.splits));
+  if (t.split == 0 && t.state == 1) write_cache<T>(p, t, kRowTile);
+
+  const int rows = p.L * p.G, row0 = t.tile * kRowTile;
+  float m = kNegInf, sum = 0.f;
+  f32x4 acc[2 * DT];
+#pragma unroll
+  for (int c = 0; c < 2 * DT; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  if (t.state == 1) {
+    const int valid_rows = min(t.n * p.G - row0, kRowTile);
+    // a lane behind the last valid row works on that one again; its result is dropped
+    const int my_row = row0 + min(col, valid_rows - 1), my_token = my_row / p.G;
+    const Seen mine(t.cached + my_token, t.end, p.causal != 0, p.left);
+    const Seen first(t.cached + row0 / p.G, t.end, p.causal != 0, p.left);
+    const Seen last(t.cached + (row0 + valid_rows - 1) / p.G, t.end, p.causal != 0, p.left);
+    const int lo = first.lo, hi = last.hi;        // keys that some row sees
+    const int all_lo = last.lo, all_hi = first.hi;  // ... that every row sees
+    const int steps = (hi - lo + kKeys - 1) / kKeys;
+    const int begin = static_cast<int>(static_cast<int64_t>(steps) * t.split / p.splits) + wave;
+    const int stop = static_cast<int>(static_cast<int64_t>(steps) * (t.split + 1) / p.splits);
+
+    const T* k_new = static_cast<const T*>(p.k) + t.b * p.k_stride_b + t.h * p.k_stride_h;
+    const T* v_new = static_cast<const T*>(p.v) + t.b * p.v_stride_b + t.h * p.v_stride_h;
+    const T *k_cache = static_cast<const T*>(p.k_cache), *v_cache = static_cast<const T*>(p.v_cache);
+    T* values = reinterpret_cast<T*>(lds) + wave * V::kElems;
+
+    Eight<T> q[DT];
+    {
+      const T* from = static_cast<const T*>(p.q) + t.b * p.q_stride_b + my_token * p.q_stride_t +
+                      (t.h * p.G + my_row - my_token * p.G) * p.q_stride_h;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        q[d].zero();
+        if (32 * d + 8 * g < p.D) q[d].load(from + 32 * d + 8 * g);
+      }
+    }
+
+    Eight<T> kk[2][DT], vv[kLoads];
+    uint32_t bad = 0;  // keys of the step whose page is none
+    const auto fetch = [&](int step) {
+      const uint32_t row = row_of(p, t, min(lo + step * kKeys + (lane & 31), hi - 1));
+      bad = static_cast<uint32_t>(__ballot(row == kBadRow));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const T* from = row_pointer(k_cache, k_new, p.k_stride_t, __shfl(row, 16 * i + col), p.D);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          kk[i][d].zero();
+          if (32 * d + 8 * g < p.D) kk[i][d].load(from + 32 * d + 8 * g);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int piece = i * 64 + lane, key = piece / kPieces, c = 8 * (piece % kPieces);
+        const T* from = row_pointer(v_cache, v_new, p.v_stride_t, __shfl(row, key), p.D);
+        vv[i].zero();
+        if (c < p.D) vv[i].load(from + c);
+      }
+    };
+
+    if (begin < stop) fetch(begin);
+    for (int step = begin; step < stop; step += kWaves) {
+      const int base = lo + step * kKeys;
+      const bool mixed = base < all_lo || base + kKeys > all_hi || bad != 0;  // some row does not see some key
+      const uint32_t bad_now = bad;
+      f32x4 s[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DT; ++d) s[i] = mma(kk[i][d], q[d], s[i]);
+      }
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int piece = i * 64 + lane;
+        if (mixed) odd |= vv[i].odd();
+        vv[i].store(values + piece / kPieces * V::kStride + 8 * (piece % kPieces));
+      }
+      const bool careful = mixed && __ballot(odd) != 0;
+      if (step + kWaves < stop) fetch(step + kWaves);
+
+      float w[8], most = kNegInf;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int at = 16 * (j / 4) + 4 * g + j % 4;
+        w[j] = s[j / 4][j % 4] * p.scale;
+        if (mixed) {
+          if (bad_now >> at & 1) w[j] = __builtin_nanf("");
+          if (!mine.holds(base + at)) w[j] = kNegInf;
+        }
+        most = __builtin_fmaxf(most, w[j]);
+      }
+      const float grown = __builtin_fmaxf(m, across_groups_max(most)), by = grown == kNegInf ? 0.f : grown;
+      if (__ballot(grown != m)) {
+        const float shrink = fast_exp2(m - by);
+        sum *= shrink;
+#pragma unroll
+        for (int c = 0; c < 2 * DT; ++c) acc[c] *= shrink;
+        m = grown;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = fast_exp2(w[j] - by);
+        sum += w[j];
+      }
+      if (!careful) {
+        // weights of 16 bits, as the values are: off by half a step each, which the sum over keys averages
+        Eight<T> weights;
+        weights.set(w);
+#pragma unroll
+        for (int c = 0; c < 2 * DT; ++c) acc[c] = mma(V::column(values, c, lane), weights, acc[c]);
+      } else {
+        // an infinity or NaN among the values, which a weight of 0 would let through: key by key, where it is seen
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll 1
+          for (int group = 0; group < 4; ++group) {
+            const int at = 16 * (j / 4) + 4 * group + j % 4;
+            const float weight = __shfl(w[j], 16 * group + col);
+            if (!mine.holds(base + at)) continue;
+#pragma unroll
+            for (int c = 0; c < 2 * DT; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[c][e] = __builtin_fmaf(weight, ElemTraits<T>::load1(values + at * V::kStride + 16 * c + 4 * g + e), acc[c][e]);
+          }
+      }
+    }
+  }
+
+  // The waves' parts, joined at the largest of their maxima.
+  sum = across_groups_sum(sum);
+  __syncthreads();
+  float* joined = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int c = 0; c < 2 * DT; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) joined[(wave * 32 * DT + 16 * c + 4 * g + e) * 17 + col] = acc[c][e];
+  if (g == 0) {
+    stat[0][wave][col] = m;
+    stat[1][wave][col] = sum;
+  }
+  __syncthreads();
+  const int64_t unit = blockIdx.x;
+  for (int i = static_cast<int>(threadIdx.x); i < kRowTile * p.D; i += 64 * kWaves) {
+    const int row = i / p.D, c = i - row * p.D;
+    float top = kNegInf, total = 0.f, value = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = __builtin_fmaxf(top, stat[0][w][row]);
+    const float by = top == kNegInf ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float shrink = fast_exp2(stat[0][w][row] - by);
+      total = __builtin_fmaf(stat[1][w][row], shrink, total);
+      value = __builtin_fmaf(joined[(w * 32 * DT + c) * 17 + row], shrink, value);
+    }
+    if (p.splits > 1) {
+      if (t.state == 1) {
+        p.part[(unit * kRowTile + row) * p.D + c] = value;
+        if (c == 0) {
+          float* stats = p.part + static_cast<int64_t>(gridDim.x) * kRowTile * p.D;
+          stats[(unit * kRowTile + row) * 2] = top;
+          stats[(unit * kRowTile + row) * 2 + 1] = total;
+        }
+      }
+    } else if (row0 + row < rows) {
+      const int token = (row0 + row) / p.G, head = t.h * p.G + row0 + row - token * p.G;
+      const float v = t.state < 0 ? __builtin_nanf("") : token < t.n ? value / total : 0.f;
+      ElemTraits<T>::store1(static_cast<T*>(p.out) + ((static_cast<int64_t>(t.b) * p.L + token) * p.Hq + head) * p.D + c, v);
+    }
+  }
+}
+
+// The splits of a tile, joined in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void enc_attention_join(AttentionParams p) {
+  const Tile t(p, blockIdx.x, 0);
+  const int rows = p.L * p.G, row0 = t.tile * kRowTile;
+  const int64_t unit0 = static_cast<int64_t>(blockIdx.x) * p.splits;
+  const float* stats = p.part + static_cast<int64_t>(gridDim.x) * p.splits * kRowTile * p.D;
+  for (int i = static_cast<int>(threadIdx.x); i < kRowTile * p.D; i += 256) {
+    const int row = i / p.D, c = i - row * p.D;
+    if (row0 + row >= rows) continue;
+    const int token = (row0 + row) / p.G, head = t.h * p.G + row0 + row - token * p.G;
+    float v = t.state < 0 ? __builtin_nanf("") : 0.f;
+    if (t.state >= 0 && token < t.n) {
+      float top = kNegInf, total = 0.f, value = 0.f;
+      for (int s = 0; s < p.splits; ++s) top = __builtin_fmaxf(top, stats[((unit0 + s) * kRowTile + row) * 2]);
+      const float by = top == kNegInf ? 0.f : top;
+      for (int s = 0; s < p.splits; ++s) {
+        const float* st = stats + ((unit0 + s) * kRowTile + row) * 2;
+        const float shrink = fast_exp2(st[0] - by);
+        total = __builtin_fmaf(st[1], shrink, total);
+        value = __builtin_fmaf(p.part[((unit0 + s) * kRowTile + row) * p.D + c], shrink, value);
+      }
+      v = value / total;
+    }
+    ElemTraits<T>::store1(static_cast<T*>(p.out) + ((static_cast<int64_t>(t.b) * p.L + token) * p.Hq + head) * p.D + c, v);
+  }
+}
+
+// ---- host ---------------------------------------------------------------------
+
+int64_t units_of(const rnnt_attention_shape_t& s) {
+  const int64_t rows = static_cast<int64_t>(s.L) * (s.Hq / s.Hkv);
+  return static_cast<int64_t>(s.B) * s.Hkv * ((rows + kRowTile - 1) / kRowTile);
+}
+
+bool whole_stride(int64_t stride, int64_t e) { return stride * e % 16 == 0; }
+
+rnnt_status_t check(const rnnt_attention_shape_t& s) {
+  if (s.B < 1 || s.L < 0 || s.Hq < 1 || s.Hkv < 1 || s.D < 1 || s.page < 1 || s.table < 1 || s.num_pages < 1 ||
+      s.Hq % s.Hkv != 0)
+    return RNNT_ERR_BAD_SHAPE;
+  const int64_t strides[9] = {s.q_stride_b, s.q_stride_t, s.q_stride_h, s.k_stride_b, s.k_stride_t,
+                              s.k_stride_h, s.v_stride_b, s.v_stride_t, s.v_stride_h};
+  for (const int64_t x : strides)
+    if (x < 0) return RNNT_ERR_BAD_SHAPE;
+  if (!net_dtype_known(s.dtype)) return RNNT_ERR_BAD_DTYPE;
+  for (const int64_t x : strides)
+    if (!whole_stride(x, net_elem_bytes(s.dtype))) return RNNT_ERR_ALIGNMENT;
+  if (s.D % 8 != 0 || s.D > 256 || (s.page & (s.page - 1)) != 0 || s.page > 1024) return RNNT_ERR_UNSUPPORTED;
+  if (s.num_pages > kMaxRows / s.page / s.Hkv || static_cast<int64_t>(s.L) * s.Hq > kMaxRows ||
+      static_cast<int64_t>(s.table) * s.page + s.L >= (int64_t{1} << 30))
+    return RNNT_ERR_UNSUPPORTED;
+  if (units_of(s) >= (int64_t{1} << 23)) return RNNT_ERR_UNSUPPORTED;
+  return RNNT_OK;
+}
+
+// Blocks that share a tile's keys out: few tiles over a long cache would leave most CUs idle.
+int splits_of(const rnnt_attention_shape_t& s) {
+  const int64_t units = units_of(s);
+  if (units == 0) return 1;
+  int64_t keys = static_cast<int64_t>(s.table) * s.page;
+  if (s.left >= 0 && static_cast<int64_t>(s.left) + s.L < keys) keys = static_cast<int64_t>(s.left) + s.L;
+  const int64_t by_grid = 1024 / units, by_keys = keys / (4 * kWaves * kKeys);
+  const int64_t n = by_grid < by_keys ? by_grid : by_keys;
+  return static_cast<int>(n < 1 ? 1 : n > 256 ? 256 : n);
+}
+
+size_t workspace_of(const rnnt_attention_shape_t& s) {
+  const int splits = splits_of(s);
+  if (splits == 1) return 0;
+  return net_align256(static_cast<size_t>(units_of(s)) * splits * kRowTile * (s.D + 2) * sizeof(float));
+}
+
+template <typename F>
+rnnt_status_t with_channels(int D, F&& f) {
+  using std::integral_constant;
+  if (D <= 32) return f(integral_constant<int, 1>{});
+  if (D <= 64) return f(integral_constant<int, 2>{});
+  if (D <= 96) return f(integral_constant<int, 3>{});
+  if (D <= 128) return f(integral_constant<int, 4>{});
+  return f(integral_constant<int, 8>{});
+}
+
+}  // namespace
+}  // namespace rnnt
+
+using namespace rnnt;
+
+extern "C" {
+
+size_t rnnt_cached_attention_workspace_bytes(rnnt_attention_shape_t shape) {
+  return check(shape) == RNNT_OK ? workspace_of(shape) : 0;
+}
+
+rnnt_status_t rnnt_cached_attention(const void* q, const void* k, const void* v, rnnt_attention_shape_t shape,
+                                    const int32_t* lens, const int32_t* cached, const int32_t* pages, void* k_cache,
+                                    void* v_cache, float scale, void* out, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream) {
+  const rnnt_attention_shape_t& s = shape;
+  rnnt_status_t st = check(s);
+  if (st != RNNT_OK) return st;
+  if (!__builtin_isfinite(scale)) return RNNT_ERR_BAD_VARIANT;
+  if (!cached || !pages || !k_cache || !v_cache || (s.L > 0 && (!q || !k || !v || !out))) return RNNT_ERR_NULL_PTR;
+  if (!multiple_of(16, q) || !multiple_of(16, k) || !multiple_of(16, v) || !multiple_of(16, k_cache) ||
+      !multiple_of(16, v_cache) || !multiple_of(net_elem_bytes(s.dtype), out))
+    return RNNT_ERR_ALIGNMENT;
+  if (s.L == 0) return RNNT_OK;
+  Workspace ws;
+  st = ws.take(workspace, workspace_bytes, workspace_of(s), stream);
+  if (st != RNNT_OK) return st;
+  AttentionParams p{};
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.k_cache = k_cache;
+  p.v_cache = v_cache;
+  p.out = out;
+  p.lens = lens;
+  p.cached = cached;
+  p.pages = pages;
+  p.part = reinterpret_cast<float*>(ws.ptr);
+  p.q_stride_b = s.q_stride_b;
+  p.q_stride_t = s.q_stride_t;
+  p.q_stride_h = s.q_stride_h;
+  p.k_stride_b = s.k_stride_b;
+  p.k_stride_t = s.k_stride_t;
+  p.k_stride_h = s.k_stride_h;
+  p.v_stride_b = s.v_stride_b;
+  p.v_stride_t = s.v_stride_t;
+  p.v_stride_h = s.v_stride_h;
+  p.B = s.B;
+  p.L = s.L;
+  p.Hq = s.Hq;
+  p.Hkv = s.Hkv;
+  p.G = s.Hq / s.Hkv;
+  p.D = s.D;
+  p.shift = __builtin_ctz(static_cast<unsigned>(s.page));
+  p.table = s.table;
+  p.num_pages = s.num_pages;
+  p.causal = s.causal != 0;
+  p.left = s.left < 0 ? -1 : s.left;
+  p.tiles = static_cast<int32_t>((static_cast<int64_t>(s.L) * p.G + kRowTile - 1) / kRowTile);
+  p.splits = splits_of(s);
+  p.scale = scale * kLog2eF;
+  const int64_t units = units_of(s);
+  return with_dtype(s.dtype, [&](auto t) {
+    using T = decltype(t);
+    st = with_channels(s.D, [&](auto channels) {
+      hipLaunchKernelGGL((enc_attention<T, decltype(channels)::value>), dim3(static_cast<uint32_t>(units * p.splits)),
+                         dim3(64 * kWaves), 0, stream, p);
+      return launched();
+    });
+    if (st != RNNT_OK || p.splits == 1) return st;
+    hipLaunchKernelGGL((enc_attention_join<T>), dim3(static_cast<uint32_t>(units)), dim3(256), 0, stream, p);
+    return launched();
+  });
+}
+
+}  // extern "C"
