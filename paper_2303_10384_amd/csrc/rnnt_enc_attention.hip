@@ -20,9 +20,12 @@ struct AttentionParams {
   const int32_t *lens, *cached, *pages;
   float* part;  // of the splits: sums over values, then {maximum, sum of weights}
   int64_t q_stride_b, q_stride_t, q_stride_h, k_stride_b, k_stride_t, k_stride_h, v_stride_b, v_stride_t, v_stride_h;
-  int32_t B, L, Hq, Hkv, G, D, shift, table, num_pages, causal, left, tiles, splits;
-  float scale;  // times log2 e
+  int32_t B, L, Hq, Hkv, G, D, shift, table, num_pages, causal, left;
+  int32_t rows, tiles, splits;  // rows of a tile, tiles of an utterance's head of keys, blocks to a tile
+  float scale;                  // times log2 e
 };
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kNegInf = -__builtin_inff();
 constexpr int kRowTile = 16;  // rows (tokens times the heads that share keys) to a block
@@ -47,10 +50,7 @@ struct Tile {
     table = PageTable{p.pages + static_cast<int64_t>(b) * p.table, p.table, p.num_pages, p.shift};
     const bool fits = lengths_fit(n, p.L, cached, static_cast<int64_t>(p.table) << p.shift);
     end = cached + n;
-    state = !fits ? -1 : static_cast<int64_t>(tile) * kRowTile < static_cast<int64_t>(n) * p.G;
-  }
-  __device__ __forceinline__ int token(const AttentionParams& p, int row) const {
-    return (tile * kRowTile + row) / p.G;
+    state = !fits ? -1 : static_cast<int64_t>(tile) * p.rows < static_cast<int64_t>(n) * p.G;
   }
 };
 
@@ -374,39 +374,325 @@ __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) 
   }
 }
 
-// The splits of a tile, joined in their order.
+// ---- many rows ------------------------------------------------------------------------------
+// A block of four waves takes 128 rows, 32 to a wave, and steps of 64 keys, whose rows go through registers (asked for a
+// step ahead, their pages two) into LDS, for all four waves: sixteen rows to a block would read every key
+// eight times as often.  Products of 32 x 32 x 16, transposed as above; half g of a wave holds the keys 8 (e / 4) + 4 g + e % 4
+// of a group of 32, in the scores and in the values alike.
+constexpr int kWideRows = 32, kWideKeys = 64;
+
+template <typename T>
+__device__ __forceinline__ f32x16 mma32(const Eight<T>& a, const Eight<T>& b, f32x16 c) {
+  if constexpr (__is_same(T, bf16_t))
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.w[0]), __builtin_bit_cast(bf16x8, b.w[0]), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a.w[0]), __builtin_bit_cast(f16x8, b.w[0]), c, 0, 0, 0);
+}
+
+template <typename T, int DT>
+__global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionParams p) {
+  constexpr int kPieces = 4 * DT;                                   // 16-byte pieces of a row
+  constexpr int kPitch = DT == 1 ? 4 : DT == 2 ? 8 : DT <= 4 ? 16 : 32;  // ... of a row of keys in LDS
+  constexpr int kRowsOfBanks = kPitch >= 16 ? 1 : 16 / kPitch;      // rows that meet all banks once
+  constexpr int kMask = (kPitch < 16 ? kPitch : 16) - 1;
+  constexpr int kValueStride = 32 * DT + 16;                        // elements of a row of values in LDS
+  constexpr int kLoads = kWideKeys * kPieces / 256;
+  __shared__ __attribute__((aligned(16))) u32x4 keys[kWideKeys * kPitch];
+  __shared__ __attribute__((aligned(16))) T values[kWideKeys * kValueStride];
+  __shared__ uint32_t flags[2][3];  // of a step, in turn: keys whose page is none, and whether a value is no number
+  const int thread = static_cast<int>(threadIdx.x), lane = thread & 63, wave = thread >> 6;
+  const int g = lane >> 5, col = lane & 31;
+  const Tile t(p, blockIdx.x / p.splits, static_cast<int>(blockIdx.x % p.splits));
+  if (t.split == 0 && t.state == 1) write_cache<T>(p, t, p.rows);
+  const int rows = p.L * p.G, row0 = t.tile * p.rows, wave_row0 = row0 + wave * kWideRows;
+
+  float m = kNegInf, sum = 0.f;  // the maximum before the scale
+  f32x16 acc[DT];
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[c][e] = 0.f;
+  const float scale = __builtin_fabsf(p.scale);
+
+  if (t.state == 1) {
+    const int all_rows = t.n * p.G, last_row = min(row0 + p.rows, all_rows) - 1;
+    const int my_row = min(wave_row0 + col, last_row), my_token = my_row / p.G;
+    const auto seen = [&](int row) { return Seen(t.cached + row / p.G, t.end, p.causal != 0, p.left); };
+    const Seen mine(t.cached + my_token, t.end, p.causal != 0, p.left);
+    const Seen first = seen(row0), last = seen(last_row);
+    const Seen wave_first = seen(min(wave_row0, last_row)), wave_last = seen(min(wave_row0 + kWideRows - 1, last_row));
+    const int lo = first.lo, hi = last.hi;
+    const int steps = (hi - lo + kWideKeys - 1) / kWideKeys;
+    const int begin = static_cast<int>(static_cast<int64_t>(steps) * t.split / p.splits);
+    const int stop = static_cast<int>(static_cast<int64_t>(steps) * (t.split + 1) / p.splits);
+
+    const T* k_new = static_cast<const T*>(p.k) + t.b * p.k_stride_b + t.h * p.k_stride_h;
+    const T* v_new = static_cast<const T*>(p.v) + t.b * p.v_stride_b + t.h * p.v_stride_h;
+    const T *k_cache = static_cast<const T*>(p.k_cache), *v_cache = static_cast<const T*>(p.v_cache);
+
+    Eight<T> q[2 * DT];
+    {
+      const T* from = static_cast<const T*>(p.q) + t.b * p.q_stride_b + my_token * p.q_stride_t +
+                      (t.h * p.G + my_row - my_token * p.G) * p.q_stride_h;
+      const uint32_t sign = p.scale < 0.f ? 0x80008000u : 0u;  // the largest score is then the largest product
+#pragma unroll
+      for (int d = 0; d < 2 * DT; ++d) {
+        q[d].zero();
+        if (16 * d + 8 * g < p.D) q[d].load(from + 16 * d + 8 * g);
+        q[d].w[0] ^= u32x4{sign, sign, sign, sign};
+      }
+    }
+
+    Eight<T> kk[kLoads], vv[kLoads];
+    int id[kLoads];
+    uint32_t bad = 0;
+    const auto ask = [&](int step) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        id[i] = t.table.pages[min(lo + step * kWideKeys + (i * 256 + thread) / kPieces, hi - 1) >> p.shift];
+    };
+    const auto fetch = [&](int step) {
+      bad = 0;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int piece = (i * 256 + thread) % kPieces, pos = min(lo + step * kWideKeys + (i * 256 + thread) / kPieces, hi - 1);
+        const uint32_t row = static_cast<uint32_t>(id[i]) >= static_cast<uint32_t>(p.num_pages) ? kBadRow
+                             : pos >= t.cached ? kNewRow | static_cast<uint32_t>(pos - t.cached)
+                                               : cache_row(id[i], p.Hkv, t.h, pos, p.shift);
+        if (row == kBadRow) bad |= 1u << i;
+        const int c = min(8 * piece, p.D - 8);  // behind D: what is there meets zeros of q, or a channel that is not stored
+        kk[i].load(row_pointer(k_cache, k_new, p.k_stride_t, row, p.D) + c);
+        vv[i].load(row_pointer(v_cache, v_new, p.v_stride_t, row, p.D) + c);
+        if (8 * piece >= p.D) kk[i].zero(), vv[i].zero();
+      }
+    };
+    if (thread < 6) flags[thread / 3][thread % 3] = 0;
+    if (begin < stop) {
+      ask(begin);
+      fetch(begin);
+      if (begin + 1 < stop) ask(begin + 1);
+    }
+    for (int step = begin; step < stop; ++step) {
+      const int base = lo + step * kWideKeys, turn = (step - begin) & 1;
+      const bool block_mixed = base < last.lo || base + kWideKeys > first.hi;
+      __syncthreads();
+      if (thread < 3) flags[turn ^ 1][thread] = 0;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = (i * 256 + thread) / kPieces, piece = (i * 256 + thread) % kPieces;
+        keys[row * kPitch + (piece ^ (row / kRowsOfBanks & kMask))] = kk[i].w[0];
+        vv[i].store(values + row * kValueStride + 8 * piece);
+        if (bad >> i & 1) atomicOr(&flags[turn][row / 32], 1u << (row % 32));
+        if (block_mixed && vv[i].odd()) flags[turn][2] = 1;
+      }
+      __syncthreads();
+      if (step + 1 < stop) {
+        fetch(step + 1);
+        if (step + 2 < stop) ask(step + 2);
+      }
+      if (base >= wave_last.hi || base + kWideKeys <= wave_first.lo) continue;  // nothing that the wave's rows see
+      const uint32_t none[2] = {flags[turn][0], flags[turn][1]};
+      const bool mixed = base < wave_last.lo || base + kWideKeys > wave_first.hi || (none[0] | none[1]) != 0;
+      const bool careful = mixed && flags[turn][2] != 0;
+      f32x16 s[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+#pragma unroll
+        for (int d = 0; d < 2 * DT; ++d) {
+          const int row = 32 * i + col;
+          Eight<T> a;
+          a.w[0] = keys[row * kPitch + ((2 * d + g) ^ (row / kRowsOfBanks & kMask))];
+          s[i] = mma32(a, q[d], s[i]);
+        }
+      }
+      float most = kNegInf;
+      uint32_t hidden[2] = {0, 0};  // bit e of half i: this lane's row does not see the key
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if (mixed) {
+            const int at = 8 * (e / 4) + 4 * g + e % 4;
+            if (none[i] >> at & 1) s[i][e] = __builtin_nanf("");
+            const bool away = !mine.holds(base + 32 * i + at);
+            hidden[i] |= static_cast<uint32_t>(away) << e;
+            s[i][e] = away ? kNegInf : s[i][e];
+          }
+          most = __builtin_fmaxf(most, s[i][e]);
+        }
+      most = __builtin_fmaxf(most, __shfl_xor(most, 32));
+      const float grown = __builtin_fmaxf(m, most);
+      if (__ballot(grown != m)) {
+        const float shrink = m == kNegInf ? 0.f : fast_exp2((m - grown) * scale);
+        sum *= shrink;
+#pragma unroll
+        for (int c = 0; c < DT; ++c) acc[c] *= shrink;
+        m = grown;
+      }
+      const float by = m == kNegInf ? 0.f : m * scale;
+      Eight<T> weights[4];
+      if (mixed) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[i][e] = hidden[i] >> e & 1 ? 0.f : fast_exp2(__builtin_fmaf(s[i][e], scale, -by));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[i][e] = fast_exp2(__builtin_fmaf(s[i][e], scale, -by));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += s[i][e];
+      if (!careful) {
+        // weights of 16 bits, as the values are
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          float w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = s[b / 2][8 * (b % 2) + j];
+          weights[b].set(w);
+        }
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            Eight<T> a;
+            const int i = lane & 15;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const T* at = values + (16 * b + 8 * half + 4 * g + (i >> 2)) * kValueStride + 32 * c + 16 * (lane >> 4 & 1) + 4 * (i & 3);
+              const i16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at);
+              const auto two = __builtin_bit_cast(uint2, four);
+              a.w[0][2 * half] = two.x;
+              a.w[0][2 * half + 1] = two.y;
+            }
+            acc[c] = mma32(a, weights[b], acc[c]);
+          }
+      } else {
+        // an infinity or NaN among the values: key by key, where it is seen
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+#pragma unroll 1
+            for (int from = 0; from < 2; ++from) {
+              const int at = 32 * i + 8 * (e / 4) + 4 * from + e % 4;
+              const float weight = __shfl(s[i][e], 32 * from + col);
+              if (!mine.holds(base + at)) continue;
+#pragma unroll
+              for (int c = 0; c < DT; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                  acc[c][r] = __builtin_fmaf(weight, ElemTraits<T>::load1(values + at * kValueStride + 32 * c + 8 * (r / 4) + 4 * g + r % 4), acc[c][r]);
+            }
+      }
+    }
+  }
+
+  sum += __shfl_xor(sum, 32);
+  const int row = wave_row0 + col;
+  const bool ends = p.splits == 1;
+  if (!ends && t.state != 1) return;
+  float* part = p.part + (static_cast<int64_t>(blockIdx.x) * p.rows + wave * kWideRows + col) * p.D;
+  if (!ends && g == 0) {
+    float* stats = p.part + static_cast<int64_t>(gridDim.x) * p.rows * p.D +
+                   (static_cast<int64_t>(blockIdx.x) * p.rows + wave * kWideRows + col) * 2;
+    stats[0] = m == kNegInf ? m : m * scale;
+    stats[1] = sum;
+  }
+  if (ends && row >= rows) return;
+  const int token = row / p.G, head = t.h * p.G + row - token * p.G;
+  const bool valid = t.state == 1 && token < t.n;
+  const float fill = t.state < 0 ? __builtin_nanf("") : 0.f, by = 1.f / sum;
+  T* out = static_cast<T*>(p.out) + ((static_cast<int64_t>(t.b) * p.L + token) * p.Hq + head) * p.D;
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = 32 * c + 8 * e + 4 * g;
+      if (at >= p.D) continue;
+      float v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = ends ? (valid ? acc[c][4 * e + j] * by : fill) : acc[c][4 * e + j];
+      if (ends) {
+        Pack<T, 4> k;
+        k.set(v);
+        k.store(out + at);
+      } else {
+        *reinterpret_cast<f32x4*>(part + at) = f32x4{v[0], v[1], v[2], v[3]};
+      }
+    }
+}
+
+// ---- the splits of a row, joined in their order --------------------------------------------------
+// A block to a row: the splits' factors in LDS, then four channels to a thread and every eighth split or so, and the
+// threads' sums.  (A block to sixteen rows that went over the splits in turn took 175 us for 48 rows of 117 splits.)
+constexpr int kMostSplits = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void enc_attention_join(AttentionParams p) {
-  const Tile t(p, blockIdx.x, 0);
-  const int rows = p.L * p.G, row0 = t.tile * kRowTile;
-  const int64_t unit0 = static_cast<int64_t>(blockIdx.x) * p.splits;
-  const float* stats = p.part + static_cast<int64_t>(gridDim.x) * p.splits * kRowTile * p.D;
-  for (int i = static_cast<int>(threadIdx.x); i < kRowTile * p.D; i += 256) {
-    const int row = i / p.D, c = i - row * p.D;
-    if (row0 + row >= rows) continue;
-    const int token = (row0 + row) / p.G, head = t.h * p.G + row0 + row - token * p.G;
-    float v = t.state < 0 ? __builtin_nanf("") : 0.f;
-    if (t.state >= 0 && token < t.n) {
-      float top = kNegInf, total = 0.f, value = 0.f;
-      for (int s = 0; s < p.splits; ++s) top = __builtin_fmaxf(top, stats[((unit0 + s) * kRowTile + row) * 2]);
-      const float by = top == kNegInf ? 0.f : top;
-      for (int s = 0; s < p.splits; ++s) {
-        const float* st = stats + ((unit0 + s) * kRowTile + row) * 2;
-        const float shrink = fast_exp2(st[0] - by);
-        total = __builtin_fmaf(st[1], shrink, total);
-        value = __builtin_fmaf(p.part[((unit0 + s) * kRowTile + row) * p.D + c], shrink, value);
-      }
-      v = value / total;
-    }
-    ElemTraits<T>::store1(static_cast<T*>(p.out) + ((static_cast<int64_t>(t.b) * p.L + token) * p.Hq + head) * p.D + c, v);
+  __shared__ float factor[kMostSplits], lds[4], total_lds[4];
+  __shared__ f32x4 sums[256];
+  const int64_t unit = blockIdx.x / p.rows;
+  const int in_tile = static_cast<int>(blockIdx.x % p.rows), thread = static_cast<int>(threadIdx.x);
+  const Tile t(p, unit, 0);
+  const int row = t.tile * p.rows + in_tile;
+  if (row >= p.L * p.G) return;
+  const int token = row / p.G, head = t.h * p.G + row - token * p.G;
+  T* out = static_cast<T*>(p.out) + ((static_cast<int64_t>(t.b) * p.L + token) * p.Hq + head) * p.D;
+  if (t.state < 0 || token >= t.n) {
+    const float fill = t.state < 0 ? __builtin_nanf("") : 0.f;
+    for (int c = thread; c < p.D; c += 256) ElemTraits<T>::store1(out + c, fill);
+    return;
   }
+  const int64_t first = unit * p.splits * p.rows + in_tile;  // the first split's row
+  const float* stats = p.part + static_cast<int64_t>(gridDim.x) * p.splits * p.D;
+  float top = kNegInf, weight = 0.f;
+  if (thread < p.splits) {
+    top = stats[(first + static_cast<int64_t>(thread) * p.rows) * 2];
+    weight = stats[(first + static_cast<int64_t>(thread) * p.rows) * 2 + 1];
+  }
+  const float mine = top;
+  top = group_reduce<64, MaxOp>(top, kNegInf);
+  if ((thread & 63) == 0) lds[thread >> 6] = top;
+  __syncthreads();
+  top = __builtin_fmaxf(__builtin_fmaxf(lds[0], lds[1]), __builtin_fmaxf(lds[2], lds[3]));
+  const float by = top == kNegInf ? 0.f : top, shrink = thread < p.splits ? fast_exp2(mine - by) : 0.f;
+  factor[thread] = shrink;
+  weight = group_reduce<64, SumOp>(weight * shrink, 0.f);
+  if ((thread & 63) == 0) total_lds[thread >> 6] = weight;
+  __syncthreads();
+  const float total = total_lds[0] + total_lds[1] + total_lds[2] + total_lds[3];
+  const int lanes = p.D / 4, groups = 256 / lanes, group = thread / lanes, c = 4 * (thread - group * lanes);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (group < groups) {
+#pragma unroll 4
+    for (int s = group; s < p.splits; s += groups)
+      sum += factor[s] * *reinterpret_cast<const f32x4*>(p.part + (first + static_cast<int64_t>(s) * p.rows) * p.D + c);
+  }
+  sums[thread] = sum;
+  __syncthreads();
+  if (group != 0) return;
+  for (int i = 1; i < groups; ++i) sum += sums[i * lanes + thread];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) ElemTraits<T>::store1(out + c + j, sum[j] / total);
 }
 
 // ---- host ---------------------------------------------------------------------
 
+// Whether the rows of an utterance's head of keys fill wide tiles
+bool wide(const rnnt_attention_shape_t& s) {
+  return s.dtype != RNNT_DTYPE_F32 && s.D <= 128 && static_cast<int64_t>(s.L) * (s.Hq / s.Hkv) > 32;
+}
+int rows_of(const rnnt_attention_shape_t& s) { return wide(s) ? kWaves * kWideRows : kRowTile; }
+
 int64_t units_of(const rnnt_attention_shape_t& s) {
-  const int64_t rows = static_cast<int64_t>(s.L) * (s.Hq / s.Hkv);
-  return static_cast<int64_t>(s.B) * s.Hkv * ((rows + kRowTile - 1) / kRowTile);
+  const int64_t rows = static_cast<int64_t>(s.L) * (s.Hq / s.Hkv), tile = rows_of(s);
+  return static_cast<int64_t>(s.B) * s.Hkv * ((rows + tile - 1) / tile);
 }
 
 bool whole_stride(int64_t stride, int64_t e) { return stride * e % 16 == 0; }
@@ -436,15 +722,15 @@ int splits_of(const rnnt_attention_shape_t& s) {
   if (units == 0) return 1;
   int64_t keys = static_cast<int64_t>(s.table) * s.page;
   if (s.left >= 0 && static_cast<int64_t>(s.left) + s.L < keys) keys = static_cast<int64_t>(s.left) + s.L;
-  const int64_t by_grid = 1024 / units, by_keys = keys / (4 * kWaves * kKeys);
+  const int64_t by_grid = (wide(s) ? 512 : 1024) / units, by_keys = keys / 512;
   const int64_t n = by_grid < by_keys ? by_grid : by_keys;
-  return static_cast<int>(n < 1 ? 1 : n > 256 ? 256 : n);
+  return static_cast<int>(n < 1 ? 1 : n > kMostSplits ? kMostSplits : n);
 }
 
 size_t workspace_of(const rnnt_attention_shape_t& s) {
   const int splits = splits_of(s);
   if (splits == 1) return 0;
-  return net_align256(static_cast<size_t>(units_of(s)) * splits * kRowTile * (s.D + 2) * sizeof(float));
+  return net_align256(static_cast<size_t>(units_of(s)) * splits * rows_of(s) * (s.D + 2) * sizeof(float));
 }
 
 template <typename F>
@@ -515,19 +801,27 @@ rnnt_status_t rnnt_cached_attention(const void* q, const void* k, const void* v,
   p.num_pages = s.num_pages;
   p.causal = s.causal != 0;
   p.left = s.left < 0 ? -1 : s.left;
-  p.tiles = static_cast<int32_t>((static_cast<int64_t>(s.L) * p.G + kRowTile - 1) / kRowTile);
+  p.rows = rows_of(s);
+  p.tiles = static_cast<int32_t>((static_cast<int64_t>(s.L) * p.G + p.rows - 1) / p.rows);
   p.splits = splits_of(s);
   p.scale = scale * kLog2eF;
   const int64_t units = units_of(s);
   return with_dtype(s.dtype, [&](auto t) {
     using T = decltype(t);
+    const dim3 grid(static_cast<uint32_t>(units * p.splits)), block(64 * kWaves);
     st = with_channels(s.D, [&](auto channels) {
-      hipLaunchKernelGGL((enc_attention<T, decltype(channels)::value>), dim3(static_cast<uint32_t>(units * p.splits)),
-                         dim3(64 * kWaves), 0, stream, p);
+      constexpr int DT = decltype(channels)::value;
+      if constexpr (sizeof(T) == 2 && DT <= 4) {
+        if (wide(s)) {
+          hipLaunchKernelGGL((enc_attention_wide<T, DT>), grid, block, 0, stream, p);
+          return launched();
+        }
+      }
+      hipLaunchKernelGGL((enc_attention<T, DT>), grid, block, 0, stream, p);
       return launched();
     });
     if (st != RNNT_OK || p.splits == 1) return st;
-    hipLaunchKernelGGL((enc_attention_join<T>), dim3(static_cast<uint32_t>(units)), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((enc_attention_join<T>), dim3(static_cast<uint32_t>(units * p.rows)), dim3(256), 0, stream, p);
     return launched();
   });
 }
