@@ -41,7 +41,7 @@ struct Tile {
   PageTable table;
 
   __device__ __forceinline__ Tile(const AttentionParams& p, int64_t unit, int split_) : split(split_) {
-    tile = static_cast<int>(unit % p.tiles);
+    tile = p.tiles - 1 - static_cast<int>(unit % p.tiles);  // the later ones, which see more, begin first
     const int bh = static_cast<int>(unit / p.tiles);
     b = bh / p.Hkv;
     h = bh - b * p.Hkv;
@@ -62,10 +62,13 @@ __device__ __forceinline__ uint32_t row_of(const AttentionParams& p, const Tile&
   return pos >= t.cached ? kNewRow | static_cast<uint32_t>(pos - t.cached) : cache_row(id, p.Hkv, t.h, pos, p.shift);
 }
 
+// A key's row without a branch: one of two bases, and one product.  A bad row is the chunk's first, a valid address; its
+// key is NaN wherever it is seen.
 template <typename T>
 __device__ __forceinline__ const T* row_pointer(const T* cache, const T* fresh, int64_t stride_t, uint32_t row, int D) {
-  if (row == kBadRow) return fresh;  // a valid address; its key is NaN wherever it is seen
-  return row & kNewRow ? fresh + static_cast<int64_t>(row & ~kNewRow) * stride_t : cache + static_cast<int64_t>(row) * D;
+  const bool own = row & kNewRow;
+  const uint32_t index = row == kBadRow ? 0u : row & ~kNewRow, by = own ? static_cast<uint32_t>(stride_t) : static_cast<uint32_t>(D);
+  return (own ? fresh : cache) + static_cast<uint64_t>(index) * by;
 }
 
 // ---- eight elements in a matrix instruction's order ------------------------------
@@ -94,6 +97,15 @@ struct Eight {
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[0][i] = Pack<T, 2>::pack2(f[2 * i], f[2 * i + 1]);
+    }
+  }
+  // (16 bits) infinities and NaN become 0
+  __device__ __forceinline__ void clear_odd() {
+    constexpr uint32_t kExp = __is_same(T, bf16_t) ? 0x7f80u : 0x7c00u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = w[0][i];
+      w[0][i] = ((x & kExp) == kExp ? 0u : x & 0xffffu) | ((x >> 16 & kExp) == kExp ? 0u : x & 0xffff0000u);
     }
   }
   // an infinity or NaN among them
@@ -197,7 +209,7 @@ __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) 
   constexpr int kJoinBytes = kWaves * 32 * DT * 17 * 4;
   __shared__ __attribute__((aligned(16))) char lds[kValueBytes > kJoinBytes ? kValueBytes : kJoinBytes];
   __shared__ float stat[2][kWaves][16];
-  const int lane = static_cast<int>(threadIdx.x) & 63, wave = static_cast<int>(threadIdx.x) >> 6;
+  const int lane = static_cast<int>(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int g = lane >> 4, col = lane & 15;
   const Tile t(p, blockIdx.x / p.splits, static_cast<int>(blockIdx.x % p.splits));
   if (t.split == 0 && t.state == 1) write_cache<T>(p, t, kRowTile);
@@ -400,7 +412,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
   __shared__ __attribute__((aligned(16))) u32x4 keys[kWideKeys * kPitch];
   __shared__ __attribute__((aligned(16))) T values[kWideKeys * kValueStride];
   __shared__ uint32_t flags[2][3];  // of a step, in turn: keys whose page is none, and whether a value is no number
-  const int thread = static_cast<int>(threadIdx.x), lane = thread & 63, wave = thread >> 6;
+  const int thread = static_cast<int>(threadIdx.x), lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int g = lane >> 5, col = lane & 31;
   const Tile t(p, blockIdx.x / p.splits, static_cast<int>(blockIdx.x % p.splits));
   if (t.split == 0 && t.state == 1) write_cache<T>(p, t, p.rows);
@@ -456,14 +468,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int piece = (i * 256 + thread) % kPieces, pos = min(lo + step * kWideKeys + (i * 256 + thread) / kPieces, hi - 1);
-        const uint32_t row = static_cast<uint32_t>(id[i]) >= static_cast<uint32_t>(p.num_pages) ? kBadRow
-                             : pos >= t.cached ? kNewRow | static_cast<uint32_t>(pos - t.cached)
-                                               : cache_row(id[i], p.Hkv, t.h, pos, p.shift);
-        if (row == kBadRow) bad |= 1u << i;
-        const int c = min(8 * piece, p.D - 8);  // behind D: what is there meets zeros of q, or a channel that is not stored
+        const bool none = static_cast<uint32_t>(id[i]) >= static_cast<uint32_t>(p.num_pages);
+        const uint32_t there = cache_row(id[i], p.Hkv, t.h, pos, p.shift), own = kNewRow | static_cast<uint32_t>(pos - t.cached);
+        const uint32_t row = none ? kBadRow : pos >= t.cached ? own : there;
+        bad |= static_cast<uint32_t>(none) << i;
+        // behind D: the last piece again; a score's channels there are taken as 0, the output's are not stored
+        const int c = min(8 * piece, p.D - 8);
         kk[i].load(row_pointer(k_cache, k_new, p.k_stride_t, row, p.D) + c);
         vv[i].load(row_pointer(v_cache, v_new, p.v_stride_t, row, p.D) + c);
-        if (8 * piece >= p.D) kk[i].zero(), vv[i].zero();
       }
     };
     if (thread < 6) flags[thread / 3][thread % 3] = 0;
@@ -480,10 +492,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int row = (i * 256 + thread) / kPieces, piece = (i * 256 + thread) % kPieces;
-        keys[row * kPitch + (piece ^ (row / kRowsOfBanks & kMask))] = kk[i].w[0];
+        keys[row * kPitch + (piece ^ (row / kRowsOfBanks & kMask))] = 8 * piece < p.D ? kk[i].w[0] : u32x4{0, 0, 0, 0};
+        if (block_mixed && vv[i].odd()) {
+          flags[turn][2] = 1;
+          vv[i].clear_odd();
+        }
         vv[i].store(values + row * kValueStride + 8 * piece);
         if (bad >> i & 1) atomicOr(&flags[turn][row / 32], 1u << (row % 32));
-        if (block_mixed && vv[i].odd()) flags[turn][2] = 1;
       }
       __syncthreads();
       if (step + 1 < stop) {
@@ -491,9 +506,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
         if (step + 2 < stop) ask(step + 2);
       }
       if (base >= wave_last.hi || base + kWideKeys <= wave_first.lo) continue;  // nothing that the wave's rows see
-      const uint32_t none[2] = {flags[turn][0], flags[turn][1]};
+      const auto flag = [&](int i) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(flags[turn][i]))); };
+      const uint32_t none[2] = {flag(0), flag(1)};
       const bool mixed = base < wave_last.lo || base + kWideKeys > wave_first.hi || (none[0] | none[1]) != 0;
-      const bool careful = mixed && flags[turn][2] != 0;
+      const bool careful = flag(2) != 0;
       f32x16 s[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -507,21 +523,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
           s[i] = mma32(a, q[d], s[i]);
         }
       }
+      // whether the lane's row sees key `at` of the step
+      const uint32_t from = static_cast<uint32_t>(base + 4 * g - mine.lo), span = static_cast<uint32_t>(mine.hi - mine.lo);
+      const auto sees = [&](int i, int e) { return from + (32 * i + 8 * (e / 4) + e % 4) < span; };
+      if (mixed) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float v = none[i] >> (8 * (e / 4) + 4 * g + e % 4) & 1 ? __builtin_nanf("") : s[i][e];
+            s[i][e] = sees(i, e) ? v : kNegInf;
+          }
+      }
       float most = kNegInf;
-      uint32_t hidden[2] = {0, 0};  // bit e of half i: this lane's row does not see the key
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (mixed) {
-            const int at = 8 * (e / 4) + 4 * g + e % 4;
-            if (none[i] >> at & 1) s[i][e] = __builtin_nanf("");
-            const bool away = !mine.holds(base + 32 * i + at);
-            hidden[i] |= static_cast<uint32_t>(away) << e;
-            s[i][e] = away ? kNegInf : s[i][e];
-          }
-          most = __builtin_fmaxf(most, s[i][e]);
-        }
+        for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
       most = __builtin_fmaxf(most, __shfl_xor(most, 32));
       const float grown = __builtin_fmaxf(m, most);
       if (__ballot(grown != m)) {
@@ -533,63 +551,68 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
       }
       const float by = m == kNegInf ? 0.f : m * scale;
       Eight<T> weights[4];
-      if (mixed) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[i][e] = fast_exp2(__builtin_fmaf(s[i][e], scale, -by));
+      if (mixed) {  // 0 also where a scale of 0 made NaN of what is not seen
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[i][e] = hidden[i] >> e & 1 ? 0.f : fast_exp2(__builtin_fmaf(s[i][e], scale, -by));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[i][e] = fast_exp2(__builtin_fmaf(s[i][e], scale, -by));
+          for (int e = 0; e < 16; ++e) s[i][e] = sees(i, e) ? s[i][e] : 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sum += s[i][e];
-      if (!careful) {
-        // weights of 16 bits, as the values are
+      // weights of 16 bits, as the values are
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          float w[8];
+      for (int b = 0; b < 4; ++b) {
+        float w[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = s[b / 2][8 * (b % 2) + j];
-          weights[b].set(w);
+        for (int j = 0; j < 8; ++j) w[j] = s[b / 2][8 * (b % 2) + j];
+        weights[b].set(w);
+      }
+      // the values of channel 32 c + lane % 32 and the sixteen keys b of the step, of which the lane holds eight
+      const auto column = [&](int c, int b) {
+        Eight<T> a;
+        const int i = lane & 15;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const T* at = values + (16 * b + 8 * half + 4 * g + (i >> 2)) * kValueStride + 32 * c + 16 * (lane >> 4 & 1) + 4 * (i & 3);
+          const i16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at);
+          const auto two = __builtin_bit_cast(uint2, four);
+          a.w[0][2 * half] = two.x;
+          a.w[0][2 * half + 1] = two.y;
         }
+        return a;
+      };
 #pragma unroll
-        for (int c = 0; c < DT; ++c)
+      for (int c = 0; c < DT; ++c)
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            Eight<T> a;
-            const int i = lane & 15;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const T* at = values + (16 * b + 8 * half + 4 * g + (i >> 2)) * kValueStride + 32 * c + 16 * (lane >> 4 & 1) + 4 * (i & 3);
-              const i16x4 four = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at);
-              const auto two = __builtin_bit_cast(uint2, four);
-              a.w[0][2 * half] = two.x;
-              a.w[0][2 * half + 1] = two.y;
-            }
-            acc[c] = mma32(a, weights[b], acc[c]);
-          }
-      } else {
-        // an infinity or NaN among the values: key by key, where it is seen
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
+        for (int b = 0; b < 4; ++b) acc[c] = mma32(column(c, b), weights[b], acc[c]);
+      if (careful) {
+        // An infinity or NaN among the values, which a weight of 0 would have let through, went into LDS as 0: it reaches the
+        // rows that see its key from here.
 #pragma unroll 1
-            for (int from = 0; from < 2; ++from) {
-              const int at = 32 * i + 8 * (e / 4) + 4 * from + e % 4;
-              const float weight = __shfl(s[i][e], 32 * from + col);
-              if (!mine.holds(base + at)) continue;
+        for (int pos = base; pos < min(base + kWideKeys, hi); ++pos) {
+          const uint32_t row = row_of(p, t, pos);
+          if (row == kBadRow || !mine.holds(pos)) continue;
+          const T* from = row_pointer(v_cache, v_new, p.v_stride_t, row, p.D);
+          int first_channel = 4 * g;
+          asm volatile("" : "+v"(first_channel));  // the places are formed here, not kept in registers all along
 #pragma unroll
-              for (int c = 0; c < DT; ++c)
+          for (int c = 0; c < DT; ++c)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                  acc[c][r] = __builtin_fmaf(weight, ElemTraits<T>::load1(values + at * kValueStride + 32 * c + 8 * (r / 4) + 4 * g + r % 4), acc[c][r]);
+            for (int e = 0; e < 4; ++e) {
+              Pack<T, 4> k;
+              k.load(from + min(32 * c + 8 * e + first_channel, p.D - 4));
+              float v[4];
+              k.get(v);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) acc[c][4 * e + j] += __builtin_isfinite(v[j]) ? 0.f : v[j];
             }
+        }
       }
     }
   }
@@ -709,6 +732,7 @@ rnnt_status_t check(const rnnt_attention_shape_t& s) {
   for (const int64_t x : strides)
     if (!whole_stride(x, net_elem_bytes(s.dtype))) return RNNT_ERR_ALIGNMENT;
   if (s.D % 8 != 0 || s.D > 256 || (s.page & (s.page - 1)) != 0 || s.page > 1024) return RNNT_ERR_UNSUPPORTED;
+  if (s.k_stride_t > kMaxRows || s.v_stride_t > kMaxRows) return RNNT_ERR_UNSUPPORTED;
   if (s.num_pages > kMaxRows / s.page / s.Hkv || static_cast<int64_t>(s.L) * s.Hq > kMaxRows ||
       static_cast<int64_t>(s.table) * s.page + s.L >= (int64_t{1} << 30))
     return RNNT_ERR_UNSUPPORTED;
