@@ -403,12 +403,17 @@ __device__ __forceinline__ f32x16 mma32(const Eight<T>& a, const Eight<T>& b, f3
 
 template <typename T, int DT>
 __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionParams p) {
-  constexpr int kPieces = 4 * DT;                                   // 16-byte pieces of a row
-  constexpr int kPitch = DT == 1 ? 4 : DT == 2 ? 8 : DT <= 4 ? 16 : 32;  // ... of a row of keys in LDS
-  constexpr int kRowsOfBanks = kPitch >= 16 ? 1 : 16 / kPitch;      // rows that meet all banks once
-  constexpr int kMask = (kPitch < 16 ? kPitch : 16) - 1;
-  constexpr int kValueStride = 32 * DT + 16;                        // elements of a row of values in LDS
-  constexpr int kLoads = kWideKeys * kPieces / 256;
+  constexpr int kPitch = DT == 1 ? 4 : DT == 2 ? 8 : 16;           // 16-byte pieces of a row of keys in LDS
+  constexpr int kWhole = 32 * (DT - 1);                             // channels that every D of this DT has
+  constexpr int kValueStride = 32 * DT + 32;                        // elements of a row of values in LDS
+  // Four threads to a key, and every fourth piece of its row to each.  Piece c of a row of keys lies at c ^ swizzle(row): the
+  // sixteen rows that are read at one piece meet all banks, and so do the four rows of four pieces that are written at
+  // once.  Rows of values begin 64 bytes of banks apart, for the same.
+  const auto swizzle = [](int row) {
+    if constexpr (kPitch == 16) return (row & 3) << 2 | (row >> 2 & 3);
+    else if constexpr (kPitch == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    else return row >> 2 & 3;
+  };
   __shared__ __attribute__((aligned(16))) u32x4 keys[kWideKeys * kPitch];
   __shared__ __attribute__((aligned(16))) T values[kWideKeys * kValueStride];
   __shared__ uint32_t flags[2][3];  // of a step, in turn: keys whose page is none, and whether a value is no number
@@ -455,27 +460,25 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
       }
     }
 
-    Eight<T> kk[kLoads], vv[kLoads];
-    int id[kLoads];
-    uint32_t bad = 0;
-    const auto ask = [&](int step) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        id[i] = t.table.pages[min(lo + step * kWideKeys + (i * 256 + thread) / kPieces, hi - 1) >> p.shift];
-    };
+    const int key = thread >> 2, piece0 = thread & 3;
+    Eight<T> kk[DT], vv[DT];
+    int id = 0;
+    bool none = false;
+    const auto place = [&](int step) { return min(lo + step * kWideKeys + key, hi - 1); };
+    const auto ask = [&](int step) { id = t.table.pages[place(step) >> p.shift]; };
     const auto fetch = [&](int step) {
-      bad = 0;
+      const int pos = place(step);
+      none = static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.num_pages);
+      const uint32_t there = cache_row(id, p.Hkv, t.h, pos, p.shift), own = kNewRow | static_cast<uint32_t>(pos - t.cached);
+      const uint32_t row = none ? kBadRow : pos >= t.cached ? own : there;
+      const T* k = row_pointer(k_cache, k_new, p.k_stride_t, row, p.D);
+      const T* v = row_pointer(v_cache, v_new, p.v_stride_t, row, p.D);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int piece = (i * 256 + thread) % kPieces, pos = min(lo + step * kWideKeys + (i * 256 + thread) / kPieces, hi - 1);
-        const bool none = static_cast<uint32_t>(id[i]) >= static_cast<uint32_t>(p.num_pages);
-        const uint32_t there = cache_row(id[i], p.Hkv, t.h, pos, p.shift), own = kNewRow | static_cast<uint32_t>(pos - t.cached);
-        const uint32_t row = none ? kBadRow : pos >= t.cached ? own : there;
-        bad |= static_cast<uint32_t>(none) << i;
+      for (int i = 0; i < DT; ++i) {
         // behind D: the last piece again; a score's channels there are taken as 0, the output's are not stored
-        const int c = min(8 * piece, p.D - 8);
-        kk[i].load(row_pointer(k_cache, k_new, p.k_stride_t, row, p.D) + c);
-        vv[i].load(row_pointer(v_cache, v_new, p.v_stride_t, row, p.D) + c);
+        const int c = 32 * i + 32 <= kWhole ? 8 * (piece0 + 4 * i) : min(8 * (piece0 + 4 * i), p.D - 8);
+        kk[i].load(k + c);
+        vv[i].load(v + c);
       }
     };
     if (thread < 6) flags[thread / 3][thread % 3] = 0;
@@ -490,16 +493,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
       __syncthreads();
       if (thread < 3) flags[turn ^ 1][thread] = 0;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int row = (i * 256 + thread) / kPieces, piece = (i * 256 + thread) % kPieces;
-        keys[row * kPitch + (piece ^ (row / kRowsOfBanks & kMask))] = 8 * piece < p.D ? kk[i].w[0] : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < DT; ++i) {
+        const int piece = piece0 + 4 * i;
+        keys[key * kPitch + (piece ^ swizzle(key))] = 32 * i + 32 <= kWhole || 8 * piece < p.D ? kk[i].w[0] : u32x4{0, 0, 0, 0};
         if (block_mixed && vv[i].odd()) {
           flags[turn][2] = 1;
           vv[i].clear_odd();
         }
-        vv[i].store(values + row * kValueStride + 8 * piece);
-        if (bad >> i & 1) atomicOr(&flags[turn][row / 32], 1u << (row % 32));
+        vv[i].store(values + key * kValueStride + 8 * piece);
       }
+      if (none) atomicOr(&flags[turn][key / 32], 1u << (key % 32));
       __syncthreads();
       if (step + 1 < stop) {
         fetch(step + 1);
@@ -507,8 +510,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
       }
       if (base >= wave_last.hi || base + kWideKeys <= wave_first.lo) continue;  // nothing that the wave's rows see
       const auto flag = [&](int i) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(flags[turn][i]))); };
-      const uint32_t none[2] = {flag(0), flag(1)};
-      const bool mixed = base < wave_last.lo || base + kWideKeys > wave_first.hi || (none[0] | none[1]) != 0;
+      const uint32_t pageless[2] = {flag(0), flag(1)};
+      const bool mixed = base < wave_last.lo || base + kWideKeys > wave_first.hi || (pageless[0] | pageless[1]) != 0;
       const bool careful = flag(2) != 0;
       f32x16 s[2];
 #pragma unroll
@@ -519,7 +522,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
         for (int d = 0; d < 2 * DT; ++d) {
           const int row = 32 * i + col;
           Eight<T> a;
-          a.w[0] = keys[row * kPitch + ((2 * d + g) ^ (row / kRowsOfBanks & kMask))];
+          a.w[0] = keys[row * kPitch + ((2 * d + g) ^ swizzle(row))];
           s[i] = mma32(a, q[d], s[i]);
         }
       }
@@ -531,7 +534,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float v = none[i] >> (8 * (e / 4) + 4 * g + e % 4) & 1 ? __builtin_nanf("") : s[i][e];
+            const float v = pageless[i] >> (8 * (e / 4) + 4 * g + e % 4) & 1 ? __builtin_nanf("") : s[i][e];
             s[i][e] = sees(i, e) ? v : kNegInf;
           }
       }
@@ -541,8 +544,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
 #pragma unroll
         for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
       most = __builtin_fmaxf(most, __shfl_xor(most, 32));
+      // The maximum that the weights are taken against follows only where one of them would pass 2^8: its place does not
+      // matter to the quotient, and most steps spare the products with the sums so far.
       const float grown = __builtin_fmaxf(m, most);
-      if (__ballot(grown != m)) {
+      if (__ballot((grown - m) * scale > 8.f || (m == kNegInf && grown > m))) {
         const float shrink = m == kNegInf ? 0.f : fast_exp2((m - grown) * scale);
         sum *= shrink;
 #pragma unroll
