@@ -172,6 +172,11 @@ __device__ __forceinline__ float across_groups_max(float x) {
   x = __builtin_fmaxf(x, __shfl_xor(x, 16));
   return __builtin_fmaxf(x, __shfl_xor(x, 32));
 }
+// the larger of a lane's and the other half's
+__device__ __forceinline__ float halves_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 __device__ __forceinline__ float across_groups_sum(float x) {
   x += __shfl_xor(x, 16);
   return x + __shfl_xor(x, 32);
@@ -402,7 +407,7 @@ __device__ __forceinline__ f32x16 mma32(const Eight<T>& a, const Eight<T>& b, f3
 }
 
 template <typename T, int DT>
-__global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionParams p) {
+__global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wide(AttentionParams p) {
   constexpr int kPitch = DT == 1 ? 4 : DT == 2 ? 8 : 16;           // 16-byte pieces of a row of keys in LDS
   constexpr int kWhole = 32 * (DT - 1);                             // channels that every D of this DT has
   constexpr int kValueStride = 32 * DT + 32;                        // elements of a row of values in LDS
@@ -429,7 +434,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
   for (int c = 0; c < DT; ++c)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[c][e] = 0.f;
-  const float scale = __builtin_fabsf(p.scale);
+  const float scale = p.scale == 0.f ? 1.f : __builtin_fabsf(p.scale);  // 0: of products with 0
 
   if (t.state == 1) {
     const int all_rows = t.n * p.G, last_row = min(row0 + p.rows, all_rows) - 1;
@@ -455,7 +460,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
 #pragma unroll
       for (int d = 0; d < 2 * DT; ++d) {
         q[d].zero();
-        if (16 * d + 8 * g < p.D) q[d].load(from + 16 * d + 8 * g);
+        if (16 * d + 8 * g < p.D && p.scale != 0.f) q[d].load(from + 16 * d + 8 * g);
         q[d].w[0] ^= u32x4{sign, sign, sign, sign};
       }
     }
@@ -515,17 +520,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
       const bool careful = flag(2) != 0;
       f32x16 s[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int e = 0; e < 16; ++e) s[0][e] = s[1][e] = 0.f;
+      // A half's pieces are all asked for before the first product (left to itself the compiler waits for each in turn, which
+      // costs more than the products), the other half's as the first one's are used.
+      const auto key_piece = [&](int i, int d) {
+        const int row = 32 * i + col;
+        Eight<T> a;
+        a.w[0] = keys[row * kPitch + ((2 * d + g) ^ swizzle(row))];
+        return a;
+      };
+      Eight<T> pieces[2 * DT];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+      for (int d = 0; d < 2 * DT; ++d) pieces[d] = key_piece(0, d);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int d = 0; d < 2 * DT; ++d) {
-          const int row = 32 * i + col;
-          Eight<T> a;
-          a.w[0] = keys[row * kPitch + ((2 * d + g) ^ swizzle(row))];
-          s[i] = mma32(a, q[d], s[i]);
-        }
+      for (int d = 0; d < 2 * DT; ++d) {
+        s[0] = mma32(pieces[d], q[d], s[0]);
+        pieces[d] = key_piece(1, d);
       }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < 2 * DT; ++d) s[1] = mma32(pieces[d], q[d], s[1]);
       // whether the lane's row sees key `at` of the step
       const uint32_t from = static_cast<uint32_t>(base + 4 * g - mine.lo), span = static_cast<uint32_t>(mine.hi - mine.lo);
       const auto sees = [&](int i, int e) { return from + (32 * i + 8 * (e / 4) + e % 4) < span; };
@@ -543,7 +558,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
-      most = __builtin_fmaxf(most, __shfl_xor(most, 32));
+      most = halves_max(most);
       // The maximum that the weights are taken against follows only where one of them would pass 2^8: its place does not
       // matter to the quotient, and most steps spare the products with the sums so far.
       const float grown = __builtin_fmaxf(m, most);
@@ -555,29 +570,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
         m = grown;
       }
       const float by = m == kNegInf ? 0.f : m * scale;
-      Eight<T> weights[4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[i][e] = fast_exp2(__builtin_fmaf(s[i][e], scale, -by));
-      if (mixed) {  // 0 also where a scale of 0 made NaN of what is not seen
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[i][e] = sees(i, e) ? s[i][e] : 0.f;
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sum += s[i][e];
-      // weights of 16 bits, as the values are
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        float w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = s[b / 2][8 * (b % 2) + j];
-        weights[b].set(w);
-      }
       // the values of channel 32 c + lane % 32 and the sixteen keys b of the step, of which the lane holds eight
       const auto column = [&](int c, int b) {
         Eight<T> a;
@@ -592,10 +584,43 @@ __global__ __launch_bounds__(64 * kWaves, 2) void enc_attention_wide(AttentionPa
         }
         return a;
       };
+      // Weights of 16 bits, as the values are.  The first half's products with the values run while the second half's weights
+      // are formed: one matrix instruction, then a few of the others.
+      Eight<T> weights[4];
+      float half_sum[2] = {0.f, 0.f};
+      const auto weigh = [&](int i) {
 #pragma unroll
-      for (int c = 0; c < DT; ++c)
+        for (int e = 0; e < 16; ++e) {
+          s[i][e] = fast_exp2(__builtin_fmaf(s[i][e], scale, -by));
+          half_sum[i] += s[i][e];
+        }
 #pragma unroll
-        for (int b = 0; b < 4; ++b) acc[c] = mma32(column(c, b), weights[b], acc[c]);
+        for (int b = 0; b < 2; ++b) {
+          float w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = s[i][8 * b + j];
+          weights[2 * i + b].set(w);
+        }
+      };
+      weigh(0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < DT; ++c) acc[c] = mma32(column(c, b), weights[b], acc[c]);
+      weigh(1);
+#pragma unroll
+      for (int i = 0; i < 2 * DT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 72 / (2 * DT), 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 2; b < 4; ++b)
+#pragma unroll
+        for (int c = 0; c < DT; ++c) acc[c] = mma32(column(c, b), weights[b], acc[c]);
+      sum += half_sum[0] + half_sum[1];
       if (careful) {
         // An infinity or NaN among the values, which a weight of 0 would have let through, went into LDS as 0: it reaches the
         // rows that see its key from here.
