@@ -61,7 +61,7 @@ def quantize_rows(x):
 
 def linear8(q, q_scale, w, w_scale, bias=None):
     """(y, the size of what is added up last)."""
-    total = q.astype(np.int64) @ w.astype(np.int64).T
+    total = q.astype(np.float64) @ w.astype(np.float64).T  # whole numbers below 2^53: exact
     y = total * q_scale[:, None] * w_scale[None]
     size = np.abs(y)
     if bias is not None:

@@ -27,15 +27,16 @@ struct MaxBitsOp {
 // with 127 / most, rounded, would put halves on either side.)
 struct Quantizer {
   float factor, most, inverse;
+  uint32_t keep;  // no bits for a row of zeros, or one that holds no number
 
-  // most: the row's largest magnitude, by its bits
+  // m: the row's largest magnitude, by its bits
   __device__ __forceinline__ explicit Quantizer(float m) {
     // 127 v stays in float32's range; powers of two change no digit
     const bool large = m > 0x1p100f;
     factor = large ? 127.f * 0x1p-64f : 127.f;
     most = large ? m * 0x1p-64f : m;
     inverse = __builtin_amdgcn_rcpf(most);
-    if (!(m >= 0x1p-100f && m < __builtin_inff())) factor = inverse = 0.f;  // zeros, or no number: q = 0
+    keep = m >= 0x1p-100f && m < __builtin_inff() ? 0xffffffffu : 0u;
   }
   // the scale of a row whose values are v * unit
   __device__ __forceinline__ static float scale(float m, float unit) {
@@ -43,16 +44,28 @@ struct Quantizer {
     const float s = m * unit * (1.f / 127.f);
     return s < __builtin_inff() && m < __builtin_inff() ? s : __builtin_nanf("");
   }
-  __device__ __forceinline__ int quantize(float v) const {
-    const float p = inverse == 0.f ? 0.f : v * factor, t = p * inverse;
+  // the integer of v, in the low byte
+  __device__ __forceinline__ uint32_t one(float v) const {
+    const float p = v * factor, t = p * inverse;
     const float q = __builtin_fmaf(__builtin_fmaf(-t, most, p), inverse, t);
-    return static_cast<int>(__builtin_rintf(inverse == 0.f ? 0.f : q));
+    return __float_as_uint(q + 12582912.f);  // 1.5 * 2^23: the sum's last digit is 1
+  }
+  // four as bytes, the first one lowest
+  __device__ __forceinline__ uint32_t four(const float* v) const {
+    const uint32_t low = __builtin_amdgcn_perm(one(v[1]), one(v[0]), 0x0c0c0400u);
+    const uint32_t high = __builtin_amdgcn_perm(one(v[3]), one(v[2]), 0x0c0c0400u);
+    return __builtin_amdgcn_perm(high, low, 0x05040100u) & keep;
   }
 };
 
-// four integers of -127 .. 127 as bytes, the first one lowest
-__device__ __forceinline__ uint32_t pack4_i8(int a, int b, int c, int d) {
-  return (a & 0xff) | (b & 0xff) << 8 | (c & 0xff) << 16 | static_cast<uint32_t>(d) << 24;
+// The largest magnitude of 16-bit elements, two at a time on their bits.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void raise_most16(uint32_t& most, uint32_t two) {
+  most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, most), __builtin_bit_cast(u16x2, two & 0x7fff7fffu)));
+}
+template <typename T>
+__device__ __forceinline__ float most16(uint32_t most) {
+  return ElemTraits<T>::from_bits((most & 0xffffu) > most >> 16 ? most & 0xffffu : most >> 16);
 }
 
 }  // namespace rnnt

@@ -116,6 +116,58 @@ __global__ __launch_bounds__(256) void enc_linear8(Linear8Params p) {
   }
 }
 
+// ---- rows to 8 bits on the way in --------------------------------------------------
+// A wave reads a few rows at once, 32 lanes to a row and four elements to a lane, and takes each to 8 bits: 128 NK
+// bytes a row, 0 from K on, and its scale.  Rows behind the last are the last again.  WHOLE: K is a multiple of four, and no load
+// has a branch.
+template <typename T, int NK>
+constexpr int kRowsAtOnce = sizeof(T) == 4 ? (NK <= 4 ? 4 : 2) : NK <= 6 ? 8 : 4;
+
+template <typename T, int NK, bool WHOLE>
+__device__ __forceinline__ void quantize_rows_of_wave(const T* x, int64_t m0, int64_t M, int K, int8_t* to, int pitch, float* scales) {
+  constexpr int kPairs = kRowsAtOnce<T, NK> / 2;
+  const int lane = static_cast<int>(threadIdx.x) & 31, half = (static_cast<int>(threadIdx.x) >> 5) & 1;
+  Pack<T, 4> k[kPairs][NK];
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    const T* row = x + min(m0 + 2 * i + half, M - 1) * K;
+#pragma unroll
+    for (int v = 0; v < NK; ++v) {
+      const int at = (v * 32 + lane) * 4;
+      if constexpr (WHOLE) {
+        k[i][v].load(row + min(at, K - 4));
+      } else {
+        k[i][v].zero();
+        if (at < K) k[i][v].load_part(row + at, min(K - at, 4));
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    float most = 0.f;
+    uint32_t most_bits = 0;
+#pragma unroll
+    for (int v = 0; v < NK; ++v) {
+      if (WHOLE && (v * 32 + lane) * 4 >= K) k[i][v].zero();
+#pragma unroll
+      for (int j = 0; j < Pack<T, 4>::kWords; ++j) {
+        if constexpr (sizeof(T) == 2) raise_most16(most_bits, k[i][v].w[j]);
+        else most = MaxBitsOp::apply(most, __uint_as_float(k[i][v].w[j] & 0x7fffffffu));
+      }
+    }
+    if constexpr (sizeof(T) == 2) most = most16<T>(most_bits);
+    most = group_reduce<32, MaxBitsOp>(most, 0.f);
+    const Quantizer quantizer(most);
+    if (lane == 0) scales[2 * i + half] = Quantizer::scale(most, 1.f);
+#pragma unroll
+    for (int v = 0; v < NK; ++v) {
+      float f[4];
+      k[i][v].get(f);
+      *reinterpret_cast<uint32_t*>(to + (2 * i + half) * pitch + (v * 32 + lane) * 4) = quantizer.four(f);
+    }
+  }
+}
+
 // ---- rows held in registers ----------------------------------------------------
 // For rows of up to 1024 a block of four waves keeps 128 rows of x, 32 to a wave, in registers in the matrix
 // instruction's order, and passes over its share of w, 64 rows at a time through LDS.  x is read once, whatever N is,
@@ -142,64 +194,15 @@ struct HeldRows {
   i32x4 piece[4 * NK];
   float scale;
 
-  // rows of `T`: a wave reads whole rows, a few at a time, and takes each to 8 bits
-  // (WHOLE: a row is a whole number of accesses, and none of them has a branch)
+  // rows of `T`, sixteen at a time through LDS
   template <bool WHOLE>
   __device__ __forceinline__ void quantize(const T* x, int64_t m0, int64_t M, int K, int8_t* lds, float* scales) {
-    constexpr int VEC = kVec<T>, NV = (128 * NK + 64 * VEC - 1) / (64 * VEC), kAtOnce = NV <= 2 ? 8 : 4;
     const int lane = static_cast<int>(threadIdx.x) & 63;
 #pragma unroll
     for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
-      for (int r = 0; r < 16; r += kAtOnce) {
-        Pack<T, VEC> k[kAtOnce][NV];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          const int64_t m = min(m0 + 16 * pass + r + i, M - 1);
-#pragma unroll
-          for (int v = 0; v < NV; ++v) {
-            const int at = (v * 64 + lane) * VEC;
-            if constexpr (WHOLE) {
-              k[i][v].load(x + m * K + min(at, K - VEC));
-              continue;
-            }
-            k[i][v].zero();
-            if (at < K) {
-              if (at + VEC <= K) k[i][v].load(x + m * K + at);
-              else k[i][v].load_part(x + m * K + at, K - at);
-            }
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          float most = 0.f;
-#pragma unroll
-          for (int v = 0; v < NV; ++v) {
-            float f[VEC];
-            if (WHOLE && (v * 64 + lane) * VEC >= K) k[i][v].zero();
-            k[i][v].get(f);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) most = MaxBitsOp::apply(most, __builtin_fabsf(f[j]));
-          }
-          most = group_reduce<64, MaxBitsOp>(most, 0.f);
-          const Quantizer quantizer(most);
-          if (lane == 0) scales[16 * pass + r + i] = Quantizer::scale(most, 1.f);
-#pragma unroll
-          for (int v = 0; v < NV; ++v) {
-            const int at = (v * 64 + lane) * VEC;
-            if (at >= 128 * NK) continue;
-            float f[VEC];
-            k[i][v].get(f);
-            int q[VEC];
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) q[j] = quantizer.quantize(f[j]);
-            Words<VEC, VEC> w;
-#pragma unroll
-            for (int j = 0; j < VEC / 4; ++j) w.w[j] = pack4_i8(q[4 * j], q[4 * j + 1], q[4 * j + 2], q[4 * j + 3]);
-            *reinterpret_cast<Words<VEC, VEC>*>(lds + (r + i) * kPitch + at) = w;
-          }
-        }
-      }
+      for (int r = 0; r < 16; r += kRowsAtOnce<T, NK>)
+        quantize_rows_of_wave<T, NK, WHOLE>(x, m0 + 16 * pass + r, M, K, lds + r * kPitch, kPitch, scales + 16 * pass + r);
       if (((lane >> 4) & 1) == pass) {
 #pragma unroll
         for (int k = 0; k < 4 * NK; ++k)
@@ -246,7 +249,8 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
   // for nothing; without a bias, a value of w in its place is not used either
   const int last_piece = 16 * min(8 * (NK - 1) + piece, pieces - 1);
   const T* bias_or_any = l.bias ? static_cast<const T*>(l.bias) : reinterpret_cast<const T*>(l.w);
-  u32x4 hold[NK][2];
+  constexpr int kTiles = kHeldTile / 32;
+  u32x4 hold[NK][kTiles];
   float hold_scale;
   T hold_bias;
   const auto fetch = [&](int turn) {
@@ -254,7 +258,7 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
     hold_scale = l.w_scale[n];
     hold_bias = bias_or_any[n];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kTiles; ++i) {
       const int8_t* from = l.w + static_cast<int64_t>(min(turn * kHeldTile + row + 32 * i, l.N - 1)) * l.w_pitch;
 #pragma unroll
       for (int s = 0; s < NK; ++s)
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
 #pragma unroll
     for (int s = 0; s < NK; ++s)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < kTiles; ++i)
         *reinterpret_cast<u32x4*>(lds + s * (kHeldTile * 128) + (row + 32 * i) * 128 + ((piece ^ key) << 4)) = hold[s][i];
     if (thread < kHeldTile) {
       columns[0][thread] = hold_scale;
@@ -334,18 +338,20 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
     const int n0 = turn * kHeldTile;
     stage();
     fetch(min(turn + 1, p.turns - 1));
-    i32x16 acc[2];
+    i32x16 acc[kTiles];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[0][e] = acc[1][e] = 0;
+    for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[tile][e] = 0;
 #pragma unroll
     for (int k = 0; k < 4 * NK; ++k)
 #pragma unroll
-      for (int tile = 0; tile < 2; ++tile) {
+      for (int tile = 0; tile < kTiles; ++tile) {
         const i32x4 w = *reinterpret_cast<const i32x4*>(lds + (k / 4) * (kHeldTile * 128) + tile * 4096 + at[k % 4]);
         acc[tile] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x.piece[k], acc[tile], 0, 0, 0);
       }
-    finish(acc[0], 0);
-    finish(acc[1], 1);
+#pragma unroll
+    for (int tile = 0; tile < kTiles; ++tile) finish(acc[tile], tile);
 #pragma unroll
     for (int i = 0; i < kHeldRows / kRowsOnce; ++i) {
       T* to;
@@ -358,7 +364,7 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
     const int n0 = whole * kHeldTile;
     stage();
 #pragma unroll 1
-    for (int tile = 0; tile < 2 && n0 + 32 * tile < l.N; ++tile) {
+    for (int tile = 0; tile < kTiles && n0 + 32 * tile < l.N; ++tile) {
       i32x16 acc;
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[e] = 0;
@@ -373,6 +379,152 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
       result(i, to, k);
       if (left >= VEC) k.store(to + n0);
       else if (left > 0) k.store_part(to + n0, left);
+    }
+  }
+}
+
+// ---- few rows ------------------------------------------------------------------
+// A block takes 16 or 32 rows of x into LDS, in 8 bits, and multiplies them with a few tiles of 16 rows of w, which go from
+// memory to registers and nowhere else.  Where tiles are fewer than CUs the four waves share out k, and their sums meet in
+// LDS; else they share out the tiles.  The first pieces of w are asked for before x is there.
+struct FewParams {
+  Linear8Params l;
+  int32_t pitch;        // of a row of x in LDS: whole steps of 64 bytes, and 16, so that sixteen rows meet all banks
+  int32_t tiles, blocks, tiles_of_wave;  // of w; blocks to the same rows of x; 0: the waves share out k
+};
+constexpr int kFewAhead = 4;
+constexpr int kFewLds = 64000;
+
+template <typename T, int MT, int NV, bool DYNAMIC>
+__global__ __launch_bounds__(256) void enc_linear8_few(FewParams p) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ float scales[16 * MT];
+  __shared__ __attribute__((aligned(16))) i32x4 sums[4][MT * 64];
+  const Linear8Params& l = p.l;
+  const int thread = static_cast<int>(threadIdx.x), lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  const int64_t m0 = static_cast<int64_t>(blockIdx.x / p.blocks) * (16 * MT);
+  const int block = static_cast<int>(blockIdx.x % p.blocks);
+  const bool shared_k = p.tiles_of_wave == 0;
+  const int steps = (l.K + 63) / 64, pieces = (l.K + 15) / 16;
+  const int first = shared_k ? block : (block * 4 + wave) * p.tiles_of_wave;
+  const int last = shared_k ? block + 1 : min(first + p.tiles_of_wave, p.tiles);
+  const int step0 = shared_k ? wave : 0, by = shared_k ? 4 : 1;
+  // x is 0 behind K: a piece in the place of one behind it counts for nothing
+  const auto w_piece = [&](int tile, int step) {
+    const int n = min(tile * 16 + (lane & 15), l.N - 1), piece = min(4 * step + (lane >> 4), pieces - 1);
+    return *reinterpret_cast<const i32x4*>(l.w + n * l.w_pitch + 16 * piece);
+  };
+  i32x4 w[kFewAhead];
+  const auto ahead = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < kFewAhead; ++i) w[i] = w_piece(min(tile, p.tiles - 1), min(step0 + i * by, steps - 1));
+  };
+  ahead(first);
+
+  // x: a wave takes every fourth row, a few at once
+  if constexpr (DYNAMIC) {
+    constexpr int kAtOnce = NV <= 4 ? 4 : sizeof(T) == 2 ? 32 / NV : 16 / NV;
+#pragma unroll 1
+    for (int r0 = 0; r0 < 4 * MT; r0 += kAtOnce) {
+      Pack<T, 4> k[kAtOnce][NV];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const T* row = reinterpret_cast<const T*>(l.x) + min(m0 + 4 * (r0 + i) + wave, static_cast<int64_t>(l.M) - 1) * l.K;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int at = (v * 64 + lane) * 4;
+          k[i][v].zero();
+          if (at + 4 <= l.K) k[i][v].load(row + at);
+          else if (at < l.K) k[i][v].load_part(row + at, l.K - at);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int row = 4 * (r0 + i) + wave;
+        float most = 0.f;
+        uint32_t most_bits = 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int j = 0; j < Pack<T, 4>::kWords; ++j) {
+            if constexpr (sizeof(T) == 2) raise_most16(most_bits, k[i][v].w[j]);
+            else most = MaxBitsOp::apply(most, __uint_as_float(k[i][v].w[j] & 0x7fffffffu));
+          }
+        if constexpr (sizeof(T) == 2) most = most16<T>(most_bits);
+        most = group_reduce<64, MaxBitsOp>(most, 0.f);
+        const Quantizer quantizer(most);
+        if (lane == 0) scales[row] = Quantizer::scale(most, 1.f);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int at = (v * 64 + lane) * 4;
+          float f[4];
+          k[i][v].get(f);
+          if (at < 64 * steps) *reinterpret_cast<uint32_t*>(lds + row * p.pitch + at) = quantizer.four(f);
+        }
+      }
+    }
+  } else {
+    for (int i = thread; i < 16 * MT * 4 * steps; i += 256) {
+      const int row = i / (4 * steps), piece = i - row * 4 * steps;
+      const int64_t m = min(m0 + row, static_cast<int64_t>(l.M) - 1);
+      *reinterpret_cast<u32x4*>(lds + row * p.pitch + 16 * piece) = load_bytes(l.x + m * l.x_pitch, 16 * piece, l.K);
+    }
+    if (thread < 16 * MT) scales[thread] = l.x_scale[min(m0 + thread, static_cast<int64_t>(l.M) - 1)];
+  }
+  __syncthreads();
+
+  // rows of w by rows: a lane's results are row lane % 16 of x and columns 4 (lane / 16) + e
+  const auto finish = [&](const i32x4& acc, int tile, int mt, int of) {
+    const int64_t m = m0 + 16 * mt + (of & 15);
+    const int n = tile * 16 + 4 * (of >> 4), left = l.N - n;
+    if (m >= l.M || left <= 0) return;
+    const float scale = scales[16 * mt + (of & 15)];
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = min(n + e, l.N - 1);
+      const float bias = l.bias ? ElemTraits<T>::load1(static_cast<const T*>(l.bias) + at) : 0.f;
+      v[e] = static_cast<float>(acc[e]) * scale * l.w_scale[at] + bias;
+    }
+    Pack<T, 4> k;
+    k.set(v);
+    T* to = static_cast<T*>(l.y) + m * l.N + n;
+    if (left >= 4) k.store(to);
+    else k.store_part(to, left);
+  };
+  const char* x = lds + (lane & 15) * p.pitch + 16 * (lane >> 4);
+#pragma unroll 1
+  for (int tile = first; tile < last; ++tile) {
+    i32x4 acc[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) acc[mt] = i32x4{0, 0, 0, 0};
+#pragma unroll 1
+    for (int s0 = step0; s0 < steps; s0 += by * kFewAhead) {
+#pragma unroll
+      for (int i = 0; i < kFewAhead; ++i) {
+        const int step = s0 + i * by;
+        const i32x4 now = w[i];
+        const bool more = step + by * kFewAhead < steps;
+        w[i] = w_piece(more ? tile : min(tile + 1, p.tiles - 1), more ? step + by * kFewAhead : min(step0 + i * by, steps - 1));
+        if (step >= steps) continue;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          acc[mt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now, *reinterpret_cast<const i32x4*>(x + 16 * mt * p.pitch + 64 * step), acc[mt], 0, 0, 0);
+      }
+    }
+    if (!shared_k) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) finish(acc[mt], tile, mt, lane);
+    } else {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) sums[wave][64 * mt + lane] = acc[mt];
+    }
+  }
+  if (shared_k) {
+    __syncthreads();
+    if (thread < 64 * MT) {
+      const i32x4 total = sums[0][thread] + sums[1][thread] + sums[2][thread] + sums[3][thread];
+      finish(total, block, thread >> 6, thread & 63);
     }
   }
 }
@@ -406,6 +558,48 @@ rnnt_status_t check_memory(const rnnt_linear8_shape_t& s, const int8_t* w, const
 }
 
 bool held(const rnnt_linear8_shape_t& s) { return s.K <= kHeldMost; }
+
+// The tiles of sixteen rows of x that a block of the form for few rows takes, 0: another form.  Tiles of sixteen by sixteen
+// results up to which it is the faster one (us, this form and the next; K x N): 640 x 1025, M = 16 6.3 and 13.0, M = 256
+// 11.7 and 13.1, M = 512 27 and 13.4; 512 x 2048, M = 256 8.7 and 11.2, M = 512 15.1 and 11.5; 1024 x 256, M = 2048 10.5 and
+// 18.9; rows of two launches, 2048 x 512, M = 1024 18.9 and 29.5, M = 2048 26 and 30, M = 4096 41 and 32.
+int few(const rnnt_linear8_shape_t& s) {
+  const int64_t pitch = (static_cast<int64_t>(s.K) + 63) / 64 * 64 + 16, tiles = (static_cast<int64_t>(s.N) + 15) / 16;
+  const int64_t all = (static_cast<int64_t>(s.M) + 15) / 16 * tiles;
+  if (s.K > 256 * 16 || pitch * 16 > kFewLds || all > (held(s) ? 2048 : 4096)) return 0;
+  // sixteen rows to a block, which come in one round, while that makes no more than four blocks to a CU
+  return all <= 1024 || pitch * 32 > kFewLds ? 1 : 2;
+}
+
+template <bool DYNAMIC>
+rnnt_status_t launch_few(const Linear8Params& q, const rnnt_linear8_shape_t& s, int mt, hipStream_t stream) {
+  FewParams p{};
+  p.l = q;
+  p.pitch = (s.K + 63) / 64 * 64 + 16;
+  p.tiles = (s.N + 15) / 16;
+  const int64_t m_blocks = (s.M + 16 * mt - 1) / (16 * mt);
+  // two blocks to a CU while that is not one tile to a block
+  const int64_t want = m_blocks * p.tiles / 512;
+  p.tiles_of_wave = want <= 1 ? 0 : static_cast<int32_t>((want + 3) / 4);
+  p.blocks = p.tiles_of_wave == 0 ? p.tiles : (p.tiles + 4 * p.tiles_of_wave - 1) / (4 * p.tiles_of_wave);
+  const dim3 grid(static_cast<uint32_t>(m_blocks * p.blocks));
+  const size_t lds = static_cast<size_t>(p.pitch) * 16 * mt;
+  return with_dtype(s.dtype, [&](auto t) {
+    using T = decltype(t);
+#define RNNT_FEW(n, nv)                                                                                       \
+  if (mt == n && s.K <= 256 * nv) {                                                                           \
+    hipLaunchKernelGGL((enc_linear8_few<T, n, nv, DYNAMIC>), grid, dim3(256), lds, stream, p);                \
+    return launched();                                                                                        \
+  }
+    RNNT_FEW(1, 4)
+    RNNT_FEW(2, 4)
+    RNNT_FEW(1, 8)
+    RNNT_FEW(2, 8)
+    RNNT_FEW(1, 16)
+#undef RNNT_FEW
+    return RNNT_ERR_UNSUPPORTED;
+  });
+}
 
 // blocks of the held form: several to the same rows while there are few rows
 HeldParams held_params(const Linear8Params& q, int64_t* blocks) {
@@ -446,6 +640,7 @@ rnnt_status_t launch_held(const Linear8Params& q, const rnnt_linear8_shape_t& s,
 
 rnnt_status_t launch(const Linear8Params& q, const rnnt_linear8_shape_t& s, hipStream_t stream) {
   if (s.M == 0) return RNNT_OK;
+  if (const int mt = few(s)) return launch_few<false>(q, s, mt, stream);
   if (held(s)) return launch_held<false>(q, s, stream);
   return with_dtype(s.dtype, [&](auto t) {
     hipLaunchKernelGGL((enc_linear8<decltype(t)>), dim3(static_cast<uint32_t>(tiles_of(s))), dim3(256), 0, stream, q);
@@ -492,7 +687,7 @@ rnnt_status_t rnnt_linear8(const int8_t* x, const float* x_scale, const int8_t* 
 }
 
 size_t rnnt_linear8_dynamic_workspace_bytes(rnnt_linear8_shape_t shape) {
-  if (check(shape, true) != RNNT_OK || held(shape)) return 0;
+  if (check(shape, true) != RNNT_OK || held(shape) || few(shape)) return 0;
   return net_align256(static_cast<size_t>(shape.M) * own_pitch(shape)) + net_align256(static_cast<size_t>(shape.M) * 4);
 }
 
@@ -509,9 +704,10 @@ rnnt_status_t rnnt_linear8_dynamic(const void* x, const int8_t* w, const float* 
   st = ws.take(workspace, workspace_bytes, rnnt_linear8_dynamic_workspace_bytes(shape), stream);
   if (st != RNNT_OK) return st;
   Linear8Params q = params_of(shape, w, w_scale, bias, y);
-  if (held(shape)) {
+  if (held(shape) || few(shape)) {
     if (shape.M == 0) return RNNT_OK;
     q.x = static_cast<const int8_t*>(x);
+    if (const int mt = few(shape)) return launch_few<true>(q, shape, mt, stream);
     return launch_held<true>(q, shape, stream);
   }
   q.x_pitch = own_pitch(shape);

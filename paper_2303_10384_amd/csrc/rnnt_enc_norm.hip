@@ -51,15 +51,12 @@ __device__ __forceinline__ void store_row(const Pack<T, kVec<T>>& k, T* p, int D
 }
 
 template <int VEC>
-__device__ __forceinline__ void store_q(int8_t* p, const int* q, int D) {
+__device__ __forceinline__ void store_q(int8_t* p, const Words<VEC, 1>& w, int D) {
   if (D < VEC) {
     for (int j = 0; j < VEC; ++j)
-      if (j < D) p[j] = static_cast<int8_t>(q[j]);
+      if (j < D) p[j] = static_cast<int8_t>(w.w[j / 4] >> (8 * (j % 4)));
     return;
   }
-  Words<VEC, 1> w;
-#pragma unroll
-  for (int j = 0; j < VEC / 4; ++j) w.w[j] = pack4_i8(q[4 * j], q[4 * j + 1], q[4 * j + 2], q[4 * j + 3]);
   *reinterpret_cast<Words<VEC, 1>*>(p) = w;
 }
 
@@ -154,9 +151,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void enc_rows(RowsParams p) {
       if (state == 0) k.zero();
       store_row(k, static_cast<T*>(p.y) + base + at.at, p.D);
     } else {
-      int q[VEC];
+      Words<VEC, 1> q;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) q[j] = quantizer.quantize(t[v][j]);
+      for (int j = 0; j < VEC / 4; ++j) q.w[j] = quantizer.four(t[v] + 4 * j);
       store_q<VEC>(p.q + row * p.pitch + at.at, q, p.D);
     }
     if (MODE != kQuantize && p.residual && state != 1) {

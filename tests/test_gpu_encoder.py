@@ -215,7 +215,10 @@ def test_quantized_halves_and_extremes(torch, pkg, dtype):  # noqa: F811
 LINEAR = [  # M, K, N
     (1, 1, 1), (1, 16, 33), (3, 5, 7), (16, 640, 1025), (2, 100, 64), (17, 127, 130), (64, 128, 128), (65, 129, 257),
     (130, 48, 31), (200, 640, 96), (300, 321, 200), (129, 1000, 129), (40, 2048, 17), (257, 64, 1025), (33, 4096, 40),
-    (0, 8, 4), (15, 2047, 1), (1100, 256, 160), (128, 16, 300), (513, 1040, 272)]
+    (0, 8, 4), (15, 2047, 1), (1100, 256, 160), (128, 16, 300), (513, 1040, 272),
+    # past the form for few rows: rows held in registers, and rows too long for that
+    (700, 127, 1000), (2100, 640, 300), (1500, 1024, 501), (4100, 5, 257), (33000, 130, 15), (2049, 768, 289), (1100, 1040, 1000),
+    (2048, 1030, 523), (40, 3969, 70), (30, 5000, 33)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
