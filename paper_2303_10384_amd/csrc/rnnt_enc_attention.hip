@@ -183,23 +183,44 @@ __device__ __forceinline__ float across_groups_sum(float x) {
 }
 
 // ---- the chunk's own keys and values, into the cache ---------------------------------
-// The tokens whose first row lies in the tile, by the tile's first split.  Nothing in this launch reads them there.
-template <typename T>
-__device__ __forceinline__ void write_cache(const AttentionParams& p, const Tile& t, int rows) {
-  const int first = (t.tile * rows + p.G - 1) / p.G, last = min(((t.tile + 1) * rows + p.G - 1) / p.G, t.n);
-  const int pieces = p.D / 8, total = (last - first) * pieces;
-  for (int i = static_cast<int>(threadIdx.x); i < total; i += static_cast<int>(blockDim.x)) {
-    const int token = first + i / pieces, c = 8 * (i % pieces), pos = t.cached + token;
-    const int id = t.table.page_of(pos);
-    if (id < 0) continue;
-    const int64_t to = static_cast<int64_t>(cache_row(id, p.Hkv, t.h, pos, p.shift)) * p.D + c;
-    Eight<T> e;
-    e.load(static_cast<const T*>(p.k) + t.b * p.k_stride_b + token * p.k_stride_t + t.h * p.k_stride_h + c);
-    e.store(static_cast<T*>(p.k_cache) + to);
-    e.load(static_cast<const T*>(p.v) + t.b * p.v_stride_b + token * p.v_stride_t + t.h * p.v_stride_h + c);
-    e.store(static_cast<T*>(p.v_cache) + to);
+// The tokens whose first row lies in the tile, by the tile's first split.  Nothing in this launch reads them there.  They are
+// asked for and stored apart: sixteen rows' come before the attention's own rows and go after its last, and neither waits for the other.
+template <typename T, int N>
+struct CacheWrite {
+  Eight<T> k[N], v[N];
+  int id[N];
+
+  __device__ __forceinline__ static int tokens(const AttentionParams& p, const Tile& t, int& first) {
+    first = (t.tile * p.rows + p.G - 1) / p.G;
+    return min(((t.tile + 1) * p.rows + p.G - 1) / p.G, t.n) - first;
   }
-}
+  __device__ __forceinline__ void ask(const AttentionParams& p, const Tile& t, int round) {
+    int first;
+    const int pieces = p.D / 8, total = tokens(p, t, first) * pieces;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = (round * N + n) * 64 * kWaves + static_cast<int>(threadIdx.x);
+      if (i >= total) continue;
+      const int token = first + i / pieces, c = 8 * (i % pieces);
+      id[n] = t.table.pages[(t.cached + token) >> p.shift];
+      k[n].load(static_cast<const T*>(p.k) + t.b * p.k_stride_b + token * p.k_stride_t + t.h * p.k_stride_h + c);
+      v[n].load(static_cast<const T*>(p.v) + t.b * p.v_stride_b + token * p.v_stride_t + t.h * p.v_stride_h + c);
+    }
+  }
+  __device__ __forceinline__ void store(const AttentionParams& p, const Tile& t, int round) const {
+    int first;
+    const int pieces = p.D / 8, total = tokens(p, t, first) * pieces;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = (round * N + n) * 64 * kWaves + static_cast<int>(threadIdx.x);
+      if (i >= total || static_cast<uint32_t>(id[n]) >= static_cast<uint32_t>(p.num_pages)) continue;
+      const int token = first + i / pieces, c = 8 * (i % pieces);
+      const int64_t to = static_cast<int64_t>(cache_row(id[n], p.Hkv, t.h, t.cached + token, p.shift)) * p.D + c;
+      k[n].store(static_cast<T*>(p.k_cache) + to);
+      v[n].store(static_cast<T*>(p.v_cache) + to);
+    }
+  }
+};
 
 // ---- attention ------------------------------------------------------------------------
 // A block of four waves takes sixteen rows and, of their keys, every wave every fourth step of 32.  Scores are formed
@@ -209,6 +230,7 @@ __device__ __forceinline__ void write_cache(const AttentionParams& p, const Tile
 template <typename T, int DT>
 __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) {
   using V = Values<T, DT>;
+  constexpr int kWrites = DT <= 4 ? 1 : 2;  // sixteen tokens of up to 4 DT pieces
   constexpr int kPieces = 4 * DT, kLoads = kKeys * kPieces / 64;  // 16-byte pieces of a row (float32: pairs of them)
   constexpr int kValueBytes = kWaves * V::kElems * static_cast<int>(sizeof(T));
   constexpr int kJoinBytes = kWaves * 32 * DT * 17 * 4;
@@ -217,7 +239,9 @@ __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) 
   const int lane = static_cast<int>(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int g = lane >> 4, col = lane & 15;
   const Tile t(p, blockIdx.x / p.splits, static_cast<int>(blockIdx.x % p.splits));
-  if (t.split == 0 && t.state == 1) write_cache<T>(p, t, kRowTile);
+  CacheWrite<T, kWrites> write;
+  const bool writes = t.split == 0 && t.state == 1;
+  if (writes) write.ask(p, t, 0);
 
   const int rows = p.L * p.G, row0 = t.tile * kRowTile;
   float m = kNegInf, sum = 0.f;
@@ -348,6 +372,7 @@ __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) 
     }
   }
 
+  if (writes) write.store(p, t, 0);
   // The waves' parts, joined at the largest of their maxima.
   sum = across_groups_sum(sum);
   __syncthreads();
@@ -425,7 +450,6 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
   const int thread = static_cast<int>(threadIdx.x), lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int g = lane >> 5, col = lane & 31;
   const Tile t(p, blockIdx.x / p.splits, static_cast<int>(blockIdx.x % p.splits));
-  if (t.split == 0 && t.state == 1) write_cache<T>(p, t, p.rows);
   const int rows = p.L * p.G, row0 = t.tile * p.rows, wave_row0 = row0 + wave * kWideRows;
 
   float m = kNegInf, sum = 0.f;  // the maximum before the scale
@@ -647,6 +671,15 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
     }
   }
 
+  if (t.split == 0 && t.state == 1) {
+    CacheWrite<T, 2> write;
+    int first;
+    const int rounds = (CacheWrite<T, 2>::tokens(p, t, first) * (p.D / 8) + 128 * kWaves - 1) / (128 * kWaves);
+    for (int i = 0; i < rounds; ++i) {
+      write.ask(p, t, i);
+      write.store(p, t, i);
+    }
+  }
   sum += __shfl_xor(sum, 32);
   const int row = wave_row0 + col;
   const bool ends = p.splits == 1;
@@ -776,7 +809,7 @@ int splits_of(const rnnt_attention_shape_t& s) {
   if (units == 0) return 1;
   int64_t keys = static_cast<int64_t>(s.table) * s.page;
   if (s.left >= 0 && static_cast<int64_t>(s.left) + s.L < keys) keys = static_cast<int64_t>(s.left) + s.L;
-  const int64_t by_grid = (wide(s) ? 512 : 1024) / units, by_keys = keys / 512;
+  const int64_t by_grid = 512 / units, by_keys = keys / 512;
   const int64_t n = by_grid < by_keys ? by_grid : by_keys;
   return static_cast<int>(n < 1 ? 1 : n > kMostSplits ? kMostSplits : n);
 }

@@ -84,6 +84,34 @@ def _shape(kind, size_of, *fields):
     return shape, getattr(_library(), size_of)(shape) if size_of else 0
 
 
+# What a call's checks found, by the sizes, strides, types and GPUs of its tensors: a program makes the same few calls again
+# and again, and the checks of eight tensors cost as much as a launch.
+_plans = {}
+
+
+def _plan(key, check, *args):
+    """check(*args), or what it gave before for tensors alike.  key: what describes them; None, where they are no tensors, is
+    not kept."""
+    try:
+        plan = _plans.get(key)
+    except TypeError:
+        key = plan = None
+    if plan is None:
+        plan = check(*args)
+        if key is not None:
+            if len(_plans) >= 1024:
+                _plans.clear()
+            _plans[key] = plan
+    return plan
+
+
+def _key(what, *tensors):
+    try:
+        return (what,) + tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in tensors])
+    except AttributeError:
+        return None
+
+
 def _no_gradient(what, *tensors):
     """Calls that only serve are refused where a gradient or a tangent would be lost."""
     if not _recorded(*tensors):
@@ -116,7 +144,7 @@ def _check_lens(lens, x):
 
 # ---------------------------------------------------------------- root-mean-square norm
 
-def _norm_args(x, weight, residual, lens, eps):
+def _norm_checks(x, weight, residual, lens):
     _check("x", x)
     if x.dim() < 1:
         raise ValueError("x must be (..., D)")
@@ -127,16 +155,20 @@ def _norm_args(x, weight, residual, lens, eps):
     if lens is not None and x.dim() != 3:
         raise ValueError("lens needs x of (B, L, D)")
     _check_lens(lens, x)
+    B, L = x.shape[:2] if lens is not None else (1, math.prod(x.shape[:-1]))
+    return _shape(NormShape, "rnnt_rms_norm_grad_workspace_bytes", B, L, x.shape[-1], code)
+
+
+def _norm_args(x, weight, residual, lens, eps):
     eps = float(eps)
     if not 0.0 <= eps < math.inf:
         raise ValueError("eps must be finite and not below 0, got %r" % eps)
-    B, L = x.shape[:2] if lens is not None else (1, math.prod(x.shape[:-1]))
-    return _shape(NormShape, "rnnt_rms_norm_grad_workspace_bytes", B, L, x.shape[-1], code), eps
+    return _plan(_key("norm", x, weight, residual, lens), _norm_checks, x, weight, residual, lens), eps
 
 
 def _norm_forward(x, weight, residual, lens, eps, shape):
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x)
+    total = None if residual is None else torch.empty_like(x)
     _call(_library().rnnt_rms_norm, x.device, _ptr(x), _ptr(residual), shape, _ptr(lens), _ptr(weight), eps, _ptr(y),
           _ptr(total))
     return y, total
@@ -246,7 +278,7 @@ def rms_norm8(x, weight, residual=None, lens=None, eps=1e-5):
     (shape, _), eps = _norm_args(x, weight, residual, lens, eps)
     _no_gradient("rms_norm8", x, weight, residual)
     rows, pitch = _empty_rows8(x.shape[:-1], x.shape[-1], x.device)
-    total = None if residual is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    total = None if residual is None else torch.empty_like(x)
     _call(_library().rnnt_rms_norm8, x.device, _ptr(x), _ptr(residual), shape, _ptr(lens), _ptr(weight), eps,
           _ptr(rows.values), pitch, _ptr(rows.scale), _ptr(total))
     return rows if total is None else (rows, total)
@@ -260,19 +292,41 @@ def linear8(x, weight, bias=None, dtype=None):
     weight, a scale for each channel); bias (N,) of the result's type.  dtype: the result's type;
     by default x's, or for Rows8 the bias's, or float32.  No gradient.
     """
-    w_pitch = _check_rows8("weight", weight)
+    rows = isinstance(x, Rows8)
+    key = None
+    if isinstance(weight, Rows8):
+        values, scale = x if rows else (x, None)
+        key = _key((Rows8, rows, dtype), values, scale, *weight, bias)
+        # a row's last 16 bytes may lie behind the tensor: looked at in every call
+        if key is not None and (not weight.values.dim() or weight.values.shape[-1] % 16):
+            key = None
+    (shape, nbytes), dev, out_shape, dtype = _plan(key, _linear8_checks, x, weight, bias, dtype)
+    if rows:
+        _no_gradient("linear8", x.scale, weight.scale, bias)
+    else:
+        _no_gradient("linear8", x, weight.scale, bias)
+    y, ws = _result(out_shape, dtype, dev, nbytes)
     w, w_scale = weight
+    if rows:
+        _call(_library().rnnt_linear8, dev, _ptr(x.values), _ptr(x.scale), _ptr(w), _ptr(w_scale), shape, _ptr(bias), _ptr(y))
+    else:
+        _call(_library().rnnt_linear8_dynamic, dev, _ptr(x), _ptr(w), _ptr(w_scale), shape, _ptr(bias), _ptr(y),
+              *_workspace_args(ws))
+    return y
+
+
+def _linear8_checks(x, weight, bias, dtype):
+    w_pitch = _check_rows8("weight", weight)
+    w = weight.values
     dev = w.device
     if w.dim() != 2:
         raise ValueError("weight must be (N, K)")
     N, K = w.shape
     rows = isinstance(x, Rows8)
     if rows:
-        x_pitch, lead = _check_rows8("x", x, dev), x.scale.shape
+        x_pitch, lead, values = _check_rows8("x", x, dev), x.scale.shape, x.values
         if dtype is None:
             dtype = torch.float32 if bias is None else bias.dtype
-        _no_gradient("linear8", x.scale, w_scale, bias)
-        values = x.values
     else:
         _check("x", x, dev)
         if x.dim() < 1:
@@ -282,21 +336,14 @@ def linear8(x, weight, bias=None, dtype=None):
             dtype = x.dtype
         elif dtype != x.dtype:
             raise TypeError("dtype must be x's, %s, got %s" % (x.dtype, dtype))
-        _no_gradient("linear8", x, w_scale, bias)
     code = dtype_code(dtype, "x")
     if values.shape[-1] != K:
         raise ValueError("x must be (..., %d), got %s" % (K, tuple(values.shape)))
     if bias is not None:
         _check("bias", bias, dev, dtype, w.shape[:1])
-    shape, nbytes = _shape(Linear8Shape, None if rows else "rnnt_linear8_dynamic_workspace_bytes", math.prod(lead), N, K, code,
-                           x_pitch, w_pitch)
-    y, ws = _result((*lead, N), dtype, dev, nbytes)
-    if rows:
-        _call(_library().rnnt_linear8, dev, _ptr(values), _ptr(x.scale), _ptr(w), _ptr(w_scale), shape, _ptr(bias), _ptr(y))
-    else:
-        _call(_library().rnnt_linear8_dynamic, dev, _ptr(x), _ptr(w), _ptr(w_scale), shape, _ptr(bias), _ptr(y),
-              *_workspace_args(ws))
-    return y
+    shape = _shape(Linear8Shape, None if rows else "rnnt_linear8_dynamic_workspace_bytes", math.prod(lead), N, K, code,
+                   x_pitch, w_pitch)
+    return shape, dev, (*lead, N), dtype
 
 
 # ---------------------------------------------------------------- rotary positions
@@ -325,7 +372,7 @@ def _rotary_call(x, freq, start, lens, interleaved, inverse):
     B, L, H, D = x.shape
     shape, _ = _shape(RotaryShape, None, B, L, H, D, 2 * freq.numel(), int(interleaved), dtype_code(x.dtype, "x"),
                       *_strides(x))
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
     _call(_library().rnnt_rotary, x.device, _ptr(x), shape, _ptr(freq), _ptr(start), _ptr(lens), inverse, _ptr(y))
     return y
 
@@ -354,6 +401,15 @@ def rotary(x, freq, start=None, lens=None, interleaved=False):
     first tokens, or None (0); lens (B,) int32: rows behind a length are exactly 0.  Angles are
     formed in float64.
     """
+    _plan(_key("rotary", x, freq, start, lens), _rotary_checks, x, freq, start, lens)
+    if freq.requires_grad:
+        raise ValueError("freq has no gradient")
+    if _recorded(x):
+        return _Rotary.apply(x, freq, start, lens, bool(interleaved))
+    return _rotary_call(x, freq, start, lens, interleaved, 0)
+
+
+def _rotary_checks(x, freq, start, lens):
     _check("x", x, contiguous=False)
     if x.dim() != 4:
         raise ValueError("x must be (B, L, H, D)")
@@ -363,14 +419,10 @@ def rotary(x, freq, start=None, lens=None, interleaved=False):
     _check("freq", freq, x.device, torch.float64)
     if freq.dim() != 1 or not 1 <= freq.numel() <= x.shape[3] // 2:
         raise ValueError("freq must hold at most half as many values as a head has channels, and one at least")
-    if freq.requires_grad:
-        raise ValueError("freq has no gradient")
     if start is not None:
         _check("start", start, x.device, torch.int32, x.shape[:1])
     _check_lens(lens, x)
-    if _recorded(x):
-        return _Rotary.apply(x, freq, start, lens, bool(interleaved))
-    return _rotary_call(x, freq, start, lens, interleaved, 0)
+    return True
 
 
 # ---------------------------------------------------------------- attention over a paged cache
@@ -389,6 +441,23 @@ def cached_attention(q, k, v, k_cache, v_cache, pages, cached, lens=None, scale=
     used.  scale: of the scores, D ** -0.5 by default.  Rows behind lens are exactly 0.  A page that
     a call writes to belongs to one utterance.  No gradient.
     """
+    if left is not None and left < 0:
+        raise ValueError("left must be None or at least 0, got %r" % (left,))
+    causal, left = bool(causal), -1 if left is None else int(left)
+    key = _key((causal, left), q, k, v, k_cache, v_cache, pages, cached, lens)
+    shape, nbytes = _plan(key, _attention_checks, q, k, v, k_cache, v_cache, pages, cached, lens, causal, left)
+    _no_gradient("cached_attention", q, k, v, k_cache, v_cache)
+    scale = max(shape.D, 1) ** -0.5 if scale is None else float(scale)
+    if nbytes or not q.is_contiguous():
+        out, ws = _result(q.shape, q.dtype, q.device, nbytes)
+    else:
+        out, ws = torch.empty_like(q), None
+    _call(_library().rnnt_cached_attention, q.device, _ptr(q), _ptr(k), _ptr(v), shape, _ptr(lens), _ptr(cached), _ptr(pages),
+          _ptr(k_cache), _ptr(v_cache), scale, _ptr(out), *_workspace_args(ws))
+    return out
+
+
+def _attention_checks(q, k, v, k_cache, v_cache, pages, cached, lens, causal, left):
     for name, t in (("q", q), ("k", k), ("v", v)):
         _check(name, t, q.device if isinstance(q, torch.Tensor) else None, q.dtype if isinstance(q, torch.Tensor) else None,
                contiguous=False)
@@ -411,14 +480,6 @@ def cached_attention(q, k, v, k_cache, v_cache, pages, cached, lens=None, scale=
     _check("cached", cached, dev, torch.int32, (B,))
     if lens is not None:
         _check("lens", lens, dev, torch.int32, (B,))
-    _no_gradient("cached_attention", q, k, v, k_cache, v_cache)
-    scale = D ** -0.5 if scale is None else float(scale)
-    if left is not None and left < 0:
-        raise ValueError("left must be None or at least 0, got %r" % (left,))
-    left = -1 if left is None else min(int(left), 0x7fffffff)
-    shape, nbytes = _shape(AttentionShape, "rnnt_cached_attention_workspace_bytes", B, L, Hq, Hkv, D, k_cache.shape[2],
-                           pages.shape[1], k_cache.shape[0], int(bool(causal)), left, code, *_strides(q), *_strides(k), *_strides(v))
-    out, ws = _result((B, L, Hq, D), q.dtype, dev, nbytes)
-    _call(_library().rnnt_cached_attention, dev, _ptr(q), _ptr(k), _ptr(v), shape, _ptr(lens), _ptr(cached), _ptr(pages),
-          _ptr(k_cache), _ptr(v_cache), scale, _ptr(out), *_workspace_args(ws))
-    return out
+    return _shape(AttentionShape, "rnnt_cached_attention_workspace_bytes", B, L, Hq, Hkv, D, k_cache.shape[2],
+                  pages.shape[1], k_cache.shape[0], int(causal), min(left, 0x7fffffff), code, *_strides(q), *_strides(k),
+                  *_strides(v))
