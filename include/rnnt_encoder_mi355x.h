@@ -32,8 +32,8 @@ extern "C" {
  * Squares are summed in float32: a row whose squares pass its range (values of about 1e18)
  * gives 0 where the values are finite, as one that holds an infinity does.
  *
- * The gradient takes t as stored (sum_out, or x where there is no residual) and the
- * gradients dy and dsum (NULL: zero) of y and of sum_out:
+ * The gradient forms t again from x and residual, without the rounding of sum_out, and takes
+ * the gradients dy and dsum (NULL: zero) of y and of sum_out:
  *   r = 1 / sqrt(mean(t^2) + eps),  g = dy * weight,
  *   dx = r (g - t r^2 mean(g t)) + dsum,   dweight = sum over valid rows of dy t r;
  * dx is the gradient of x and of residual alike.  dweight's sums have one order, so equal
@@ -51,9 +51,9 @@ rnnt_status_t rnnt_rms_norm(const void* x, const void* residual, rnnt_norm_shape
                             const void* weight, float eps, void* y, void* sum_out, hipStream_t stream);
 
 size_t rnnt_rms_norm_grad_workspace_bytes(rnnt_norm_shape_t shape);
-rnnt_status_t rnnt_rms_norm_grad(const void* sum, rnnt_norm_shape_t shape, const int32_t* lens, const void* weight,
-                                 float eps, const void* dy, const void* dsum, void* dx, void* dweight, void* workspace,
-                                 size_t workspace_bytes, hipStream_t stream);
+rnnt_status_t rnnt_rms_norm_grad(const void* x, const void* residual, rnnt_norm_shape_t shape, const int32_t* lens,
+                                 const void* weight, float eps, const void* dy, const void* dsum, void* dx,
+                                 void* dweight, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Rows in 8 bits: signed integers and one float32 scale a row,

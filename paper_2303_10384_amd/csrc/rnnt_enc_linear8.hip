@@ -271,7 +271,7 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
   if constexpr (DYNAMIC) {
     const T* from = reinterpret_cast<const T*>(l.x);
     int8_t* to = reinterpret_cast<int8_t*>(lds) + wave * Rows::kBytes;
-    if (l.K % kVec<T> == 0) x.template quantize<true>(from, m0, l.M, l.K, to, row_scales[wave]);
+    if (l.K % 4 == 0) x.template quantize<true>(from, m0, l.M, l.K, to, row_scales[wave]);
     else x.template quantize<false>(from, m0, l.M, l.K, to, row_scales[wave]);
   } else {
     x.take(l.x, l.x_pitch, l.x_scale, m0, l.M, l.K);

@@ -60,7 +60,7 @@ def _library():
     for name, res, args in (
             ("rnnt_rms_norm", ints, [_vp, _vp, n, _vp, _vp, f32, _vp, _vp, _vp]),
             ("rnnt_rms_norm_grad_workspace_bytes", _sz, [n]),
-            ("rnnt_rms_norm_grad", ints, [_vp, n, _vp, _vp, f32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+            ("rnnt_rms_norm_grad", ints, [_vp, _vp, n, _vp, _vp, f32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
             ("rnnt_quantize_rows", ints, [_vp, _i64, _i32, ints, _vp, _i64, _vp, _vp]),
             ("rnnt_rms_norm8", ints, [_vp, _vp, n, _vp, _vp, f32, _vp, _i64, _vp, _vp, _vp]),
             ("rnnt_linear8", ints, [_vp, _vp, _vp, _vp, m, _vp, _vp, _vp]),
@@ -180,20 +180,20 @@ class _RmsNorm(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         ctx.shape, ctx.eps = shape, eps
         y, total = _norm_forward(x, weight, residual, lens, eps, shape[0])
-        ctx.save_for_backward(x if total is None else total, weight, lens)
+        ctx.save_for_backward(x, residual, weight, lens)
         return y if total is None else (y, total)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, dsum=None):
-        total, weight, lens = _dense(*ctx.saved_tensors)
+        x, residual, weight, lens = _dense(*ctx.saved_tensors)
         shape, nbytes = ctx.shape
-        dy = torch.zeros_like(total) if dy is None else dy.contiguous()
+        dy = torch.zeros_like(x) if dy is None else dy.contiguous()
         dsum = None if dsum is None else dsum.contiguous()
-        dx, ws = _result(total.shape, total.dtype, total.device, nbytes)
+        dx, ws = _result(x.shape, x.dtype, x.device, nbytes)
         dw = torch.empty_like(weight)
-        _call(_library().rnnt_rms_norm_grad, total.device, _ptr(total), shape, _ptr(lens), _ptr(weight), ctx.eps, _ptr(dy),
-              _ptr(dsum), _ptr(dx), _ptr(dw), *_workspace_args(ws))
+        _call(_library().rnnt_rms_norm_grad, x.device, _ptr(x), _ptr(residual), shape, _ptr(lens), _ptr(weight), ctx.eps,
+              _ptr(dy), _ptr(dsum), _ptr(dx), _ptr(dw), *_workspace_args(ws))
         return dx, dw, dx if ctx.needs_input_grad[2] else None, None, None, None
 
 
@@ -297,9 +297,9 @@ def linear8(x, weight, bias=None, dtype=None):
     if isinstance(weight, Rows8):
         values, scale = x if rows else (x, None)
         key = _key((Rows8, rows, dtype), values, scale, *weight, bias)
-        # a row's last 16 bytes may lie behind the tensor: looked at in every call
-        if key is not None and (not weight.values.dim() or weight.values.shape[-1] % 16):
-            key = None
+        # a row's last 16 bytes may lie behind the tensor, which its memory says
+        if key is not None and weight.values.dim() and weight.values.shape[-1] % 16:
+            key += tuple([(t.storage_offset(), t.untyped_storage().nbytes()) for t in ((values, weight.values) if rows else (weight.values,))])
     (shape, nbytes), dev, out_shape, dtype = _plan(key, _linear8_checks, x, weight, bias, dtype)
     if rows:
         _no_gradient("linear8", x.scale, weight.scale, bias)

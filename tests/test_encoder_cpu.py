@@ -51,7 +51,7 @@ def test_norm_refusals(enc):
           "scale": FAKE, "sum": FAKE, "stream": None}
     need = lib.rnnt_rms_norm_grad_workspace_bytes(ok)
     assert need > 0 and need % 256 == 0
-    bwd = {"sum": FAKE, "shape": ok, "lens": FAKE, "weight": FAKE, "eps": 0.0, "dy": FAKE, "dsum": FAKE, "dx": FAKE, "dw": FAKE,
+    bwd = {"x": FAKE, "residual": FAKE, "shape": ok, "lens": FAKE, "weight": FAKE, "eps": 0.0, "dy": FAKE, "dsum": FAKE, "dx": FAKE, "dw": FAKE,
            "ws": FAKE, "bytes": need - 1, "stream": None}
     calls = ((lib.rnnt_rms_norm, fwd), (lib.rnnt_rms_norm8, q8), (lib.rnnt_rms_norm_grad, bwd))
     for shape, want in ((S(0, 3, 40, 1), 2), (S(2, -1, 40, 1), 2), (S(2, 3, 0, 1), 2), (S(2, 3, 40, 3), 4),
@@ -69,7 +69,8 @@ def test_norm_refusals(enc):
     for over, want in (({"q": None}, 1), ({"scale": None}, 1), ({"q": FAKE + 8}, 7), ({"pitch": 40}, 7), ({"pitch": 32}, 7),
                        ({"scale": FAKE + 2}, 7), ({"sum": None}, 1)):
         assert call(lib.rnnt_rms_norm8, q8, over) == want
-    for over, want in (({}, 6), ({"sum": None}, 1), ({"dy": None}, 1), ({"dx": None}, 1), ({"dw": None}, 1), ({"dsum": None}, 6),
+    for over, want in (({}, 6), ({"x": None}, 1), ({"dy": None}, 1), ({"dx": None}, 1), ({"dw": None}, 1), ({"dsum": None}, 6),
+                       ({"residual": None}, 6), ({"x": FAKE + 1}, 7), ({"residual": FAKE + 1}, 7),
                        ({"dy": FAKE + 1}, 7), ({"dsum": FAKE + 1}, 7), ({"dw": FAKE + 1}, 7), ({"ws": FAKE + 16, "bytes": need}, 7)):
         assert call(lib.rnnt_rms_norm_grad, bwd, over) == want
     assert call(lib.rnnt_rms_norm, fwd, {"shape": S(2, 0, 40, 1), "x": None, "y": None}) == 0
@@ -361,4 +362,4 @@ def test_norm_gradient_of_tensors_saved_elsewhere(enc, calls):
             y = got if residual is None else got[0]
             torch.autograd.grad(y, (x, w), torch.ones_like(y).transpose(0, 1).contiguous().transpose(0, 1))
         name, bwd = calls[-1]
-        assert name == "rnnt_rms_norm_grad" and bwd[6] is None and bwd[5] is not None
+        assert name == "rnnt_rms_norm_grad" and bwd[7] is None and bwd[6] is not None and (bwd[1] is None) == (residual is None)

@@ -79,9 +79,8 @@ def test_norm(torch, pkg, case, dtype):  # noqa: F811
     ups = (dy, ds) if r is not None else (dy,)
     heads = (y, total) if r is not None else (y,)
     grads = torch.autograd.grad(heads, leaves, ups, retain_graph=True)
-    stored = xd if r is None else total.detach().double().cpu().numpy()  # the sum as it was stored
-    dx, dw, size, dw_size = R.rms_norm_grad(stored, wd, dyd, dsd if r is not None else None, lens, 1e-3)
-    # sums of up to 42 roundings in the two sums, the square's half twice; a few products around them
+    dx, dw, size, dw_size = R.rms_norm_grad(t, wd, dyd, dsd if r is not None else None, lens, 1e-3)
+    # sums of up to 42 roundings in the two sums, the square's half twice; a few products around them; t's own rounding
     close(grads[0], dx, HALF[dtype] * np.abs(dx) + 2 * 60 * ONE * size + TINY[dtype], "dx")
     n = x.shape[0] * x.shape[1]
     # a column: its rows in order within a block and the blocks' sums, at most n roundings; r and two products
@@ -96,7 +95,7 @@ def test_norm(torch, pkg, case, dtype):  # noqa: F811
         close(only[0], np.where(valid[..., None], dsd, 0.0), 0.0, "dsum alone")
         assert not bool(only[1].any())
         only = torch.autograd.grad(y, leaves, dy)
-        dx, _, size, _ = R.rms_norm_grad(stored, wd, dyd, None, lens, 1e-3)
+        dx, _, size, _ = R.rms_norm_grad(t, wd, dyd, None, lens, 1e-3)
         close(only[0], dx, HALF[dtype] * np.abs(dx) + 2 * 60 * ONE * size + TINY[dtype], "dy alone")
     with torch.no_grad():
         again = pkg.rms_norm(x, w, r, ints(torch, lens), eps=1e-3)
@@ -218,7 +217,7 @@ LINEAR = [  # M, K, N
     (0, 8, 4), (15, 2047, 1), (1100, 256, 160), (128, 16, 300), (513, 1040, 272),
     # past the form for few rows: rows held in registers, and rows too long for that
     (700, 127, 1000), (2100, 640, 300), (1500, 1024, 501), (4100, 5, 257), (33000, 130, 15), (2049, 768, 289), (1100, 1040, 1000),
-    (2048, 1030, 523), (40, 3969, 70), (30, 5000, 33)]
+    (2048, 1030, 523), (40, 3969, 70), (30, 5000, 33), (900, 516, 700)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
