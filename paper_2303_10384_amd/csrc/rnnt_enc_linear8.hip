@@ -40,9 +40,10 @@ __device__ __forceinline__ u32x4 load_bytes(const int8_t* row, int k, int K) {
   return v;
 }
 
-// A tile of 128 x 128 results to a block, 64 x 64 to a wave.  Steps of 128 bytes of k go through registers into two
-// buffers of LDS in turn; the 16-byte pieces of a row lie at (piece ^ row % 8), so that the 32 rows that a matrix
-// instruction reads at one piece meet all banks.
+// Rows of any length, already in 8 bits: a tile of 128 x 128 results to a block, 64 x 64 to a wave.  Steps of 128 bytes of
+// k go through registers into two buffers of LDS in turn; the 16-byte pieces of a row lie at (piece ^ row % 8), so that the
+// 32 rows that a matrix instruction reads at one piece meet all banks.  For rows past kHeldMost alone: at K = 640 the two
+// launches, with x in 8 bits through memory between them, took 1969 us where the form below takes 810 (M = 648000).
 template <typename T>
 __global__ __launch_bounds__(256) void enc_linear8(Linear8Params p) {
   __shared__ u32x4 lds[2][2][kTile * kStep / 16];
@@ -171,8 +172,12 @@ __device__ __forceinline__ void quantize_rows_of_wave(const T* x, int64_t m0, in
 // ---- rows held in registers ----------------------------------------------------
 // For rows of up to 1024 a block of four waves keeps 128 rows of x, 32 to a wave, in registers in the matrix
 // instruction's order, and passes over its share of w, 64 rows at a time through LDS.  x is read once, whatever N is,
-// and taken to 8 bits on the way in, so no copy of it in 8 bits goes through memory.  LDS serves a quarter of what two
-// operands from LDS would need.  Results go through LDS to whole runs of a row.
+// and taken to 8 bits on the way in, so no copy of it in 8 bits goes through memory; results go through LDS to whole runs of
+// a row.  648000 rows of 640 bf16 to 1025: 810 us, 1.05 POP/s and 2.7 TB/s, the product alone by the library 933.  The
+// matrix units are busy for 28 % of the cycles, LDS for 36 %, the vector units for 35 %, at about 1.9 GHz: without quantizing 190 us
+// less, without storing 190, without both 440 in all.  Tried, and no faster: 64 rows to a wave (half the reads of w, one wave to a
+// SIMD: 900 us, with a turn's results among the next one's products too), 32 rows of w to a turn and three blocks to a CU (890-1040),
+// half the blocks out of step with the others (815), results stored past the caches (1300).
 constexpr int kHeldRows = 32;     // of x to a wave
 constexpr int kHeldTile = 64;     // rows of w to a turn
 constexpr int kHeldWaves = 4;
@@ -386,14 +391,15 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
 // ---- few rows ------------------------------------------------------------------
 // A block takes 16 or 32 rows of x into LDS, in 8 bits, and multiplies them with a few tiles of 16 rows of w, which go from
 // memory to registers and nowhere else.  Where tiles are fewer than CUs the four waves share out k, and their sums meet in
-// LDS; else they share out the tiles.  The first pieces of w are asked for before x is there.
+// LDS; else they share out the tiles.  The first pieces of w are asked for before x is there.  Bound by the way from launch to
+// store, three round trips to memory: 16 rows of 640 f16 to 1025 take 6.9 us in one launch, 2.8 + 10.3 in two.
 struct FewParams {
   Linear8Params l;
   int32_t pitch;        // of a row of x in LDS: whole steps of 64 bytes, and 16, so that sixteen rows meet all banks
   int32_t tiles, blocks, tiles_of_wave;  // of w; blocks to the same rows of x; 0: the waves share out k
 };
 constexpr int kFewAhead = 4;
-constexpr int kFewLds = 64000;
+constexpr int kFewLds = 56000;  // and the waves' sums, within the 64 KB that a launch has without asking
 
 template <typename T, int MT, int NV, bool DYNAMIC>
 __global__ __launch_bounds__(256) void enc_linear8_few(FewParams p) {

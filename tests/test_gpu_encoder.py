@@ -217,7 +217,7 @@ LINEAR = [  # M, K, N
     (0, 8, 4), (15, 2047, 1), (1100, 256, 160), (128, 16, 300), (513, 1040, 272),
     # past the form for few rows: rows held in registers, and rows too long for that
     (700, 127, 1000), (2100, 640, 300), (1500, 1024, 501), (4100, 5, 257), (33000, 130, 15), (2049, 768, 289), (1100, 1040, 1000),
-    (2048, 1030, 523), (40, 3969, 70), (30, 5000, 33), (900, 516, 700)]
+    (2048, 1030, 523), (40, 3969, 70), (30, 5000, 33), (900, 516, 700), (20, 3420, 70)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -695,6 +695,34 @@ def test_workspaces_of_two_graphs(torch, pkg):  # noqa: F811
             again = fn()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(again, want))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_odd_addresses(torch, pkg, dtype):  # noqa: F811
+    """Tensors that begin an element past an aligned address give the bits of aligned ones."""
+    g = torch.Generator(device="cuda").manual_seed(10)
+
+    def two(*shape):
+        n = int(np.prod(shape))
+        a = torch.randn(n + 1, device="cuda", generator=g).to(td(torch, dtype))[1:].view(shape)
+        return a, a.clone()
+    (x, x1), (r, r1), (w, w1), (dy, dy1) = two(3, 40, 136), two(3, 40, 136), two(136), two(3, 40, 136)
+    for t in (x, x1, w, w1):
+        t.requires_grad_(True)
+    got, want = pkg.rms_norm(x, w, r), pkg.rms_norm(x1, w1, r1)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(got[0], (x, w), dy), torch.autograd.grad(want[0], (x1, w1), dy1)))
+    x, x1, w, w1 = (t.detach() for t in (x, x1, w, w1))
+    got, want = pkg.rms_norm8(x, w, r), pkg.rms_norm8(x1, w1, r1)
+    assert torch.equal(got[0].values, want[0].values) and torch.equal(got[0].scale, want[0].scale) and torch.equal(got[1], want[1])
+    assert torch.equal(pkg.quantize_rows(x).values, pkg.quantize_rows(x1).values)
+    freq = pkg.rotary_frequencies(8)
+    for inter in (False, True):
+        assert torch.equal(pkg.rotary(x.view(3, 40, 8, 17), freq, interleaved=inter), pkg.rotary(x1.view(3, 40, 8, 17), freq, interleaved=inter))
+    w8 = pkg.quantize_rows(torch.randn((70, 136), device="cuda", generator=g))
+    (bias, bias1), (many, many1) = two(70), two(9000, 136)
+    assert torch.equal(pkg.linear8(x, w8, bias), pkg.linear8(x1, w8, bias1))
+    assert torch.equal(pkg.linear8(many, w8, bias), pkg.linear8(many1, w8, bias1))
 
 
 def test_two_streams_at_once(torch, pkg):  # noqa: F811
