@@ -28,7 +28,8 @@ extern "C" {
  *
  *   t = x + residual (x where residual is NULL),   y = t / sqrt(mean(t^2) + eps) * weight
  * over the rows of x (B, L, D); weight (D) of the same type.  sum_out receives t, rounded
- * (NULL only where residual is NULL); y is formed from t before that rounding.
+ * (where residual is NULL it is not written, and may be NULL); y is formed from t before that
+ * rounding.
  * Squares are summed in float32: a row whose squares pass its range (values of about 1e18)
  * gives 0 where the values are finite, as one that holds an infinity does.
  *

@@ -352,6 +352,39 @@ def test_gradients_past_a_launch_and_forward_mode(enc, calls):
         assert len(calls) == n + 1
 
 
+def test_checks_are_made_again_for_other_tensors(enc, monkeypatch):
+    """What the checks of a call found holds for tensors of its sizes, strides, types and GPU alone."""
+    import paper_2303_10384_amd as rnnt
+    from paper_2303_10384_amd import binding
+    made = []
+    monkeypatch.setattr(enc, "_plans", {})
+    monkeypatch.setattr(enc, "_call", lambda fn, device, *args: made.append((fn.__name__, args)))
+    monkeypatch.setattr(binding, "_capturing", lambda device: False)
+    checks = []
+    monkeypatch.setattr(enc, "_check", lambda name, t, *args, **kw: checks.append(name))
+    x, w = torch.randn(4, 32), torch.randn(32)
+    for t, again in ((x, True), (x.clone(), False), (torch.randn(5, 32), True), (torch.randn(32, 4).t(), True), (x.half(), True),
+                     (x.clone(), False), (torch.randn(8, 32)[::2], True)):
+        n = len(checks)
+        rnnt.rms_norm(t, w)
+        assert (len(checks) > n) == again
+    w8 = rnnt.Rows8(torch.zeros(5, 32, dtype=torch.int8), torch.zeros(5))
+    odd = torch.zeros(5 * 32, dtype=torch.int8).as_strided((5, 20), (32, 1))
+    short = torch.zeros(4 * 32 + 20, dtype=torch.int8).as_strided((5, 20), (32, 1))  # the last row ends inside 16 bytes
+    rnnt.linear8(x, w8)
+    rnnt.linear8(x[:, :20].contiguous(), rnnt.Rows8(odd, torch.zeros(5)))
+    with pytest.raises(ValueError, match="pieces"):
+        rnnt.linear8(x[:, :20].contiguous(), rnnt.Rows8(short, torch.zeros(5)))
+    with pytest.raises(ValueError, match="x must be"):
+        rnnt.linear8(x[:, :20].contiguous(), w8)
+    for _ in range(2):
+        with pytest.raises(TypeError, match="dtype"):
+            rnnt.linear8(x, w8, dtype=torch.float16)
+    for i in range(1030):  # and not without end
+        rnnt.rms_norm(torch.empty(i + 1, 2), w[:2])
+    assert len(enc._plans) <= 1024
+
+
 def test_norm_gradient_of_tensors_saved_elsewhere(enc, calls):
     """Hooks on saved tensors may give any layout back: the gradient's call takes dense ones."""
     import paper_2303_10384_amd as rnnt

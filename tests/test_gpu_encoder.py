@@ -725,6 +725,40 @@ def test_odd_addresses(torch, pkg, dtype):  # noqa: F811
     assert torch.equal(pkg.linear8(many, w8, bias), pkg.linear8(many1, w8, bias1))
 
 
+def test_capture_without_a_workspace_is_refused(torch, pkg):  # noqa: F811
+    """The C calls under a capture take no workspace of their own, and eagerly do."""
+    enc = pkg.encoder
+    lib = enc._library()
+    x, w = torch.ones((40, 96), device="cuda"), torch.ones((96,), device="cuda")
+    dx, dw = torch.zeros_like(x), torch.zeros_like(w)
+    wide = torch.ones((3000, 1040), device="cuda")
+    w8 = pkg.quantize_rows(torch.ones((900, 1040), device="cuda"))
+    y = torch.zeros((3000, 900), device="cuda")
+    q, cache = torch.ones((1, 1, 2, 64), device="cuda"), torch.ones((100, 2, 64, 64), device="cuda")
+    pages, cached, out = torch.arange(100, device="cuda", dtype=torch.int32), ints(torch, [6000]), torch.zeros((1, 1, 2, 64), device="cuda")
+    ptr = lambda t: t.data_ptr()  # noqa: E731
+    attention = enc.AttentionShape(1, 1, 2, 2, 64, 64, 100, 100, 1, -1, 0, *[128, 128, 64] * 3)
+
+    def calls(stream):
+        return (lib.rnnt_rms_norm_grad(ptr(x), None, enc.NormShape(1, 40, 96, 0), None, ptr(w), 1e-5, ptr(x), None, ptr(dx), ptr(dw), None, 0, stream),
+                lib.rnnt_linear8_dynamic(ptr(wide), ptr(w8.values), ptr(w8.scale), enc.Linear8Shape(3000, 900, 1040, 0, 0, 1040), None, ptr(y), None, 0, stream),
+                lib.rnnt_cached_attention(ptr(q), ptr(q), ptr(q), attention, None, ptr(cached), ptr(pages), ptr(cache), ptr(cache.clone()), 0.125, ptr(out), None, 0, stream))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        status = calls(torch.cuda.current_stream().cuda_stream)
+        dx.zero_()
+    assert status == (6, 6, 6)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert calls(torch.cuda.current_stream().cuda_stream) == (0, 0, 0)
+    torch.cuda.synchronize()
+    # rows of ones: dw = the sum of 40 rows of t r, y = 1040 (both scales 1 / 127), attention of ones
+    r = (1 + 1e-5) ** -0.5
+    assert bool(((dw - 40 * r).abs() <= 200 * ONE * 40).all()) and bool(((y - 1040).abs() <= 8 * ONE * 1040).all())
+    assert bool(((out - 1).abs() <= 1e-4).all())
+
+
 def test_two_streams_at_once(torch, pkg):  # noqa: F811
     g = torch.Generator(device="cuda").manual_seed(8)
     x = torch.randn((4, 3000, 640), device="cuda", generator=g).bfloat16()
