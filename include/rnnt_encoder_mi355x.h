@@ -154,8 +154,8 @@ rnnt_status_t rnnt_rotary(const void* x, rnnt_rotary_shape_t shape, const double
  * stride below 0.  RNNT_ERR_BAD_VARIANT: scale not finite.  RNNT_ERR_ALIGNMENT: q, k or v not 16-byte
  * aligned, or a stride that is no multiple of 16 bytes.  RNNT_ERR_UNSUPPORTED: D no multiple of 8 or above 256, page
  * no power of two or above 1024, a stride of k's or v's tokens of 2^31 or more, num_pages * Hkv * page or L * Hq of 2^31 or more, table * page + L of 2^30 or more,
- * or B * Hkv times the tiles of an utterance's L * (Hq / Hkv) rows (16 rows, or 128 in 16 bits with D <= 128 and
- * more than 32 rows) of 2^23 or more.
+ * or B * Hkv times the tiles of an utterance's L * (Hq / Hkv) rows (16 rows, or 128 where they are many) of 2^23 or
+ * more.
  */
 typedef struct {
   int32_t B, L, Hq, Hkv, D, page, table, num_pages, causal, left;

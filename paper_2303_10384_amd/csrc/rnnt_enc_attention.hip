@@ -775,9 +775,14 @@ __global__ __launch_bounds__(256) void enc_attention_join(AttentionParams p) {
 
 // ---- host ---------------------------------------------------------------------
 
-// Whether the rows of an utterance's head of keys fill wide tiles
+// Whether wide tiles take the rows of an utterance's head of keys: past 64 of them, or past 16 where tiles of sixteen would be more
+// than two to a CU (us, sixteen rows and wide; tokens, 64 streams of 8 heads of 64 over 300: 20 24.2 and 17.5, 40 31 and 20.6, 128 79 and
+// 25.8; 8 of 4 heads of 128 over 1000: 20 16.2 and 19.8, 64 22.9 and 23.8, 128 32.5 and 29.7; 1 of 4 heads of 64 over 4000: 64 13.8 and
+// 13.9, 128 14.8 and 14.3).
 bool wide(const rnnt_attention_shape_t& s) {
-  return s.dtype != RNNT_DTYPE_F32 && s.D <= 128 && static_cast<int64_t>(s.L) * (s.Hq / s.Hkv) > 32;
+  const int64_t rows = static_cast<int64_t>(s.L) * (s.Hq / s.Hkv);
+  const int64_t narrow = static_cast<int64_t>(s.B) * s.Hkv * ((rows + kRowTile - 1) / kRowTile);
+  return s.dtype != RNNT_DTYPE_F32 && s.D <= 128 && (rows > 64 || (rows > 16 && narrow > 512));
 }
 int rows_of(const rnnt_attention_shape_t& s) { return wide(s) ? kWaves * kWideRows : kRowTile; }
 
@@ -815,7 +820,10 @@ int splits_of(const rnnt_attention_shape_t& s) {
   if (units == 0) return 1;
   int64_t keys = static_cast<int64_t>(s.table) * s.page;
   if (s.left >= 0 && static_cast<int64_t>(s.left) + s.L < keys) keys = static_cast<int64_t>(s.left) + s.L;
-  const int64_t by_grid = 512 / units, by_keys = keys / 512;
+  // few keys: the join costs more (128 tiles over 600: 11.6 us in one block each, 15 in four); else 128 keys to a block at least (1000
+  // keys, one tile: 13.2 with 512, 10.9 with 256, 9.6; 4000 keys, 8 tiles: 19.6, 16.1, 15.0; 20000, 2 tiles: 15.4, 12.9, 13.3)
+  if (keys < 768) return 1;
+  const int64_t by_grid = 512 / units, by_keys = keys / 128;
   const int64_t n = by_grid < by_keys ? by_grid : by_keys;
   return static_cast<int>(n < 1 ? 1 : n > kMostSplits ? kMostSplits : n);
 }
