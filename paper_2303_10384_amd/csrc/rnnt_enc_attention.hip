@@ -773,6 +773,46 @@ __global__ __launch_bounds__(256) void enc_attention_join(AttentionParams p) {
   for (int j = 0; j < 4; ++j) ElemTraits<T>::store1(out + c + j, sum[j] / total);
 }
 
+// The same of few splits, where rows are many and a block to a row would fetch a few hundred bytes.  Four channels of a row to a
+// thread, which goes over the splits in their order.  A call with a block to a row and with this (us; streams, heads of queries on heads
+// of keys, D, tokens, cached): two splits, 8 of 8 of 64, 512 over 500 79 and 32.5; five, 2 of 16 on 2 of 64, 374 over 2000 45.6 and 29.3;
+// eight, 2 of 4 on 1 of 64, 600 over 500 23.8 and 17.4; sixteen, 16 of 16 on 2 of 128, one over 3000 20 and 21.2; 47 splits, 1 of 4 of 64,
+// one over 6000 10.3 and 17.6.  (units x splits <= 512 keeps the indexes within 32 bits.)
+constexpr int kFewSplits = 8;
+template <typename T>
+__global__ __launch_bounds__(256) void enc_attention_join_few(AttentionParams p) {
+  const int lanes = p.D / 4, thread = static_cast<int>(blockIdx.x * 256 + threadIdx.x), at = thread / lanes, c = 4 * (thread - at * lanes);
+  const int units = p.B * p.Hkv * p.tiles, unit = at / p.rows, in_tile = at - unit * p.rows;
+  if (unit >= units) return;
+  const Tile t(p, unit, 0);
+  const int row = t.tile * p.rows + in_tile;
+  if (row >= p.L * p.G) return;
+  const int token = row / p.G, head = t.h * p.G + row - token * p.G;
+  T* out = static_cast<T*>(p.out) + ((static_cast<int64_t>(t.b) * p.L + token) * p.Hq + head) * p.D + c;
+  if (t.state < 0 || token >= t.n) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ElemTraits<T>::store1(out + j, t.state < 0 ? __builtin_nanf("") : 0.f);
+    return;
+  }
+  const int64_t first = static_cast<int64_t>(unit) * p.splits * p.rows + in_tile;  // the first split's row
+  const float* stats = p.part + static_cast<int64_t>(units) * p.splits * p.rows * p.D;
+  float top = kNegInf;
+#pragma unroll 4
+  for (int s = 0; s < p.splits; ++s) top = __builtin_fmaxf(top, stats[(first + static_cast<int64_t>(s) * p.rows) * 2]);
+  const float by = top == kNegInf ? 0.f : top;
+  float total = 0.f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < p.splits; ++s) {
+    const int64_t of = first + static_cast<int64_t>(s) * p.rows;
+    const float factor = fast_exp2(stats[of * 2] - by);
+    total = __builtin_fmaf(stats[of * 2 + 1], factor, total);
+    sum += factor * *reinterpret_cast<const f32x4*>(p.part + of * p.D + c);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) ElemTraits<T>::store1(out + j, sum[j] / total);
+}
+
 // ---- host ---------------------------------------------------------------------
 
 // Whether wide tiles take the rows of an utterance's head of keys: past 64 of them, or past 16 where tiles of sixteen would be more
@@ -922,6 +962,11 @@ rnnt_status_t rnnt_cached_attention(const void* q, const void* k, const void* v,
       return launched();
     });
     if (st != RNNT_OK || p.splits == 1) return st;
+    if (p.splits <= kFewSplits) {
+      const int64_t threads = units * p.rows * (s.D / 4);
+      hipLaunchKernelGGL((enc_attention_join_few<T>), dim3(static_cast<uint32_t>((threads + 255) / 256)), dim3(256), 0, stream, p);
+      return launched();
+    }
     hipLaunchKernelGGL((enc_attention_join<T>), dim3(static_cast<uint32_t>(units * p.rows)), dim3(256), 0, stream, p);
     return launched();
   });

@@ -515,6 +515,18 @@ def test_attention_over_a_long_cache(torch, pkg, dtype, B, L, Hq, Hkv, D, page, 
         close(out[b], want, attention_tolerance(want, size, score_size, D, S, float(v.abs().max()), dtype), "out")
 
 
+@pytest.mark.parametrize("dtype,L,Hkv", [(d, 60, 2) for d in DTYPES] + [("bf16", 300, 4)])
+def test_attention_keys_of_many_rows_shared_by_few_blocks(torch, pkg, dtype, L, Hkv):  # noqa: F811
+    """Two to eight blocks to a tile of rows; an utterance is empty, one has a single token, then one's length is bad."""
+    cached, lens = np.array([600, 700, 0, 650, 3]), np.array([L, 0, 1, L - 21, L])
+    new, newd, caches, cachesd, pages, _ = attention_case(torch, 5, L, 2 * Hkv, Hkv, 40, 32, cached, lens, dtype, L)
+    out = check_attention(torch, pkg, new, newd, caches, cachesd, pages, cached, lens, dtype)
+    for wrong in (-1, L + 1):
+        lens[4] = wrong
+        again = pkg.cached_attention(*new, *[c.clone() for c in caches], ints(torch, pages), ints(torch, cached), ints(torch, lens))
+        assert torch.equal(again[:4], out[:4]) and bool(again[4].isnan().all())
+
+
 def test_attention_offsets_past_32_bits(torch, pkg):  # noqa: F811
     """A cache of 6 GB: pages whose rows lie past 2^31 elements and 2^32 bytes."""
     D, page, Hkv = 128, 64, 2
