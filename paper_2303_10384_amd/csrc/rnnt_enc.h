@@ -21,6 +21,15 @@ struct MaxBitsOp {
   }
 };
 
+// What the lanes of a wave stored into LDS before this is there for its other lanes behind it, and what they read before it
+// is read.  A wave's accesses to LDS keep their order, so it takes no instruction: it is the compiler that must not move any
+// of them across, which nothing else forbids where the addresses of two lanes differ.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // ---- rows in 8 bits -----------------------------------------------------------
 // q = 127 v / most, correctly rounded before it goes to an integer wherever the quotient is one of
 // float32's: a half, which values of 16 bits meet often, is then a half and goes to the even side.  (A product

@@ -316,12 +316,14 @@ __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) 
         for (int d = 0; d < DT; ++d) s[i] = mma(kk[i][d], q[d], s[i]);
       }
       bool odd = false;
+      wave_exchange();  // the step before has read its values
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int piece = i * 64 + lane;
         if (mixed) odd |= vv[i].odd();
         vv[i].store(values + piece / kPieces * V::kStride + 8 * (piece % kPieces));
       }
+      wave_exchange();
       const bool careful = mixed && __ballot(odd) != 0;
       if (step + kWaves < stop) fetch(step + kWaves);
 

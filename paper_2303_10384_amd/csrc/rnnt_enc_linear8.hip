@@ -208,11 +208,13 @@ struct HeldRows {
 #pragma unroll 1
       for (int r = 0; r < 16; r += kRowsAtOnce<T, NK>)
         quantize_rows_of_wave<T, NK, WHOLE>(x, m0 + 16 * pass + r, M, K, lds + r * kPitch, kPitch, scales + 16 * pass + r);
+      wave_exchange();
       if (((lane >> 4) & 1) == pass) {
 #pragma unroll
         for (int k = 0; k < 4 * NK; ++k)
           piece[k] = *reinterpret_cast<const i32x4*>(lds + (lane & 15) * kPitch + 32 * k + 16 * (lane >> 5));
       }
+      wave_exchange();  // the next sixteen rows take their place
     }
     scale = scales[lane & 31];
   }
@@ -357,6 +359,7 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
       }
 #pragma unroll
     for (int tile = 0; tile < kTiles; ++tile) finish(acc[tile], tile);
+    wave_exchange();  // the wave's own rows of results; the next turn's go there behind a barrier
 #pragma unroll
     for (int i = 0; i < kHeldRows / kRowsOnce; ++i) {
       T* to;
@@ -376,6 +379,7 @@ __global__ __launch_bounds__(64 * kHeldWaves, NK <= (sizeof(T) == 4 ? 5 : 7) ? 2
       product(acc, tile);
       finish(acc, tile);
     }
+    wave_exchange();
     const int left = l.N - n0 - c;
 #pragma unroll 1
     for (int i = 0; i < kHeldRows / kRowsOnce; ++i) {

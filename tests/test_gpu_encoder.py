@@ -881,3 +881,57 @@ def test_binding_refusals(torch, pkg):  # noqa: F811
     (g,) = torch.autograd.grad(y, leaf, torch.ones_like(y), create_graph=True)
     with pytest.raises(RuntimeError):
         torch.autograd.grad(g.sum(), leaf)
+
+
+# ---------------------------------------------------------------- values that lanes give one another
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [100, 256, 301, 512, 640, 767, 860, 1024])
+def test_linear8_of_whole_numbers(torch, pkg, K, dtype):  # noqa: F811
+    """Rows held in registers, of every width: with scales of 1 each result is a whole number, rounded once, and a row or a
+    piece of one in another's place is seen.  The product in float64 is exact."""
+    g = torch.Generator(device="cuda").manual_seed(K)
+    M, N = 2100, 331
+    x = torch.randint(-60, 61, (M, K), device="cuda", generator=g)
+    x[torch.arange(M, device="cuda"), torch.randint(0, K, (M,), device="cuda", generator=g)] = 127  # the scale is 1
+    w = pkg.quantize_rows(torch.cat([torch.randint(-126, 127, (N, K - 1), device="cuda", generator=g),
+                                     torch.full((N, 1), 127, device="cuda")], 1).float())
+    assert bool((w.scale == 1).all())
+    want = (x.double() @ w.values.double().t()).to(td(torch, dtype))
+    rows = pkg.quantize_rows(x.to(td(torch, dtype)))
+    assert torch.equal(rows.values.long(), x)
+    for _ in range(3):
+        assert torch.equal(pkg.linear8(x.to(td(torch, dtype)), w), want)
+        assert torch.equal(pkg.linear8(rows, w, dtype=td(torch, dtype)), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,L,cached", [(40, 5, 300), (64, 1, 777), (64, 16, 40), (128, 3, 2500), (200, 7, 130), (128, 150, 90), (64, 100, 900)])
+def test_attention_of_one_key(torch, pkg, D, L, cached, dtype):  # noqa: F811
+    """Every row's weights are 1 for one key, anywhere among those it sees, and 0 for the others: the row is that key's
+    value, to the bit, and a value in another's place is seen."""
+    g = torch.Generator(device="cuda").manual_seed(D + L)
+    B, H, page = 2, 2, 16
+    to, S = td(torch, dtype), cached + L
+    k = torch.where(torch.rand((B, S, H, D), device="cuda", generator=g) < 0.5, -1.0, 1.0)
+    v = torch.randint(-255, 256, (B, S, H, D), device="cuda", generator=g).float()
+    to_key = torch.randint(0, S, (B, L, H), device="cuda", generator=g)
+    pick = lambda t: torch.gather(t, 1, to_key[..., None].expand(-1, -1, -1, D))  # noqa: E731
+    # keys of random signs agree in at most D - 8 more places than not, so the others' scores are 8 * 4 * 8 lower
+    q = pick(k)
+    agree = torch.einsum("blhd,bshd->blsh", q.cpu(), k.cpu()).to("cuda")
+    agree.scatter_(2, to_key[:, :, None], -float(D))
+    assert float(agree.max()) <= D - 8
+    width = -(-S // page)
+    pages = torch.randperm(B * width, device="cuda", generator=g).view(B, width)
+    caches = []
+    for t in (k, v):
+        c = torch.zeros((B * width, H, page, D), dtype=to, device="cuda")
+        at = torch.arange(cached, device="cuda")
+        for b in range(B):
+            c[pages[b, at // page], :, at % page] = t[b, :cached].to(to)
+        caches.append(c)
+    args = [t.to(to).contiguous() for t in (4 * q, k[:, cached:], v[:, cached:])]
+    for _ in range(3):
+        out = pkg.cached_attention(*args, *caches, pages.to(torch.int32), ints(torch, [cached] * B), causal=False, scale=8.0)
+        assert torch.equal(out, pick(v).to(to))
