@@ -12,7 +12,8 @@
  * inputs or with one another; lens is (B) int32 or NULL (every row is valid), rows
  * behind a length are never used and are exactly 0 in every output, and a length
  * outside its range gives NaN in that utterance's outputs and zeros in its gradients;
- * arithmetic and sums are float32, rounded once to nearest even; workspaces as there.
+ * arithmetic and sums are float32, rounded once to nearest even, but for the attention's weights (below);
+ * workspaces as there.
  */
 #ifndef RNNT_ENCODER_MI355X_H
 #define RNNT_ENCODER_MI355X_H
@@ -149,6 +150,9 @@ rnnt_status_t rnnt_rotary(const void* x, rnnt_rotary_shape_t shape, const double
  * written.  lens[b] outside [0, L], or cached[b] outside [0, table * page - lens[b]], gives NaN in
  * that utterance's outputs, and nothing of it is written.
  * Keys and values that a query does not see do not reach it, whatever they hold.
+ * In the 16-bit types the weights p_j, before they are divided by their sum, are rounded to that type for their
+ * product with the values (in float16 scaled, so that one of 2^-26 of the row's largest keeps 2^-10 of itself); scores,
+ * maxima and sums are float32 in every type.
  *
  * RNNT_ERR_BAD_SHAPE: B, Hq, Hkv, D, page, table or num_pages < 1, L < 0, Hq no multiple of Hkv, a
  * stride below 0.  RNNT_ERR_BAD_VARIANT: scale not finite.  RNNT_ERR_ALIGNMENT: q, k or v not 16-byte

@@ -32,6 +32,18 @@ constexpr int kRowTile = 16;  // rows (tokens times the heads that share keys) t
 constexpr int kKeys = 32;     // keys to a wave's step
 constexpr int kWaves = 4;
 
+// Weights are rounded to the values' type for their product.  Float16 ends at 2^-24, and the many small weights of a long
+// cache beside one large one would end with it, while the sum that divides them has them whole: they are formed 2^kLift times
+// as large, in the product and the sum alike, which the quotient and the joins do not see.  The largest is 1 in the kernel
+// of sixteen rows; in the wide one up to 2^kLag, by which the maximum may lag behind.  65504 is the end on the other side.
+// (Weights of 2^-25.25 to 2^-26 beside one of 1: without the factor their share of the result is 0.)
+template <typename T>
+constexpr int kLift = __is_same(T, f16_t) ? 14 : 0;
+template <typename T>
+constexpr int kLag = __is_same(T, f16_t) ? 4 : 8;
+template <typename T>
+constexpr int kWideLift = __is_same(T, f16_t) ? 11 : 0;
+
 // ---- an utterance and its tile of rows ------------------------------------------
 // Row r of an utterance's head of keys is token r / G and query head h G + r % G.
 struct Tile {
@@ -348,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) 
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        w[j] = fast_exp2(w[j] - by);
+        w[j] = fast_exp2(w[j] - by) * static_cast<float>(1 << kLift<T>);
         sum += w[j];
       }
       if (!careful) {
@@ -590,17 +602,17 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
 #pragma unroll
         for (int e = 0; e < 16; ++e) most = __builtin_fmaxf(most, s[i][e]);
       most = halves_max(most);
-      // The maximum that the weights are taken against follows only where one of them would pass 2^8: its place does not
+      // The maximum that the weights are taken against follows only where one of them would pass 2^kLag: its place does not
       // matter to the quotient, and most steps spare the products with the sums so far.
       const float grown = __builtin_fmaxf(m, most);
-      if (__ballot((grown - m) * scale > 8.f || (m == kNegInf && grown > m))) {
+      if (__ballot((grown - m) * scale > static_cast<float>(kLag<T>) || (m == kNegInf && grown > m))) {
         const float shrink = m == kNegInf ? 0.f : fast_exp2((m - grown) * scale);
         sum *= shrink;
 #pragma unroll
         for (int c = 0; c < DT; ++c) acc[c] *= shrink;
         m = grown;
       }
-      const float by = m == kNegInf ? 0.f : m * scale;
+      const float by = m == kNegInf ? 0.f : m * scale - static_cast<float>(kWideLift<T>);
       // the values of channel 32 c + lane % 32 and the sixteen keys b of the step, of which the lane holds eight
       const auto column = [&](int c, int b) {
         Eight<T> a;

@@ -935,3 +935,36 @@ def test_attention_of_one_key(torch, pkg, D, L, cached, dtype):  # noqa: F811
     for _ in range(3):
         out = pkg.cached_attention(*args, *caches, pages.to(torch.int32), ints(torch, [cached] * B), causal=False, scale=8.0)
         assert torch.equal(out, pick(v).to(to))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("low,high", [(20, 26), (25.25, 26)])
+@pytest.mark.parametrize("B,L,at", [(1, 1, 5), (600, 1, 5), (600, 1, 9000), (1, 100, 5), (260, 100, 5), (260, 100, 9000)])
+def test_attention_of_many_small_weights(torch, pkg, B, L, at, low, high, dtype):  # noqa: F811
+    """One key takes nearly all of the weight and has value 0; 9984 others, of weights down to 2^-26 of its own, make the
+    result, in blocks that share them out and in one block.  Scores are exact, so a weight is off by the exponential's 2^-22, the
+    exponent's 2^-18 (26 bits, 2^-23 each) and half a step of the values' type, or a whole one below 2^-25 of the largest, however
+    many they are; besides there are float32's sums, of terms of one sign."""
+    g = torch.Generator(device="cuda").manual_seed(B + L + at)
+    N, D, page, to = 9984, 64, 64, td(torch, dtype)
+    bits = torch.randint(int(low * 8), high * 8 + 1, (N,), device="cuda", generator=g).double() / 8
+    bits[at] = 0
+    v = (torch.rand((N, D), device="cuda", generator=g) * 0.5 + 0.5).to(to)
+    v[at] = 0
+    k = torch.zeros((N, D), device="cuda", dtype=to)
+    k[:, 3] = -bits.to(to)
+    # all utterances read the same pages; their new tokens, whose keys are too far down to count, go to pages of their own
+    P, own = N // page, -(-L // page)
+    pages = torch.randperm(P, device="cuda", generator=g)
+    caches = [torch.zeros((P + B * own, 1, page, D), dtype=to, device="cuda") for _ in range(2)]
+    for c, t in zip(caches, (k, v)):
+        c[pages, 0] = t.view(P, page, D)
+    table = torch.cat([pages.expand(B, P), P + torch.arange(B * own, device="cuda").view(B, own)], 1).to(torch.int32)
+    q, new_k = torch.zeros((B, L, 2, D), device="cuda", dtype=to), torch.zeros((B, L, 1, D), device="cuda", dtype=to)
+    q[..., 3], new_k[..., 3] = 1, -200
+    out = pkg.cached_attention(q, new_k, torch.ones_like(new_k), *caches, table, ints(torch, [N] * B), scale=float(np.log(2.0)))
+    w = torch.exp2(-bits)
+    want = (w @ v.double()) / w.sum()
+    weights = 0.0 if dtype == "f32" else 2 * HALF[dtype]
+    tol = (HALF[dtype] + weights + 2.0 ** -18 + 2.0 ** -22 + (N + L) * ONE) * want + TINY[dtype]
+    assert bool(((out.double() - want).abs() <= tol).all()), (float((out.double() / want).min()), float((out.double() / want).max()))
