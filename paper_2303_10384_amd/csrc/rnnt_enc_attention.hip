@@ -472,6 +472,8 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
   const int rows = p.L * p.G, row0 = t.tile * p.rows, wave_row0 = row0 + wave * kWideRows;
 
   float m = kNegInf, sum = 0.f;  // the maximum before the scale
+  float by = 0.f;                // and after it, less the weights' factor
+  bool far = false;              // one of the wave's rows has a maximum past 2^10
   f32x16 acc[DT];
 #pragma unroll
   for (int c = 0; c < DT; ++c)
@@ -605,14 +607,25 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
       // The maximum that the weights are taken against follows only where one of them would pass 2^kLag: its place does not
       // matter to the quotient, and most steps spare the products with the sums so far.
       const float grown = __builtin_fmaxf(m, most);
-      if (__ballot((grown - m) * scale > static_cast<float>(kLag<T>) || (m == kNegInf && grown > m))) {
+      if (far || __ballot((grown - m) * scale > static_cast<float>(kLag<T>) || (m == kNegInf && grown > m))) {
         const float shrink = m == kNegInf ? 0.f : fast_exp2((m - grown) * scale);
         sum *= shrink;
 #pragma unroll
         for (int c = 0; c < DT; ++c) acc[c] *= shrink;
         m = grown;
+        by = m == kNegInf ? 0.f : m * scale - static_cast<float>(kWideLift<T>);
+        // A weight is 2^(s scale - by), the product exact and by rounded: past 2^24 its rounding alone would be several
+        // powers of two, and past 2^31 a weight of 1 infinity or 0.  There the difference comes first.
+        far = __ballot(__builtin_fabsf(by) > 1024.f) != 0;
+        if (far) {
+          const float top = m == kNegInf ? 0.f : m;
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[i][e] -= top;
+          by = -static_cast<float>(kWideLift<T>);
+        }
       }
-      const float by = m == kNegInf ? 0.f : m * scale - static_cast<float>(kWideLift<T>);
       // the values of channel 32 c + lane % 32 and the sixteen keys b of the step, of which the lane holds eight
       const auto column = [&](int c, int b) {
         Eight<T> a;
@@ -713,7 +726,7 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
   if (ends && row >= rows) return;
   const int token = row / p.G, head = t.h * p.G + row - token * p.G;
   const bool valid = t.state == 1 && token < t.n;
-  const float fill = t.state < 0 ? __builtin_nanf("") : 0.f, by = 1.f / sum;
+  const float fill = t.state < 0 ? __builtin_nanf("") : 0.f, over = 1.f / sum;
   T* out = static_cast<T*>(p.out) + ((static_cast<int64_t>(t.b) * p.L + token) * p.Hq + head) * p.D;
 #pragma unroll
   for (int c = 0; c < DT; ++c)
@@ -723,7 +736,7 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
       if (at >= p.D) continue;
       float v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = ends ? (valid ? acc[c][4 * e + j] * by : fill) : acc[c][4 * e + j];
+      for (int j = 0; j < 4; ++j) v[j] = ends ? (valid ? acc[c][4 * e + j] * over : fill) : acc[c][4 * e + j];
       if (ends) {
         Pack<T, 4> k;
         k.set(v);

@@ -968,3 +968,27 @@ def test_attention_of_many_small_weights(torch, pkg, B, L, at, low, high, dtype)
     weights = 0.0 if dtype == "f32" else 2 * HALF[dtype]
     tol = (HALF[dtype] + weights + 2.0 ** -18 + 2.0 ** -22 + (N + L) * ONE) * want + TINY[dtype]
     assert bool(((out.double() - want).abs() <= tol).all()), (float((out.double() / want).min()), float((out.double() / want).max()))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("L,G,cached", [(5, 1, 200), (100, 1, 200), (60, 2, 900)])
+@pytest.mark.parametrize("scale", [1.0, 0.37, -0.61])
+def test_attention_of_scores_of_billions(torch, pkg, L, G, cached, scale, dtype):  # noqa: F811
+    """Scores whose last digit in float32 stands for hundreds of powers of two: every row has one key far above the others, so its
+    weight is 1 and the row that key's value."""
+    g = torch.Generator(device="cuda").manual_seed(L)
+    D, page, to, S = 64, 16, td(torch, dtype), cached + L
+    k = torch.where(torch.rand((1, S, 1, D), device="cuda", generator=g) < 0.5, -1.0, 1.0)
+    v = torch.randint(-255, 256, (1, S, 1, D), device="cuda", generator=g).float()
+    to_key = torch.randint(0, S, (1, L, G), device="cuda", generator=g)
+    q = k[0, to_key[0], 0][None] * (1.0 if scale > 0 else -1.0)
+    width = -(-S // page)
+    pages = torch.arange(width, device="cuda", dtype=torch.int32)[None]
+    caches = []
+    for t in (5120 * k, v):
+        c = torch.zeros((width * page, D), dtype=to, device="cuda")
+        c[:cached] = t[0, :cached, 0].to(to)
+        caches.append(c.view(width, 1, page, D))
+    out = pkg.cached_attention((24576 * q).to(to), (5120 * k[:, cached:]).to(to), v[:, cached:].to(to), *caches, pages,
+                               ints(torch, [cached]), causal=False, scale=scale)
+    assert torch.equal(out, v[0, to_key[0], 0][None].to(to))
