@@ -84,12 +84,15 @@ __device__ __forceinline__ int row_state(const int32_t* lens, int64_t row, int L
   return static_cast<int>(row - static_cast<int64_t>(b) * L) < n;
 }
 
+// A launch takes fewer than 2^32 threads along x, and 2^24 rows of 1024 lanes are 2^34: from here on blocks go along y.
+constexpr int64_t kGridX = int64_t{1} << 21;
+
 template <typename T, int G, int NV, int MODE>
 __global__ __launch_bounds__(G > 256 ? G : 256) void enc_rows(RowsParams p) {
   constexpr int VEC = kVec<T>, kRows = G > 256 ? 1 : 256 / G;
   __shared__ float lds[2][G > 64 ? G / 64 : 1];
   const int lane = static_cast<int>(threadIdx.x) % G;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / G;
+  const int64_t row = (blockIdx.y * kGridX + blockIdx.x) * kRows + threadIdx.x / G;
   const bool there = row < p.rows;
   const int state = MODE == kQuantize ? there : there ? row_state(p.lens, row, p.L) : 0;
   const int64_t base = row * p.D;
@@ -352,9 +355,9 @@ rnnt_status_t launch_rows(const RowsParams& q, rnnt_dtype_t dtype, hipStream_t s
   return with_dtype(dtype, [&](auto t) {
     return with_layout(accesses_of(q.D, dtype), [&](auto lanes, auto n) {
       constexpr int G = decltype(lanes)::value, NV = decltype(n)::value;
-      const int64_t per = rows_of_block(G);
-      hipLaunchKernelGGL((enc_rows<decltype(t), G, NV, MODE>), dim3(static_cast<uint32_t>((q.rows + per - 1) / per)),
-                         dim3(G > 256 ? G : 256), 0, stream, q);
+      const int64_t per = rows_of_block(G), blocks = (q.rows + per - 1) / per, x = blocks < kGridX ? blocks : kGridX;
+      const dim3 grid(static_cast<uint32_t>(x), static_cast<uint32_t>((blocks + x - 1) / x));
+      hipLaunchKernelGGL((enc_rows<decltype(t), G, NV, MODE>), grid, dim3(G > 256 ? G : 256), 0, stream, q);
       return launched();
     });
   });

@@ -992,3 +992,24 @@ def test_attention_of_scores_of_billions(torch, pkg, L, G, cached, scale, dtype)
     out = pkg.cached_attention((24576 * q).to(to), (5120 * k[:, cached:]).to(to), v[:, cached:].to(to), *caches, pages,
                                ints(torch, [cached]), causal=False, scale=scale)
     assert torch.equal(out, v[0, to_key[0], 0][None].to(to))
+
+
+def test_rows_past_a_launch_along_x(torch, pkg):  # noqa: F811
+    """4194307 rows of a block of 1024 lanes each are more threads than a launch takes along x."""
+    n, D = (1 << 22) + 3, 8200
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 150 GiB of GPU memory")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    at = torch.tensor([0, (1 << 21) - 1, 1 << 21, (1 << 22) - 1, 1 << 22, n - 1], device="cuda")
+    x = torch.ones((n, D), dtype=torch.bfloat16, device="cuda")
+    x[at] = torch.randn((len(at), D), device="cuda", generator=g).bfloat16()
+    w = torch.ones((D,), dtype=torch.bfloat16, device="cuda")
+    for call in (pkg.quantize_rows, lambda t: pkg.rms_norm8(t, w)):
+        rows, few, one = call(x), call(x[at]), call(x[1:2])
+        assert torch.equal(rows.values[at], few.values) and torch.equal(rows.scale[at], few.scale)
+        assert int((rows.scale != one.scale).sum()) == len(at)  # and every other row is one of ones
+        del rows
+    y = pkg.rms_norm(x, w)
+    assert torch.equal(y[at], pkg.rms_norm(x[at], w)) and bool((y[2::999983] == y[1]).all())
+    del x, y
+    torch.cuda.empty_cache()
