@@ -22,6 +22,7 @@ from typing import NamedTuple
 import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from .binding import RNNT_ERR_UNSUPPORTED, RNNTError, _ptr, _result, _workspace_args, dtype_code, load_library
 from .network import _call, _check, _dense, _recorded
@@ -454,6 +455,8 @@ def cached_attention(q, k, v, k_cache, v_cache, pages, cached, lens=None, scale=
         out, ws = torch.empty_like(q), None
     _call(_library().rnnt_cached_attention, q.device, _ptr(q), _ptr(k), _ptr(v), shape, _ptr(lens), _ptr(cached), _ptr(pages),
           _ptr(k_cache), _ptr(v_cache), scale, _ptr(out), *_workspace_args(ws))
+    # autograd then refuses what it saved of the caches before the call, as after any write in place
+    increment_version((k_cache, v_cache))
     return out
 
 

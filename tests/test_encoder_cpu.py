@@ -396,3 +396,27 @@ def test_norm_gradient_of_tensors_saved_elsewhere(enc, calls):
             torch.autograd.grad(y, (x, w), torch.ones_like(y).transpose(0, 1).contiguous().transpose(0, 1))
         name, bwd = calls[-1]
         assert name == "rnnt_rms_norm_grad" and bwd[7] is None and bwd[6] is not None and (bwd[1] is None) == (residual is None)
+
+
+def test_autograd_sees_the_caches_written(enc, calls):
+    """A tensor that shares memory with a cache and was saved for a backward pass is refused there after a call."""
+    import paper_2303_10384_amd as rnnt
+    pool = torch.zeros(2, 6, 2, 16, 8)
+    pages, cached = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    q, k, v = torch.randn(2, 3, 4, 8), torch.randn(2, 3, 2, 8), torch.randn(2, 3, 2, 8)
+    attend = lambda *caches: rnnt.cached_attention(q, k, v, *caches, pages, cached)  # noqa: E731
+    for saved in (pool[0], pool[1], pool):
+        leaf = torch.ones_like(saved, requires_grad=True)
+        y = (leaf * saved).sum()
+        attend(pool[0], pool[1])
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.backward()
+    leaf, apart = torch.ones_like(q, requires_grad=True), torch.zeros(2, 6, 2, 16, 8)
+    y = (leaf * q).sum()  # the call's inputs are as they were
+    attend(apart[0], apart[1])
+    y.backward()
+    versions = [t._version for t in (q, k, v, pages, cached)]
+    with torch.inference_mode():  # caches without a counter
+        made = torch.zeros(2, 6, 2, 16, 8)
+        attend(made[0], made[1])
+    assert versions == [t._version for t in (q, k, v, pages, cached)]
