@@ -114,7 +114,7 @@ rnnt_status_t rnnt_linear8_dynamic(const void* x, const int8_t* w, const float* 
  * 2i + 1 (interleaved), or i and R/2 + i; channels from R on are copied.  start (B) int32 is
  * the position of an utterance's first token, or NULL (0); freq (R / 2) float64, radians a
  * position, 8-byte aligned: angles are formed and reduced in float64, so far positions keep
- * their digits.  inverse != 0 turns the other way, which is the gradient.
+ * their digits.  inverse != 0 turns the other way, which is the gradient: a length outside its range gives 0 there.
  * x may be a view with contiguous channels (strides in elements); y (B, L, H, D) is dense.
  *
  * RNNT_ERR_BAD_SHAPE: B < 1, L < 0, H < 1, D < 1, R odd or outside [2, D], or a stride below 0.

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void enc_rotary(RotaryParams p) {
     T* y = static_cast<T*>(p.y) + (row * p.H + h) * p.D;
     const int n = p.lens ? p.lens[b] : p.L;
     const bool bad = n < 0 || n > p.L, valid = !bad && t < n;
-    const float fill = bad ? __builtin_nanf("") : 0.f;
+    const float fill = bad && p.sign > 0.f ? __builtin_nanf("") : 0.f;  // gradients of a bad length are 0
     if (item < p.pair_items) {
       // the last eight pairs begin early, and write what they share with their neighbours twice alike
       const int count = min(half, 8), at = min(item * 8, half - count);

@@ -1013,3 +1013,18 @@ def test_rows_past_a_launch_along_x(torch, pkg):  # noqa: F811
     assert torch.equal(y[at], pkg.rms_norm(x[at], w)) and bool((y[2::999983] == y[1]).all())
     del x, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_gradient_of_bad_lengths(torch, pkg, interleaved, dtype):  # noqa: F811
+    """A length outside its range: NaN in the utterance's results and 0 in its gradient, as the other operators have it."""
+    x, xd = rounded(torch, rng_of(14).standard_normal((5, 3, 2, 21)), dtype)
+    x.requires_grad_(True)
+    freq, lens = pkg.rotary_frequencies(18), np.array([3, 4, -1, 2, -2**31])
+    y = pkg.rotary(x, freq, None, ints(torch, lens), interleaved=interleaved)
+    (dx,) = torch.autograd.grad(y, x, torch.ones_like(y))
+    assert bool(y[[1, 2, 4]].isnan().all()) and bool(y[[0, 3]].isfinite().all())
+    assert not bool(dx[[1, 2, 4]].any()) and not bool(dx[3, 2:].any())
+    want, size = R.rotary(np.ones(xd.shape), freq.cpu().numpy(), None, np.array([3, 0, 0, 2, 0]), interleaved, -1.0)
+    close(dx, want, HALF[dtype] * np.abs(want) + (2.0 ** -21 + 2 * ONE) * size + TINY[dtype] * (size > 0), "dx")
