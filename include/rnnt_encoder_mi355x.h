@@ -32,7 +32,8 @@ extern "C" {
  * (where residual is NULL it is not written, and may be NULL); y is formed from t before that
  * rounding.
  * Squares are summed in float32: a row whose squares pass its range (values of about 1e18)
- * gives 0 where the values are finite, as one that holds an infinity does.
+ * gives 0 where the values are finite, as one that holds an infinity does; with eps 0 one whose
+ * squares fall below it (values of about 1e-19) can give infinities, and one of zeros NaN.
  *
  * The gradient forms t again from x and residual, without the rounding of sum_out, and takes
  * the gradients dy and dsum (NULL: zero) of y and of sum_out:
@@ -60,9 +61,9 @@ rnnt_status_t rnnt_rms_norm_grad(const void* x, const void* residual, rnnt_norm_
 /* ---------------------------------------------------------------------------
  * Rows in 8 bits: signed integers and one float32 scale a row,
  *   scale = max |v| / 127,   q = v / scale to the nearest integer, ties to even,
- * so |q| <= 127 and the value is q * scale.  A row of zeros, or one whose largest value is
- * below 2^-100, has q = 0 and scale 0; one that holds an infinity or NaN has q = 0 and
- * scale NaN.  Row i begins at q + i * pitch (bytes, a multiple of 16 and at least D; q is
+ * so |q| <= 127 and the value is q * scale.  A row of zeros, or one whose largest value (in
+ * rnnt_rms_norm8 the largest t * weight) is below 2^-100, has q = 0 and scale 0; one that holds an infinity
+ * or NaN has q = 0 and scale NaN.  Row i begins at q + i * pitch (bytes, a multiple of 16 and at least D; q is
  * 16-byte aligned); the bytes behind the D first are not written.
  *
  * rnnt_quantize_rows: v = x, `rows` rows of D elements.  rnnt_rms_norm8: v = the norm's y

@@ -49,7 +49,7 @@ struct Quantizer {
   }
   // the scale of a row whose values are v * unit
   __device__ __forceinline__ static float scale(float m, float unit) {
-    if (m < 0x1p-100f) return 0.f;
+    if (m < 0x1p-100f && unit < __builtin_inff()) return 0.f;  // a norm of zeros without eps is 0 / 0
     const float s = m * unit * (1.f / 127.f);
     return s < __builtin_inff() && m < __builtin_inff() ? s : __builtin_nanf("");
   }

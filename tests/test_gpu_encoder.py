@@ -1028,3 +1028,16 @@ def test_rotary_gradient_of_bad_lengths(torch, pkg, interleaved, dtype):  # noqa
     assert not bool(dx[[1, 2, 4]].any()) and not bool(dx[3, 2:].any())
     want, size = R.rotary(np.ones(xd.shape), freq.cpu().numpy(), None, np.array([3, 0, 0, 2, 0]), interleaved, -1.0)
     close(dx, want, HALF[dtype] * np.abs(want) + (2.0 ** -21 + 2 * ONE) * size + TINY[dtype] * (size > 0), "dx")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [5, 40, 1025])
+def test_norm8_without_eps(torch, pkg, D, dtype):  # noqa: F811
+    """With eps 0 a row of zeros is 0 / 0: NaN in the norm, and a scale of NaN in 8 bits."""
+    x = torch.zeros((3, D), device="cuda", dtype=td(torch, dtype))
+    x[1] = 2
+    w = torch.ones((D,), device="cuda", dtype=td(torch, dtype))
+    y, rows = pkg.rms_norm(x, w, eps=0.0), pkg.rms_norm8(x, w, eps=0.0)
+    assert bool(y[0].isnan().all()) and bool((y[1] == 1).all())
+    assert bool(rows.scale[[0, 2]].isnan().all()) and not bool(rows.values[[0, 2]].any())
+    assert bool((rows.values[1] == 127).all()) and abs(float(rows.scale[1]) * 127 - 1) <= 4 * ONE
