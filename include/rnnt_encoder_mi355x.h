@@ -91,7 +91,7 @@ rnnt_status_t rnnt_rms_norm8(const void* x, const void* residual, rnnt_norm_shap
  * RNNT_ERR_BAD_SHAPE: M < 0, N < 1, K < 1, a pitch below K.  RNNT_ERR_ALIGNMENT: x or w in 8 bits not
  * 16-byte aligned, or a pitch that is no multiple of 16.  RNNT_ERR_UNSUPPORTED: K of 2^17 or more
  * (the sum could pass 32 bits), rnnt_linear8_dynamic with K > 32768 (16384 in float32), M of
- * 2^31 / 128 or more, N > 2^21, or a pitch of 2^20 or more.
+ * 2^31 / 128 or more, N > 2^21, 2^23 or more tiles of 128 x 128 results, or a pitch of 2^20 or more.
  */
 typedef struct {
   int32_t M, N, K;

@@ -420,3 +420,13 @@ def test_autograd_sees_the_caches_written(enc, calls):
         made = torch.zeros(2, 6, 2, 16, 8)
         attend(made[0], made[1])
     assert versions == [t._version for t in (q, k, v, pages, cached)]
+
+
+def test_linear8_limit_on_tiles(enc):
+    """2^23 - 1 tiles of 128 x 128 results are taken (and end at the next check), 2^23 are not."""
+    lib, S = enc._library(), enc.Linear8Shape
+    for M, N, want in ((511 * 128, 1 << 21, 1), (511 * 128 + 1, 1 << 21, 9), (8191 * 128, 1024 * 128, 1), (8191 * 128 + 1, 1024 * 128, 9),
+                       ((1 << 23) - 128, 127 * 128 + 1, 1), ((1 << 24) - 1, 63 * 128, 1), ((1 << 24) - 1, 64 * 128, 9)):
+        shape = S(M, N, 40, 1, 48, 48)
+        assert lib.rnnt_linear8(None, FAKE, FAKE, FAKE, shape, None, FAKE, None) == want, (M, N)
+        assert lib.rnnt_linear8_dynamic(None, FAKE, FAKE, shape, None, FAKE, None, 0, None) == want, (M, N)
