@@ -1041,3 +1041,121 @@ def test_norm8_without_eps(torch, pkg, D, dtype):  # noqa: F811
     assert bool(y[0].isnan().all()) and bool((y[1] == 1).all())
     assert bool(rows.scale[[0, 2]].isnan().all()) and not bool(rows.values[[0, 2]].any())
     assert bool((rows.values[1] == 127).all()) and abs(float(rows.scale[1]) * 127 - 1) <= 4 * ONE
+
+
+def test_product_in_8_bits_into_the_alignment(torch, pkg):  # noqa: F811
+    """The joint's hidden layer through the 8-bit product into forced alignment: logits against float64, and the path of those
+    logits against the oracle's."""
+    from oracle import network_ref as N
+    from oracle import rnnt_ref
+    from oracle import viterbi as VB
+    rng = rng_of(15)
+    B, T, U, H, V = 3, 9, 4, 40, 21
+    tl, ul = np.array([9, 6, 5]), np.array([4, 2, 0])
+    labels = rng.integers(1, V, size=(B, U))
+    enc, encd = rounded(torch, rng.standard_normal((B, T, H)), "bf16")
+    pred, predd = rounded(torch, rng.standard_normal((B, U + 1, H)), "bf16")
+    bias, biasd = rounded(torch, rng.standard_normal(V), "bf16")
+    w8 = pkg.quantize_rows(torch.from_numpy(2 * rng.standard_normal((V, H))).to("cuda").float())
+    hidden = pkg.joint_hidden(enc, pred, ints(torch, tl), ints(torch, ul), "tanh")
+    logits = pkg.linear8(hidden, w8, bias)
+    rows = pkg.quantize_rows(hidden)
+    y, size = R.linear8(rows.values.reshape(-1, H).cpu().numpy(), rows.scale.reshape(-1).double().cpu().numpy(),
+                        w8.values.cpu().numpy(), w8.scale.double().cpu().numpy(), biasd)
+    close(logits.reshape(-1, V), y, HALF["bf16"] * np.abs(y) + 4 * ONE * size, "logits")
+    # and the hidden layer itself, whose rows are 8 bits of it: half a step of each row's largest value, a bf16 rounding
+    want = N.joint_hidden(encd, predd, tl, ul, "tanh")
+    held = (rows.values.double() * rows.scale.double()[..., None]).cpu().numpy()
+    most = np.abs(want).max(-1, keepdims=True)
+    assert np.all(np.abs(held - want) <= (1 / 254 + 2 * HALF["bf16"]) * most + 1e-6)
+    score, frames, span = pkg.viterbi_align(logits, ints(torch, labels), ints(torch, tl), ints(torch, ul))
+    seen = logits.double().cpu().numpy()
+    for b in range(B):
+        z = seen[b, :tl[b], :ul[b] + 1]
+        _, blank, label = rnnt_ref.lattice_weights(z, labels[b, :ul[b]], 0)
+        best = VB.best_alignment(blank, label, "rnnt")
+        assert abs(float(score[b]) - best["score"]) <= 1e-5 * max(1.0, abs(best["score"]))
+        got = [int(f) for f in frames[b, :ul[b]]]
+        assert bool((frames[b, ul[b]:] == -1).all())
+        own = VB.alignment_score(blank, label, got, int(span[b, 0]), int(span[b, 1]), "rnnt")
+        assert abs(own - best["score"]) <= 1e-5 * max(1.0, abs(best["score"]))
+
+
+# tiles of 128 rows at every width of heads, and what a scale of 0 or below and a window do there; then tiles of 128 for 17 to 64
+# rows, where utterances are many
+WIDE = [  # B, L, Hq, Hkv, D, page, cached, lens, layout, options
+    (2, 75, 1, 1, 72, 16, [21, 60], [75, 70], "dense", {}),
+    (1, 71, 2, 1, 80, 8, [33], [69], "fused", {"left": 25}),
+    (2, 150, 1, 1, 80, 16, [0, 40], [150, 1], "fused", {"causal": False, "left": 30}),
+    (2, 70, 1, 1, 96, 16, [50, 3], [70, 67], "heads first", {"causal": False}),
+    (1, 37, 4, 2, 96, 32, [20], [37], "fused", {}),
+    (1, 130, 1, 1, 88, 16, [7], [129], "dense", {"left": 0}),
+    (2, 75, 2, 2, 64, 16, [40, 0], [75, 33], "dense", {"scale": 0.0}),
+    (2, 75, 2, 2, 64, 16, [40, 0], [75, 33], "fused", {"scale": -0.3}),
+    (1, 90, 2, 1, 128, 16, [35], [87], "fused", {"scale": -0.3, "left": 40}),
+    (1, 90, 1, 1, 32, 8, [35], None, "dense", {"scale": 0.0, "left": 17, "causal": False}),
+    (1, 80, 1, 1, 24, 16, [300], [80], "dense", {"scale": 0.9, "left": 100})]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", WIDE, ids=lambda c: "-".join(map(str, c[:6])))
+def test_attention_of_many_rows(torch, pkg, case, dtype):  # noqa: F811
+    B, L, Hq, Hkv, D, page, cached, lens, layout, options = case
+    cached, lens = np.array(cached), None if lens is None else np.array(lens)
+    new, newd, caches, cachesd, pages, _ = attention_case(torch, B, L, Hq, Hkv, D, page, cached, lens, dtype, B + L + D, layout)
+    check_attention(torch, pkg, new, newd, caches, cachesd, pages, cached, lens, dtype, **options)
+
+
+def check_on_gpu(torch, pkg, dtype, B, L, Hq, Hkv, D, page, cached, lens=None, spare=2, **kw):  # noqa: F811
+    """A call against float64 on the GPU; returns what it gave."""
+    cached = np.array(cached)
+    new, _, caches, _, pages, _ = attention_case(torch, B, L, Hq, Hkv, D, page, cached, lens, dtype, 3, spare=spare)
+    out = pkg.cached_attention(*new, *caches, ints(torch, pages), ints(torch, cached), ints(torch, lens), **kw)
+    tab, left, scale = torch.from_numpy(pages).to("cuda"), kw.get("left"), kw.get("scale", D ** -0.5)
+    for b in range(B):
+        n = L if lens is None else int(lens[b])
+        assert not bool(out[b, n:].any())
+        if not n:
+            continue
+        S = int(cached[b]) + n
+        j = torch.arange(S, device="cuda")
+        k, v = (c[tab[b, j // page], :, j % page].double().transpose(0, 1).repeat_interleave(Hq // Hkv, 0) for c in caches)
+        q, at = new[0][b, :n].double().transpose(0, 1), torch.arange(n, device="cuda")[:, None] + int(cached[b])
+        score = q @ k.transpose(1, 2).contiguous() * scale
+        hidden = (j > at) if kw.get("causal", True) else (j < 0).expand(n, S)
+        if left is not None:
+            hidden = hidden | (j < at - left)
+        w = torch.softmax(score.masked_fill(hidden, -np.inf), -1)
+        want, size = (w @ v).transpose(0, 1), (w @ v.abs()).transpose(0, 1)
+        score_size = (q.abs() @ k.abs().transpose(1, 2).contiguous()).amax(-1).transpose(0, 1)[..., None] * abs(scale)
+        want, size, score_size = (t.cpu().numpy() for t in (want, size, score_size))
+        close(out[b, :n], want, attention_tolerance(want, size, score_size, D, S, float(v.abs().max()), dtype), "out of %d" % b)
+    return out
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("L,D,options", [(20, 64, {}), (33, 40, {"causal": False}), (17, 96, {"left": 9}), (5, 128, {})])
+def test_attention_of_many_streams(torch, pkg, L, D, options, dtype):  # noqa: F811
+    """64 streams of 8 heads, some with no token: more tiles of sixteen rows than two to a CU, and waves that own no row."""
+    rng = rng_of(L)
+    lens, cached = rng.integers(0, L + 1, size=64), rng.integers(0, 60, size=64)
+    lens[:3] = 0, L, 1
+    check_on_gpu(torch, pkg, dtype, 64, L, 8, 8, D, 16, cached, lens, **options)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,L,Hq,Hkv,D,page,cached,lens,options", [
+    # two to eight blocks to a tile, and more; sixteen rows to a tile, and 128; the chunk's tokens see one another
+    (20, 3, 8, 4, 64, 16, [900] * 19 + [0], [3] * 18 + [0, 1], {"causal": False}),
+    (1, 5, 2, 1, 64, 32, [3000], None, {"causal": False, "left": 1500}),
+    (16, 100, 4, 4, 64, 16, [800] * 16, [100] * 15 + [37], {"causal": False}),
+    (1, 130, 2, 2, 80, 16, [2500], [127], {"causal": False, "left": 2000}),
+    # heads past 128 channels
+    (1, 1, 2, 1, 256, 64, [4000], None, {}), (1, 9, 4, 2, 200, 32, [3001], [7], {"causal": False}),
+    (20, 2, 4, 4, 256, 16, [1000] * 19 + [5], None, {}), (24, 3, 4, 4, 136, 16, [777] * 24, [3] * 23 + [0], {"left": 770}),
+    # many splits of tables far wider than what they hold
+    (1, 1, 4, 1, 64, 64, [80], None, {"spare": 900}), (3, 2, 2, 2, 128, 16, [0, 700, 31], [1, 2, 0], {"spare": 2000}),
+    (20, 1, 8, 4, 64, 16, [30] * 20, None, {"spare": 100, "causal": False}), (2, 100, 2, 2, 64, 16, [30, 0], [100, 3], {"spare": 800}),
+    (1, 2, 2, 1, 256, 16, [50], None, {"spare": 400})])
+def test_attention_keys_shared_out(torch, pkg, B, L, Hq, Hkv, D, page, cached, lens, options, dtype):  # noqa: F811
+    check_on_gpu(torch, pkg, dtype, B, L, Hq, Hkv, D, page, cached, None if lens is None else np.array(lens), **options)
