@@ -239,7 +239,7 @@ struct CacheWrite {
 // transposed, keys by rows, so that a lane holds one row's scores and the weights are already where the product with
 // the values takes them: group g's eight keys are 4 g + j and 16 + 4 g + j in both.  The waves' maxima, sums and
 // products meet in LDS, or, where a sequence is split among blocks, in memory.  One token of three sequences of 60013 keys,
-// 2 heads of 128 f16: 41 us (184 MB, 4.5 TB/s) and 5.5 for the join; 64 chunks of 16 tokens, 8 heads of 64 bf16, 256 keys
+// 2 heads of 128 f16: 39.5 us (184 MB, 4.7 TB/s; a step's pages are waited for before its rows are asked for) and 5.6 for the join; 64 chunks of 16 tokens, 8 heads of 64 bf16, 256 keys
 // before them: 14 us, most of it the way lengths -> page -> rows -> products -> join of blocks that have two steps to a wave.
 template <typename T, int DT>
 __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) {
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(64 * kWaves) void enc_attention(AttentionParams p) 
 // step ahead, their pages two) into LDS, for all four waves: sixteen rows to a block would read every key
 // eight times as often.  Products of 32 x 32 x 16, transposed as above; half g of a wave holds the keys 8 (e / 4) + 4 g + e % 4
 // of a group of 32, in the scores and in the values alike.  8 chunks of up to 1500 tokens over up to 1000, 16 heads on 4 of 128
-// bf16: 151 us, 0.57 PFLOP/s (sixteen rows to a block: 629).  The matrix units are busy for 26 % of the cycles, the vector units for 35 %
+// bf16: 153 us, 0.57 PFLOP/s (sixteen rows to a block: 629).  The matrix units are busy for 26 % of the cycles, the vector units for 35 %
 // (an exponential is four others), LDS for 21 %; two waves to a SIMD do not hide the waits between them.  A second buffer of rows with
 // one barrier to a step, and tiles ordered by length over all utterances, were no faster.
 constexpr int kWideRows = 32, kWideKeys = 64;
@@ -457,7 +457,8 @@ __global__ __launch_bounds__(64 * kWaves, DT <= 2 ? 3 : 2) void enc_attention_wi
   constexpr int kValueStride = 32 * DT + 32;                        // elements of a row of values in LDS
   // Four threads to a key, and every fourth piece of its row to each.  Piece c of a row of keys lies at c ^ swizzle(row): the
   // sixteen rows that are read at one piece meet all banks, and so do the four rows of four pieces that are written at
-  // once.  Rows of values begin 64 bytes of banks apart, for the same.
+  // once.  Rows of values begin 64 bytes of banks apart, for the same, at a DT of 2 and 4; at 1 every other one meets the same
+  // banks, and at 3 (72 to 96 channels) all do.
   const auto swizzle = [](int row) {
     if constexpr (kPitch == 16) return (row & 3) << 2 | (row >> 2 & 3);
     else if constexpr (kPitch == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);

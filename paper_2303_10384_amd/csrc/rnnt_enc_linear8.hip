@@ -43,7 +43,7 @@ __device__ __forceinline__ u32x4 load_bytes(const int8_t* row, int k, int K) {
 // Rows of any length, already in 8 bits: a tile of 128 x 128 results to a block, 64 x 64 to a wave.  Steps of 128 bytes of
 // k go through registers into two buffers of LDS in turn; the 16-byte pieces of a row lie at (piece ^ row % 8), so that the
 // 32 rows that a matrix instruction reads at one piece meet all banks.  For rows past kHeldMost alone: at K = 640 the two
-// launches, with x in 8 bits through memory between them, took 1969 us where the form below takes 810 (M = 648000).
+// launches, with x in 8 bits through memory between them, took 1969 us where the form below takes 800 (M = 648000).
 template <typename T>
 __global__ __launch_bounds__(256) void enc_linear8(Linear8Params p) {
   __shared__ u32x4 lds[2][2][kTile * kStep / 16];
@@ -173,8 +173,8 @@ __device__ __forceinline__ void quantize_rows_of_wave(const T* x, int64_t m0, in
 // For rows of up to 1024 a block of four waves keeps 128 rows of x, 32 to a wave, in registers in the matrix
 // instruction's order, and passes over its share of w, 64 rows at a time through LDS.  x is read once, whatever N is,
 // and taken to 8 bits on the way in, so no copy of it in 8 bits goes through memory; results go through LDS to whole runs of
-// a row.  648000 rows of 640 bf16 to 1025: 810 us, 1.05 POP/s and 2.7 TB/s, the product alone by the library 933.  The
-// matrix units are busy for 28 % of the cycles, LDS for 36 %, the vector units for 35 %, at about 1.9 GHz: without quantizing 190 us
+// a row.  648000 rows of 640 bf16 to 1025: 800 us, 1.06 POP/s and 2.7 TB/s, the product alone by the library 933.  The
+// matrix units are busy for 32 % of 1.30 million cycles, LDS for 43 %, the vector units for 41 %: without quantizing 190 us
 // less, without storing 190, without both 440 in all.  Tried, and no faster: 64 rows to a wave (half the reads of w, one wave to a
 // SIMD: 900 us, with a turn's results among the next one's products too), 32 rows of w to a turn and three blocks to a CU (890-1040),
 // half the blocks out of step with the others (815), results stored past the caches (1300).

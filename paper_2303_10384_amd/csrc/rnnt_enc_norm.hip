@@ -11,8 +11,8 @@ namespace {
 
 // A row is held by G lanes, in NV accesses of 16 bytes each, and read once: the sums need all of it before
 // anything can be written.  G is as small as the row allows, so that narrow rows share a wave.  Bound by memory: with a
-// residual, B=64 L=1000 D=1024 bf16 takes 73 us (458 MB, 6.3 TB/s), in 8 bits B=32 L=1500 D=640 44 us (188 MB, 4.3 TB/s: 80 of
-// 128 accesses of a row's lanes are there).
+// residual, B=64 L=1000 D=1024 bf16 takes 73 us (465 MB, 6.4 TB/s).  In 8 bits B=32 L=1500 D=640 takes 41 us (188 MB, 4.5
+// TB/s): 80 of 128 accesses of a row's lanes are there, and the vector units are busy for 87 % of the cycles.
 struct RowsParams {
   const void *x, *residual, *weight;
   void *y, *sum;
@@ -175,7 +175,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void enc_rows(RowsParams p) {
 // A block takes every gridDim.x-th group of rows and keeps the sums of dy t r over its rows in registers; they meet in
 // LDS and go out once, and enc_norm_join adds the blocks' up in their order.  t is added up again from x and the residual:
 // the stored sum's rounding, of the size of dweight's own, would make dweight's error half as large again (B=64 L=1000
-// D=1024 bf16: 2.6e-3 and 1.8e-3) for the 131 MB that are not read (99 and 120 us; 524 MB, 4.8 TB/s with 16 waves to a CU).
+// D=1024 bf16: 2.6e-3 and 1.8e-3) for the 101 MB that are not read (99 and 120 us; 536 MB, 4.5 TB/s with 16 waves to a CU,
+// 80 % of which wait: dsum is asked for only behind both sums of a row).  Past 8192 channels (4096 in float32) a block's
+// registers do not hold the row, and spill: 4000 rows of 16384 bf16 take 439 us.
 
 struct NormGradParams {
   const void *x, *residual, *weight, *dy, *dsum;

@@ -354,7 +354,8 @@ def rotary_frequencies(dim, base=10000.0, stretch=1.0, trained=None, slow=1.0, f
 
     For contexts `stretch` times the ones trained on, all of them are divided by stretch, or, with
     `trained` (tokens), those that turn at most `slow` times within the trained context; pairs that
-    turn `fast` times or more keep their frequency, and between the two it goes over linearly.
+    turn `fast` times or more keep their frequency, and between the two it goes over linearly: the
+    interpolation by parts of YaRN (Peng et al., ICLR 2024), without its factor on the scores.
     """
     if dim < 2 or dim % 2:
         raise ValueError("dim must be even and at least 2, got %r" % (dim,))
