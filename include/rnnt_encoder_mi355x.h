@@ -156,7 +156,7 @@ rnnt_status_t rnnt_rotary(const void* x, rnnt_rotary_shape_t shape, const double
  * maxima and sums are float32 in every type.
  *
  * RNNT_ERR_BAD_SHAPE: B, Hq, Hkv, D, page, table or num_pages < 1, L < 0, Hq no multiple of Hkv, a
- * stride below 0.  RNNT_ERR_BAD_VARIANT: scale not finite.  RNNT_ERR_ALIGNMENT: q, k or v not 16-byte
+ * stride below 0.  RNNT_ERR_BAD_VARIANT: scale times log2 e no finite float32.  RNNT_ERR_ALIGNMENT: q, k or v not 16-byte
  * aligned, or a stride that is no multiple of 16 bytes.  RNNT_ERR_UNSUPPORTED: D no multiple of 8 or above 256, page
  * no power of two or above 1024, a stride of k's or v's tokens of 2^31 or more, num_pages * Hkv * page or L * Hq of 2^31 or more, table * page + L of 2^30 or more,
  * or B * Hkv times the tiles of an utterance's L * (Hq / Hkv) rows (16 rows, or 128 where they are many) of 2^23 or

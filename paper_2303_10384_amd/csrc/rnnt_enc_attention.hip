@@ -930,7 +930,7 @@ rnnt_status_t rnnt_cached_attention(const void* q, const void* k, const void* v,
   const rnnt_attention_shape_t& s = shape;
   rnnt_status_t st = check(s);
   if (st != RNNT_OK) return st;
-  if (!__builtin_isfinite(scale)) return RNNT_ERR_BAD_VARIANT;
+  if (!__builtin_isfinite(scale * kLog2eF)) return RNNT_ERR_BAD_VARIANT;
   if (!cached || !pages || !k_cache || !v_cache || (s.L > 0 && (!q || !k || !v || !out))) return RNNT_ERR_NULL_PTR;
   if (!multiple_of(16, q) || !multiple_of(16, k) || !multiple_of(16, v) || !multiple_of(16, k_cache) ||
       !multiple_of(16, v_cache) || !multiple_of(net_elem_bytes(s.dtype), out))

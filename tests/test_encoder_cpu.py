@@ -430,3 +430,14 @@ def test_linear8_limit_on_tiles(enc):
         shape = S(M, N, 40, 1, 48, 48)
         assert lib.rnnt_linear8(None, FAKE, FAKE, FAKE, shape, None, FAKE, None) == want, (M, N)
         assert lib.rnnt_linear8_dynamic(None, FAKE, FAKE, shape, None, FAKE, None, 0, None) == want, (M, N)
+
+
+def test_attention_scale_past_float32_in_powers_of_two(enc):
+    """The kernels take scores in powers of two: a scale whose product with log2 e is no float32 is refused, the largest one
+    below goes on to the next check."""
+    lib = enc._library()
+    ok = enc.AttentionShape(*ATTENTION.values())
+    fwd = {"q": FAKE, "k": FAKE, "v": FAKE, "shape": ok, "lens": FAKE, "cached": FAKE, "pages": FAKE, "kc": FAKE, "vc": FAKE,
+           "scale": 0.5, "out": None, "ws": None, "bytes": 0, "stream": None}
+    for scale, want in ((2.3586e38, 1), (-2.3586e38, 1), (2.3587e38, 5), (-2.3587e38, 5), (3.4e38, 5)):
+        assert call(lib.rnnt_cached_attention, fwd, {"scale": scale}) == want, scale
